@@ -26,6 +26,16 @@ Functions keep the C names:
     softmax_copy_probe(x, out=None, stream=None) -> torch.Tensor
     softmax_strerror(code) -> str
     softmax_last_hip_error() -> int
+
+and those of attention.py, the attention of language models:
+
+    softmax_packed_attention(q, k, v, cu_q, ...) -> torch.Tensor, differentiable
+    softmax_packed_attention_fwd(q, k, v, cu_q, cu_k=None, ...) -> (o, lse)
+    softmax_packed_attention_bwd(dout, q, k, v, o, lse, cu_q, cu_k=None, ...)
+    softmax_paged_attention_fwd(q, k_cache, v_cache, block_table, cu_q, key_lens, ...)
+    softmax_cache_slots(context_lens, new_lens, block_table, free_blocks, free_count,
+                        total, block_size) -> dict
+    softmax_cache_append(k, v, k_cache, v_cache, slots)
 """
 from __future__ import annotations
 
@@ -40,6 +50,9 @@ __all__ = [
     "softmax_attention_fwd", "softmax_attention_fwd_ptr", "ATTN_MAX_KEYS", "ATTN_MAX_DIM",
     "softmax_exp_probe", "softmax_copy_probe", "softmax_strerror", "softmax_last_hip_error",
     "softmax_fwd_planned", "softmax_fwd_planned_ptr", "softmax_exchange_status",
+    "softmax_packed_attention", "softmax_packed_attention_fwd", "softmax_packed_attention_bwd",
+    "softmax_paged_attention_fwd", "softmax_cache_slots", "softmax_cache_append",
+    "HEADS_MAX_DIM",
     "CLIP_LO", "CLIP_MAX", "KERNEL_NAMES",
 ]
 
@@ -123,6 +136,7 @@ def load_library() -> ctypes.CDLL:
     u64p = ctypes.POINTER(ctypes.c_uint64)
     lib.softmax_exchange_status.argtypes = [u64p, u64p, ctypes.POINTER(ctypes.c_int32)]
     lib.softmax_exchange_status.restype = ctypes.c_int
+    attention.declare(lib)
     _lib = lib
     return lib
 
@@ -437,3 +451,9 @@ def softmax_copy_probe(x, out=None, stream=None):
     if rc != OK:
         raise SoftmaxError(rc, "softmax_copy_probe")
     return out
+
+
+from . import attention  # noqa: E402  (it uses the helpers above)
+from .attention import (  # noqa: E402,F401
+    HEADS_MAX_DIM, softmax_cache_append, softmax_cache_slots, softmax_packed_attention,
+    softmax_packed_attention_bwd, softmax_packed_attention_fwd, softmax_paged_attention_fwd)

@@ -1,0 +1,312 @@
+// C ABI of multi-head attention: argument checks and launches.
+// Declarations and contract: include/attention_mi355x.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "../../include/attention_mi355x.h"
+#include "sm_heads.hpp"
+#include "sm_heads_f32.hpp"
+#include "sm_heads_host.hpp"
+
+namespace {
+
+using namespace smx;
+using namespace smx_host;
+
+HeadsView view(const softmax_heads_t* t) { return {t->data, t->token_stride, t->head_stride}; }
+
+// Workgroup slots of tiles of T rows (sm_heads.hpp).
+int64_t tile_slots(int64_t rows, int64_t docs, int tile) { return rows / tile + docs + 1; }
+
+void set_shape(HeadsArgs* a, int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads,
+               int64_t d, int64_t docs, const softmax_score_t* s) {
+  a->tokens_q = static_cast<int>(tokens_q);
+  a->tokens_k = static_cast<int>(tokens_k);
+  a->heads = static_cast<int>(heads);
+  a->kv_heads = static_cast<int>(kv_heads);
+  a->group = static_cast<int>(heads / kv_heads);
+  a->d = static_cast<int>(d);
+  a->n = static_cast<int>(docs);
+  a->slopes = s->slopes;
+  a->prefix = s->prefix;
+  a->causal = s->causal;
+  a->scale = s->scale;
+  a->cap = s->cap;
+}
+
+// Sizes that a call's index arithmetic holds.
+bool sizes_ok(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t docs) {
+  return kv_heads > 0 && heads % kv_heads == 0 && docs >= 0 && docs < INT32_MAX / 4 &&
+         tokens <= INT32_MAX / std::max<int64_t>(heads, 1) &&
+         tile_slots(tokens * heads / kv_heads, docs, 16) <= INT32_MAX / kv_heads;
+}
+
+hipError_t launch2(const void* fn, int64_t x, int64_t y, int block, HeadsArgs* a, hipStream_t s) {
+  void* args[] = {a};
+  return hipLaunchKernel(fn, dim3(static_cast<uint32_t>(x), static_cast<uint32_t>(y)),
+                         dim3(block), args, 0, s);
+}
+
+// The instance of a head width: its columns padded to 64, 128 or 256.
+#define SMX_FOR_WIDTH(d, K, ...)                                            \
+  ((d) <= 64    ? reinterpret_cast<const void*>(&K<__VA_ARGS__, 64>)        \
+   : (d) <= 128 ? reinterpret_cast<const void*>(&K<__VA_ARGS__, 128>)       \
+                : reinterpret_cast<const void*>(&K<__VA_ARGS__, 256>))
+
+template <typename T, bool PAGED>
+const void* fwd_f32(int d) {
+  if (d <= 64) return reinterpret_cast<const void*>(&k_heads_fwd_f32<T, 64, PAGED>);
+  if (d <= 128) return reinterpret_cast<const void*>(&k_heads_fwd_f32<T, 128, PAGED>);
+  return reinterpret_cast<const void*>(&k_heads_fwd_f32<T, 256, PAGED>);
+}
+
+template <bool PAGED>
+const void* fwd_fn(int dtype, int d) {
+  return dtype == SOFTMAX_F32   ? fwd_f32<float, PAGED>(d)
+         : dtype == SOFTMAX_F16 ? fwd_f32<f16, PAGED>(d)
+                                : fwd_f32<bf16, PAGED>(d);
+}
+
+const void* dq_fn(int dtype, int d) {
+  return dtype == SOFTMAX_F32   ? SMX_FOR_WIDTH(d, k_heads_dq_f32, float)
+         : dtype == SOFTMAX_F16 ? SMX_FOR_WIDTH(d, k_heads_dq_f32, f16)
+                                : SMX_FOR_WIDTH(d, k_heads_dq_f32, bf16);
+}
+
+const void* dkv_fn(int dtype, int d) {
+  return dtype == SOFTMAX_F32   ? SMX_FOR_WIDTH(d, k_heads_dkv_f32, float)
+         : dtype == SOFTMAX_F16 ? SMX_FOR_WIDTH(d, k_heads_dkv_f32, f16)
+                                : SMX_FOR_WIDTH(d, k_heads_dkv_f32, bf16);
+}
+
+const void* join_fn(int dtype) {
+  return dtype == SOFTMAX_F32 ? reinterpret_cast<const void*>(&k_heads_join<float, kF32Rows>)
+         : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_heads_join<f16, kF32Rows>)
+                                : reinterpret_cast<const void*>(&k_heads_join<bf16, kF32Rows>);
+}
+
+// Splits of the keys to launch: enough that the call's tiles fill `target`
+// workgroups, no more than the longest request has chunks of, at most 64.
+constexpr int64_t kMaxSplits = 64;
+
+int64_t paged_splits(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t requests,
+                     int64_t max_keys, int64_t target) {
+  // Tiles that the requests have at least.
+  const int64_t rows = tokens * (heads / kv_heads);
+  const int64_t tiles = std::max<int64_t>(1, std::max(rows / kF32Rows, std::min(requests, tokens)));
+  const int64_t wanted = ceil_div(target, tiles * kv_heads);
+  return std::clamp<int64_t>(std::min(wanted, ceil_div(max_keys, kMinChunk)), 1, kMaxSplits);
+}
+
+int64_t split_bytes(int64_t splits, int64_t tokens, int64_t heads, int64_t d) {
+  return splits <= 1 ? 0 : splits * tokens * heads * (d + 2) * 4;
+}
+
+// Workgroups that fill the device: two per CU.
+int fill_target(int64_t* target) {
+  int dev = 0, cus = 0;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return fail_hip(e);
+  const int rc = device_cus(dev, &cus);
+  *target = 2 * cus;
+  return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+SOFTMAX_API int softmax_packed_attention_fwd(const softmax_heads_t* q, const softmax_heads_t* k,
+                                             const softmax_heads_t* v, void* o, float* lse,
+                                             const int32_t* cu_q, const int32_t* cu_k,
+                                             int64_t docs, const softmax_score_t* score,
+                                             int dtype, hipStream_t stream) {
+  const int size = dtype_size(dtype);
+  int64_t qb = 0, kb = 0, vb = 0;
+  if (size == 0 || !score_ok(score) || !heads_ok(q, size, &qb) || !heads_ok(k, size, &kb) ||
+      !heads_ok(v, size, &vb))
+    return SOFTMAX_ERR_INVALID_ARG;
+  if (k->tokens != v->tokens || k->heads != v->heads || k->d != v->d || q->d != k->d ||
+      !sizes_ok(q->tokens, q->heads, k->heads, docs) ||
+      !sizes_ok(k->tokens, q->heads, k->heads, docs) || !aligned16(o))
+    return SOFTMAX_ERR_INVALID_ARG;
+  if (qb == 0) return SOFTMAX_OK;
+  const int64_t rows = q->tokens * q->heads;
+  const Range inputs[] = {{q->data, qb},
+                          {k->data, kb},
+                          {v->data, vb},
+                          {cu_q, (docs + 1) * 4},
+                          {cu_k, (docs + 1) * 4},
+                          {score->slopes, score->slopes ? q->heads * 4 : 0},
+                          {score->prefix, score->prefix ? docs * 4 : 0}};
+  const Range outputs[] = {{o, rows * q->d * size}, {lse, rows * 4}};
+  const int rc = check_ranges(inputs, outputs);
+  if (rc != SOFTMAX_OK) return rc;
+  HeadsArgs a = {};
+  set_shape(&a, q->tokens, k->tokens, q->heads, k->heads, q->d, docs, score);
+  a.q = view(q);
+  a.k = view(k);
+  a.v = view(v);
+  a.out = o;
+  a.lse = lse;
+  a.cu_q = cu_q;
+  a.cu_k = cu_k;
+  const int64_t slots = tile_slots(q->tokens * a.group, docs, kF32Rows);
+  const hipError_t e =
+      launch2(fwd_fn<false>(dtype, a.d), slots * a.kv_heads, 1, kF32Threads, &a, stream);
+  return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
+}
+
+SOFTMAX_API int64_t softmax_packed_attention_bwd_workspace(int64_t tokens_q, int64_t heads) {
+  if (tokens_q < 0 || heads < 0 || (heads > 0 && tokens_q > INT32_MAX / heads)) return -1;
+  return tokens_q * heads * 4;
+}
+
+SOFTMAX_API int softmax_packed_attention_bwd(const softmax_heads_t* dout,
+                                             const softmax_heads_t* q, const softmax_heads_t* k,
+                                             const softmax_heads_t* v, const softmax_heads_t* o,
+                                             const float* lse, void* dq, void* dk, void* dv,
+                                             const int32_t* cu_q, const int32_t* cu_k,
+                                             int64_t docs, const softmax_score_t* score,
+                                             int dtype, void* workspace, int64_t workspace_bytes,
+                                             hipStream_t stream) {
+  const int size = dtype_size(dtype);
+  int64_t qb = 0, kb = 0, vb = 0, ob = 0, db = 0;
+  if (size == 0 || !score_ok(score) || !heads_ok(q, size, &qb) || !heads_ok(k, size, &kb) ||
+      !heads_ok(v, size, &vb) || !heads_ok(o, size, &ob) || !heads_ok(dout, size, &db))
+    return SOFTMAX_ERR_INVALID_ARG;
+  if (k->tokens != v->tokens || k->heads != v->heads || k->d != v->d || q->d != k->d ||
+      o->tokens != q->tokens || o->heads != q->heads || o->d != q->d ||
+      dout->tokens != q->tokens || dout->heads != q->heads || dout->d != q->d ||
+      !sizes_ok(q->tokens, q->heads, k->heads, docs) ||
+      !sizes_ok(k->tokens, q->heads, k->heads, docs) || !aligned16(dq) || !aligned16(dk) ||
+      !aligned16(dv) || !aligned16(workspace))
+    return SOFTMAX_ERR_INVALID_ARG;
+  const int64_t rows = q->tokens * q->heads, krows = k->tokens * k->heads;
+  const int64_t need = softmax_packed_attention_bwd_workspace(q->tokens, q->heads);
+  if (workspace_bytes < need) return SOFTMAX_ERR_INVALID_ARG;
+  if (rows == 0 && krows == 0) return SOFTMAX_OK;
+  const Range inputs[] = {{dout->data, db},
+                          {q->data, qb},
+                          {k->data, kb},
+                          {v->data, vb},
+                          {o->data, ob},
+                          {lse, rows * 4},
+                          {cu_q, (docs + 1) * 4},
+                          {cu_k, (docs + 1) * 4},
+                          {score->slopes, score->slopes ? q->heads * 4 : 0},
+                          {score->prefix, score->prefix ? docs * 4 : 0}};
+  const Range outputs[] = {{dq, rows * q->d * size},
+                           {dk, krows * k->d * size},
+                           {dv, krows * k->d * size},
+                           {workspace, need}};
+  const int rc = check_ranges(inputs, outputs);
+  if (rc != SOFTMAX_OK) return rc;
+  HeadsArgs a = {};
+  set_shape(&a, q->tokens, k->tokens, q->heads, k->heads, q->d, docs, score);
+  a.q = view(q);
+  a.k = view(k);
+  a.v = view(v);
+  a.o = view(o);
+  a.dout = view(dout);
+  a.out = dq;
+  a.dk = dk;
+  a.dv = dv;
+  a.lse = const_cast<float*>(lse);
+  a.delta = static_cast<float*>(workspace);
+  a.cu_q = cu_q;
+  a.cu_k = cu_k;
+  if (rows > 0) {
+    const int64_t slots = tile_slots(q->tokens * a.group, docs, kF32Rows);
+    const hipError_t e =
+        launch2(dq_fn(dtype, a.d), slots * a.kv_heads, 1, kF32Threads, &a, stream);
+    if (e != hipSuccess) return fail_hip(e);
+  }
+  if (krows > 0) {
+    const int64_t slots = tile_slots(k->tokens, docs, kF32Rows);
+    const hipError_t e =
+        launch2(dkv_fn(dtype, a.d), slots * a.kv_heads, 1, kF32Threads, &a, stream);
+    if (e != hipSuccess) return fail_hip(e);
+  }
+  return SOFTMAX_OK;
+}
+
+SOFTMAX_API int64_t softmax_paged_attention_workspace(int64_t tokens, int64_t heads,
+                                                      int64_t kv_heads, int64_t d,
+                                                      int64_t requests, int64_t max_keys) {
+  if (tokens < 0 || heads < 0 || d < 8 || d > SOFTMAX_HEADS_MAX_DIM || max_keys < 0 ||
+      !sizes_ok(tokens, heads, kv_heads, requests))
+    return -1;
+  int64_t target = 0;
+  if (fill_target(&target) != SOFTMAX_OK) return -1;
+  return split_bytes(paged_splits(tokens, heads, kv_heads, requests, max_keys, target), tokens,
+                     heads, d);
+}
+
+SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const softmax_cache_t* k,
+                                            const softmax_cache_t* v, const int32_t* block_table,
+                                            int64_t table_width, const int32_t* cu_q,
+                                            const int32_t* key_lens, int64_t requests,
+                                            const softmax_score_t* score, int dtype, void* o,
+                                            float* lse, void* workspace, int64_t workspace_bytes,
+                                            hipStream_t stream) {
+  const int size = dtype_size(dtype);
+  int64_t qb = 0, kb = 0, vb = 0;
+  if (size == 0 || !score_ok(score) || !heads_ok(q, size, &qb) || !cache_ok(k, size, &kb) ||
+      !cache_ok(v, size, &vb) || !same_cache(k, v) || q->d != k->d || table_width < 0 ||
+      table_width > INT32_MAX / k->block_size ||
+      !sizes_ok(q->tokens, q->heads, k->heads, requests) || !aligned16(o) ||
+      !aligned16(workspace))
+    return SOFTMAX_ERR_INVALID_ARG;
+  if (qb == 0) return SOFTMAX_OK;
+  int64_t target = 0;
+  int rc = fill_target(&target);
+  if (rc != SOFTMAX_OK) return rc;
+  const int64_t max_keys = table_width * k->block_size;
+  const int64_t splits =
+      paged_splits(q->tokens, q->heads, k->heads, requests, max_keys, target);
+  const int64_t need = split_bytes(splits, q->tokens, q->heads, q->d);
+  if (workspace_bytes < need) return SOFTMAX_ERR_INVALID_ARG;
+  const int64_t rows = q->tokens * q->heads;
+  const Range inputs[] = {{q->data, qb},
+                          {k->data, kb},
+                          {v->data, vb},
+                          {block_table, requests * table_width * 4},
+                          {cu_q, (requests + 1) * 4},
+                          {key_lens, requests * 4},
+                          {score->slopes, score->slopes ? q->heads * 4 : 0},
+                          {score->prefix, score->prefix ? requests * 4 : 0}};
+  const Range outputs[] = {
+      {o, rows * q->d * size}, {lse, lse ? rows * 4 : 0}, {workspace, need}};
+  rc = check_ranges(inputs, outputs);
+  if (rc != SOFTMAX_OK) return rc;
+  HeadsArgs a = {};
+  set_shape(&a, q->tokens, 0, q->heads, k->heads, q->d, requests, score);
+  a.q = view(q);
+  a.k = {k->data, k->token_stride, k->head_stride};
+  a.v = {v->data, v->token_stride, v->head_stride};
+  a.k_bs = k->block_stride;
+  a.v_bs = v->block_stride;
+  a.blocks = k->blocks;
+  a.max_keys = max_keys;
+  a.width = static_cast<int>(table_width);
+  a.log_block = log2_of(k->block_size);
+  a.table = block_table;
+  a.out = o;
+  a.lse = lse;
+  a.cu_q = cu_q;
+  a.cu_k = key_lens;
+  a.splits = static_cast<int>(splits);
+  a.target = static_cast<int>(target);
+  a.part_o = static_cast<float*>(workspace);
+  a.part_ml = a.part_o + splits * rows * q->d;
+  const int64_t slots = tile_slots(q->tokens * a.group, requests, kF32Rows);
+  hipError_t e =
+      launch2(fwd_fn<true>(dtype, a.d), slots * a.kv_heads, splits, kF32Threads, &a, stream);
+  if (e == hipSuccess && splits > 1)
+    e = launch2(join_fn(dtype), ceil_div(rows, 4), 1, 256, &a, stream);
+  return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
+}
+
+}  // extern "C"

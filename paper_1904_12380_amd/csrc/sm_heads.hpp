@@ -1,0 +1,207 @@
+// What the kernels of multi-head attention share (include/attention_mi355x.h
+// has the operation): their arguments, the map from workgroups to documents,
+// addresses of rows, and the scores.
+//
+// Rows.  The query heads that share a key/value head are packed as rows: row
+// r of a document is the token r / G and the head hk G + r % G of the group
+// of G.  A tile of rows then reads each key and value once for the whole
+// group, and single tokens still fill a part of a tile.
+//
+// Documents.  Their lengths are device data, so the host launches for the
+// largest number of tiles that any lengths could need: with documents that
+// start at the rows s(b), the tiles of T rows of document b take the
+// workgroup slots from floor(s(b) / T) + b on.  Slots of different documents
+// never meet: floor((s + l) / T) + 1 >= floor(s / T) + ceil(l / T).  A slot's
+// document is the last whose first slot is not past it, found by 64-way
+// search (one step for up to 64 documents).  Tokens past the last document
+// are a document of their own, without keys.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "sm_device.hpp"
+
+namespace smx {
+
+typedef _Float16 f16;
+typedef __bf16 bf16;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kLog2eF = 0x1.715476p+0f;
+constexpr float kLn2F = 0x1.62e430p-1f;
+
+// Rows of a tensor [tokens, heads, d].
+struct HeadsView {
+  const void* data;
+  int64_t ts, hs;  // strides in elements between tokens and heads
+};
+
+struct HeadsArgs {
+  HeadsView q, k, v, o, dout;
+  void* out;         // o of the forward pass, or dq
+  void* dk;
+  void* dv;
+  float* lse;        // written by the forward pass (may be null), read by the backward
+  float* delta;      // D of every query row (backward)
+  const int* cu_q;   // [n + 1]
+  const int* cu_k;   // [n + 1]; paged: key_lens [n]
+  const float* slopes;
+  const int* prefix;
+  // Paged cache.
+  const int* table;
+  int64_t k_bs, v_bs;  // strides between blocks
+  int64_t blocks;
+  int64_t max_keys;    // table width times block size
+  int width, log_block;
+  // Splits of the keys (paged).
+  float* part_o;       // [splits, tokens, heads, d]
+  float* part_ml;      // [splits, tokens, heads, 2]
+  int splits;
+  int target;          // workgroups that fill the device
+  int n, tokens_q, tokens_k, heads, kv_heads, group, d;
+  int causal;
+  float scale, cap;
+};
+
+__device__ __forceinline__ int clamp_i(int x, int lo, int hi) {
+  return x < lo ? lo : (x > hi ? hi : x);
+}
+
+// First token of document b of n (sums in cu, clamped); b == n: the tokens
+// past the last document.
+__device__ __forceinline__ int doc_start(const int* cu, int b, int tokens) {
+  return b == 0 ? 0 : clamp_i(cu[b], 0, tokens);
+}
+
+// A document and one of its tiles.
+struct DocTile {
+  int b;        // document, n for the tokens past the last
+  int q0, lq;   // its queries
+  int k0, lk;   // its keys (paged: k0 = 0)
+  int prefix;   // keys that every query sees
+  int tile;     // tile of the document
+};
+
+// The last of 0 .. n whose base is at most t (base(0) <= t, not falling).
+template <typename F>
+__device__ __forceinline__ int last_at_most(int n, int t, F base) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int step = (hi - lo) / 64 + 1;
+    const int b = lo + static_cast<int>(__lane_id()) * step;
+    const uint64_t at = __ballot(b <= hi && base(min(b, hi)) <= t);
+    const int count = at == 0 ? 1 : 64 - __builtin_clzll(at);
+    lo = lo + (count - 1) * step;
+    if (step == 1) break;
+    hi = min(hi, lo + step - 1);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// The document of slot t, where the documents' rows are `group` per token and
+// a tile has T of them.
+template <int T>
+__device__ __forceinline__ int find_doc(const int* cu, int n, int tokens, int group, int t,
+                                        int* tile) {
+  auto base = [&](int b) {
+    return static_cast<int>(static_cast<int64_t>(doc_start(cu, b, tokens)) * group / T) + b;
+  };
+  const int b = last_at_most(n, t, base);
+  *tile = __builtin_amdgcn_readfirstlane(t - base(b));
+  return b;
+}
+
+// The document of a token.
+__device__ __forceinline__ int find_doc_of_token(const int* cu, int n, int tokens, int token) {
+  return last_at_most(n, token, [&](int b) { return doc_start(cu, b, tokens); });
+}
+
+template <bool PAGED>
+__device__ __forceinline__ void doc_keys(const HeadsArgs& a, DocTile* w) {
+  const int b = w->b;
+  if (b >= a.n) {
+    w->k0 = 0;
+    w->lk = 0;
+  } else if constexpr (PAGED) {
+    w->k0 = 0;
+    w->lk = static_cast<int>(min(static_cast<int64_t>(max(a.cu_k[b], 0)), a.max_keys));
+  } else {
+    w->k0 = doc_start(a.cu_k, b, a.tokens_k);
+    w->lk = max(doc_start(a.cu_k, b + 1, a.tokens_k) - w->k0, 0);
+  }
+  w->prefix = a.prefix != nullptr && b < a.n ? clamp_i(a.prefix[b], 0, w->lk) : 0;
+}
+
+__device__ __forceinline__ void doc_queries(const HeadsArgs& a, DocTile* w) {
+  w->q0 = doc_start(a.cu_q, w->b, a.tokens_q);
+  const int end = w->b >= a.n ? a.tokens_q : doc_start(a.cu_q, w->b + 1, a.tokens_q);
+  w->lq = max(end - w->q0, 0);
+}
+
+// Keys that the query `tok` of a document sees: those before this one.
+__device__ __forceinline__ int keys_seen(const HeadsArgs& a, const DocTile& w, int tok) {
+  if (!a.causal) return w.lk;
+  return clamp_i(max(tok + w.lk - w.lq + 1, w.prefix), 0, w.lk);
+}
+
+// Splits of the keys (paged).  All chunks of a call have the same length: the
+// keys of all of its tiles of ROWS rows over the workgroups that fill the
+// device, in whole tiles of 64 keys, at least kMinChunk, and such that the
+// longest request fits the launched splits.  0: not split.  Every wavefront of
+// a call computes the same from the lengths.
+constexpr int kMinChunk = 256;
+
+template <int ROWS>
+__device__ __forceinline__ int split_chunk(const HeadsArgs& a) {
+  if (a.splits <= 1) return 0;
+  int64_t sum = 0, longest = 0;
+  for (int b = static_cast<int>(__lane_id()); b < a.n; b += 64) {
+    const int64_t lk = min(static_cast<int64_t>(max(a.cu_k[b], 0)), a.max_keys);
+    const int lq = doc_start(a.cu_q, b + 1, a.tokens_q) - doc_start(a.cu_q, b, a.tokens_q);
+    if (lq <= 0) continue;
+    sum += lk * ((lq * a.group + ROWS - 1) / ROWS);
+    longest = max(longest, lk);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    sum += __shfl_xor(sum, o);
+    longest = max(longest, __shfl_xor(longest, o));
+  }
+  int64_t chunk = (sum * a.kv_heads + a.target - 1) / a.target;
+  chunk = max(chunk, (longest + a.splits - 1) / a.splits);
+  chunk = max((chunk + 63) / 64 * 64, static_cast<int64_t>(kMinChunk));
+  return chunk >= longest ? 0 : static_cast<int>(chunk);
+}
+
+// Keys [from, to) of split `split` of a tile that sees the first `end`; false
+// past its last split (a tile without keys has one).
+__device__ __forceinline__ bool split_range(int end, int chunk, int split, int* from, int* to) {
+  *from = 0;
+  *to = end;
+  if (chunk == 0) return split == 0;
+  if (split > 0 && split * static_cast<int64_t>(chunk) >= end) return false;
+  *from = split * chunk;
+  *to = min(end, *from + chunk);
+  return true;
+}
+
+// Key j of request b in a paged cache: its element offset, or -1 where the
+// table holds no block of the cache.
+__device__ __forceinline__ int64_t paged_row(const HeadsArgs& a, int b, int j, int64_t bs,
+                                             int64_t ts) {
+  const int id = a.table[static_cast<int64_t>(b) * a.width + (j >> a.log_block)];
+  if (id < 0 || id >= a.blocks) return -1;
+  return id * bs + (j & ((1 << a.log_block) - 1)) * ts;
+}
+
+__device__ __forceinline__ float group4_max(float v) {  // over lanes l % 16
+  v = fmaxf(v, row16_partner(v));
+  return fmaxf(v, half32_partner(v));
+}
+__device__ __forceinline__ float group4_sum(float v) {
+  v = v + row16_partner(v);
+  return v + half32_partner(v);
+}
+
+}  // namespace smx

@@ -1,0 +1,436 @@
+// Multi-head attention with all products on the fp32 matrix cores.
+//
+// v_mfma_f32_16x16x4f32 takes A[16][4] and B[4][16]: lane l holds A at row
+// l % 16, column l / 16, B at row l / 16, column l % 16, and D at column
+// l % 16, rows 4 (l / 16) + i.  With scores transposed, S^T = K Q^T, a lane
+// holds one query's scores of the keys 4 (l / 16) + i: the softmax is
+// lane-local but for two exchanges, and S^T register i is the B operand of
+// the value product O^T += V^T P^T at the keys {i, 4 + i, 8 + i, 12 + i},
+// without a move.  The gradients work the same way: with S^T and dP^T = V
+// dO^T, dQ^T += K^T dS^T; with keys as columns, S = Q K^T and dP = dO V^T,
+// dV^T += dO^T P and dK^T += Q^T dS.
+//
+// A workgroup of four wavefronts takes 64 rows (16 each, operands in
+// registers) against tiles of 32 keys (or 64 keys against tiles of 32 rows),
+// staged as fp32 in LDS, whose rows are 4 floats longer than a row so that 16
+// rows read at one column spread over the banks.
+#pragma once
+
+#include "sm_heads.hpp"
+
+namespace smx {
+
+constexpr int kF32Rows = 64;   // rows (or keys) of a workgroup
+constexpr int kF32Step = 32;   // keys (or rows) of a staged tile
+constexpr int kF32Threads = 256;
+
+template <typename T>
+__device__ __forceinline__ f32x4 load4(const T* p) {
+  if constexpr (sizeof(T) == 4) {
+    return *reinterpret_cast<const f32x4*>(p);
+  } else {
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    const t4 v = *reinterpret_cast<const t4*>(p);
+    return f32x4{static_cast<float>(v[0]), static_cast<float>(v[1]), static_cast<float>(v[2]),
+                 static_cast<float>(v[3])};
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, f32x4 v) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<f32x4*>(p) = v;
+  } else {
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<t4*>(p) = t4{static_cast<T>(v[0]), static_cast<T>(v[1]),
+                                   static_cast<T>(v[2]), static_cast<T>(v[3])};
+  }
+}
+
+__device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+// The score of a dot product, and the derivative of its cap.
+__device__ __forceinline__ float score_f32(const HeadsArgs& a, float dot, float slope, int dist,
+                                           float* dcap) {
+  float x = dot * a.scale;
+  *dcap = 1.0f;
+  if (a.cap > 0.0f) {
+    const float t = tanhf(x / a.cap);
+    x = a.cap * t;
+    *dcap = 1.0f - t * t;
+  }
+  return x - slope * static_cast<float>(abs(dist));
+}
+
+// One row (of 16) of a register operand: element 4 t + j of the lane is
+// column 16 t + 4 (l / 16) + j of the row, 0 past d.
+template <typename T, int DP>
+__device__ __forceinline__ void load_row(f32x4 (&r)[DP / 16], const T* row, bool valid, int g,
+                                         int d) {
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) {
+    const int c = 16 * t + 4 * g;
+    r[t] = valid && c < d ? load4(row + c) : f32x4{0, 0, 0, 0};
+  }
+}
+
+// Rows of a staged tile against the lane's row: D[row of the tile][lane row].
+template <int DP>
+__device__ __forceinline__ f32x4 tile_dot(const float (*tile)[DP + 4], int row0,
+                                          const f32x4 (&r)[DP / 16], int c, int g) {
+  f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(&tile[row0 + c][16 * t + 4 * g]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = mfma4(x[j], r[t][j], s);
+  }
+  return s;
+}
+
+// acc[column of the tile][lane row] += tile^T w, for the tile's rows row0 +
+// 4 (l / 16) + i with the weights w[i].
+template <int DP>
+__device__ __forceinline__ void tile_accumulate(f32x4 (&acc)[DP / 16],
+                                                const float (*tile)[DP + 4], int row0, f32x4 w,
+                                                int c, int g) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t)
+      acc[t] = mfma4(tile[row0 + 4 * g + i][16 * t + c], w[i], acc[t]);
+  }
+}
+
+template <typename T, int DP, bool PAGED>
+__global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
+  __shared__ __attribute__((aligned(16))) float ks[kF32Step][DP + 4];
+  __shared__ __attribute__((aligned(16))) float vs[kF32Step][DP + 4];
+  __shared__ int held[kF32Step];
+  const int hk = blockIdx.x % a.kv_heads;
+  const int slot = static_cast<int>(gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads);
+  const int split = blockIdx.y;
+  DocTile w;
+  w.b = find_doc<kF32Rows>(a.cu_q, a.n, a.tokens_q, a.group, slot, &w.tile);
+  doc_queries(a, &w);
+  doc_keys<PAGED>(a, &w);
+  const int rows = w.lq * a.group;
+  if (w.tile * kF32Rows >= rows) return;
+  const int chunk = PAGED ? split_chunk<kF32Rows>(a) : 0;
+
+  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
+  const int c = lane % 16, g = lane / 16;
+  const int row = w.tile * kF32Rows + 16 * wave + c;
+  const bool valid = row < rows;
+  const int tok = valid ? row / a.group : w.lq - 1;
+  const int head = hk * a.group + (valid ? row % a.group : 0);
+  const int pos = tok + w.lk - w.lq;
+  const int lim = valid ? keys_seen(a, w, tok) : 0;
+  const int last_tok = (min(rows, (w.tile + 1) * kF32Rows) - 1) / a.group;
+  int from, to;
+  if (!split_range(keys_seen(a, w, last_tok), chunk, split, &from, &to)) return;
+  const float slope = a.slopes != nullptr ? a.slopes[head] : 0.0f;
+  const int64_t token = w.q0 + tok;
+
+  f32x4 q[DP / 16];
+  load_row<T, DP>(q, static_cast<const T*>(a.q.data) + token * a.q.ts + head * a.q.hs, valid, g,
+                  a.d);
+  f32x4 acc[DP / 16] = {};
+  float m = -INFINITY, l = 0.0f;
+
+  for (int k0 = from; k0 < to; k0 += kF32Step) {
+    __syncthreads();
+    for (int i = tid; i < kF32Step * (DP / 4); i += kF32Threads) {
+      const int r = i / (DP / 4), col = 4 * (i % (DP / 4)), j = k0 + r;
+      f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+      bool have = j < to;
+      if (have) {
+        int64_t kr, vr;
+        if constexpr (PAGED) {
+          kr = paged_row(a, w.b, j, a.k_bs, a.k.ts);
+          vr = paged_row(a, w.b, j, a.v_bs, a.v.ts);
+          have = kr >= 0;
+        } else {
+          kr = static_cast<int64_t>(w.k0 + j) * a.k.ts;
+          vr = static_cast<int64_t>(w.k0 + j) * a.v.ts;
+        }
+        if (have && col < a.d) {
+          x = load4(static_cast<const T*>(a.k.data) + kr + hk * a.k.hs + col);
+          y = load4(static_cast<const T*>(a.v.data) + vr + hk * a.v.hs + col);
+        }
+      }
+      *reinterpret_cast<f32x4*>(&ks[r][col]) = x;
+      *reinterpret_cast<f32x4*>(&vs[r][col]) = y;
+      if (col == 0) held[r] = have;
+    }
+    __syncthreads();
+    f32x4 s[2];
+    float top = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      s[kt] = tile_dot<DP>(ks, 16 * kt, q, c, g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 16 * kt + 4 * g + i, j = k0 + r;
+        float dcap;
+        const float x = score_f32(a, s[kt][i], slope, pos - j, &dcap);
+        s[kt][i] = j < lim && held[r] ? x : -INFINITY;
+        top = fmaxf(top, s[kt][i]);
+      }
+    }
+    const float next = fmaxf(m, group4_max(top));
+    const float base = next == -INFINITY ? 0.0f : next;
+    const float alpha = __builtin_amdgcn_exp2f((m - base) * kLog2eF);
+    m = next;
+    float part = 0.0f;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[kt][i] = __builtin_amdgcn_exp2f((s[kt][i] - base) * kLog2eF);
+        part += s[kt][i];
+      }
+    }
+    l = l * alpha + group4_sum(part);
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) acc[t] *= alpha;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) tile_accumulate<DP>(acc, vs, 16 * kt, s[kt], c, g);
+  }
+
+  if (!valid) return;
+  const int64_t out = token * a.heads + head;
+  if (chunk > 0) {
+    const int64_t at = split * static_cast<int64_t>(a.tokens_q) * a.heads + out;
+    if (g == 0) {
+      a.part_ml[2 * at] = m;
+      a.part_ml[2 * at + 1] = l;
+    }
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t)
+      if (16 * t + 4 * g < a.d)
+        *reinterpret_cast<f32x4*>(a.part_o + at * a.d + 16 * t + 4 * g) = acc[t];
+    return;
+  }
+  const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
+  if (g == 0 && a.lse != nullptr)
+    a.lse[out] = m == -INFINITY ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2F;
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t)
+    if (16 * t + 4 * g < a.d)
+      store4(static_cast<T*>(a.out) + out * a.d + 16 * t + 4 * g, acc[t] * inv);
+}
+
+// D of every row and the gradient of the queries.
+template <typename T, int DP>
+__global__ __launch_bounds__(kF32Threads) void k_heads_dq_f32(HeadsArgs a) {
+  __shared__ __attribute__((aligned(16))) float ks[kF32Step][DP + 4];
+  __shared__ __attribute__((aligned(16))) float vs[kF32Step][DP + 4];
+  const int hk = blockIdx.x % a.kv_heads;
+  const int slot = static_cast<int>(gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads);
+  DocTile w;
+  w.b = find_doc<kF32Rows>(a.cu_q, a.n, a.tokens_q, a.group, slot, &w.tile);
+  doc_queries(a, &w);
+  doc_keys<false>(a, &w);
+  const int rows = w.lq * a.group;
+  if (w.tile * kF32Rows >= rows) return;
+
+  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
+  const int c = lane % 16, g = lane / 16;
+  const int row = w.tile * kF32Rows + 16 * wave + c;
+  const bool valid = row < rows;
+  const int tok = valid ? row / a.group : w.lq - 1;
+  const int head = hk * a.group + (valid ? row % a.group : 0);
+  const int pos = tok + w.lk - w.lq;
+  const int lim = valid ? keys_seen(a, w, tok) : 0;
+  const int to = keys_seen(a, w, (min(rows, (w.tile + 1) * kF32Rows) - 1) / a.group);
+  const float slope = a.slopes != nullptr ? a.slopes[head] : 0.0f;
+  const int64_t token = w.q0 + tok, out = token * a.heads + head;
+
+  f32x4 q[DP / 16], dout[DP / 16];
+  load_row<T, DP>(q, static_cast<const T*>(a.q.data) + token * a.q.ts + head * a.q.hs, valid, g,
+                  a.d);
+  load_row<T, DP>(dout, static_cast<const T*>(a.dout.data) + token * a.dout.ts + head * a.dout.hs,
+                  valid, g, a.d);
+  float delta = 0.0f;
+  {
+    f32x4 o[DP / 16];
+    load_row<T, DP>(o, static_cast<const T*>(a.o.data) + token * a.o.ts + head * a.o.hs, valid, g,
+                    a.d);
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) delta = __builtin_fmaf(o[t][j], dout[t][j], delta);
+    delta = group4_sum(delta);
+  }
+  const float lse = valid ? a.lse[out] : 0.0f;
+  if (valid && g == 0) a.delta[out] = delta;
+  f32x4 acc[DP / 16] = {};
+
+  for (int k0 = 0; k0 < to; k0 += kF32Step) {
+    __syncthreads();
+    for (int i = tid; i < kF32Step * (DP / 4); i += kF32Threads) {
+      const int r = i / (DP / 4), col = 4 * (i % (DP / 4)), j = k0 + r;
+      f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+      if (j < to && col < a.d) {
+        const int64_t at = w.k0 + j;
+        x = load4(static_cast<const T*>(a.k.data) + at * a.k.ts + hk * a.k.hs + col);
+        y = load4(static_cast<const T*>(a.v.data) + at * a.v.ts + hk * a.v.hs + col);
+      }
+      *reinterpret_cast<f32x4*>(&ks[r][col]) = x;
+      *reinterpret_cast<f32x4*>(&vs[r][col]) = y;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      const f32x4 s = tile_dot<DP>(ks, 16 * kt, q, c, g);
+      const f32x4 dp = tile_dot<DP>(vs, 16 * kt, dout, c, g);
+      f32x4 ds;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = k0 + 16 * kt + 4 * g + i;
+        float dcap;
+        const float x = score_f32(a, s[i], slope, pos - j, &dcap);
+        const float p = j < lim ? __builtin_amdgcn_exp2f((x - lse) * kLog2eF) : 0.0f;
+        ds[i] = j < lim ? p * (dp[i] - delta) * dcap : 0.0f;
+      }
+      tile_accumulate<DP>(acc, ks, 16 * kt, ds, c, g);
+    }
+  }
+  if (!valid) return;
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t)
+    if (16 * t + 4 * g < a.d)
+      store4(static_cast<T*>(a.out) + out * a.d + 16 * t + 4 * g, acc[t] * a.scale);
+}
+
+// The gradients of the keys and values: 64 keys per workgroup, against the
+// rows of their document that see any of them.
+template <typename T, int DP>
+__global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
+  __shared__ __attribute__((aligned(16))) float qs[kF32Step][DP + 4];
+  __shared__ __attribute__((aligned(16))) float os[kF32Step][DP + 4];
+  __shared__ float row_lse[kF32Step], row_delta[kF32Step], row_slope[kF32Step];
+  const int hk = blockIdx.x % a.kv_heads;
+  DocTile w;
+  w.b = find_doc<kF32Rows>(a.cu_k, a.n, a.tokens_k, 1, blockIdx.x / a.kv_heads, &w.tile);
+  doc_queries(a, &w);
+  doc_keys<false>(a, &w);
+  if (w.b >= a.n) {  // keys past the last document
+    w.k0 = doc_start(a.cu_k, a.n, a.tokens_k);
+    w.lk = a.tokens_k - w.k0;
+    w.lq = 0;
+  }
+  if (w.tile * kF32Rows >= w.lk) return;
+
+  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
+  const int c = lane % 16, g = lane / 16;
+  const int first = w.tile * kF32Rows;
+  const int key = first + 16 * wave + c;
+  const bool valid = key < w.lk;
+  const int64_t token = w.k0 + key;
+
+  f32x4 k[DP / 16], v[DP / 16];
+  load_row<T, DP>(k, static_cast<const T*>(a.k.data) + token * a.k.ts + hk * a.k.hs, valid, g,
+                  a.d);
+  load_row<T, DP>(v, static_cast<const T*>(a.v.data) + token * a.v.ts + hk * a.v.hs, valid, g,
+                  a.d);
+  f32x4 dk[DP / 16] = {}, dv[DP / 16] = {};
+
+  // The first token that sees the tile's first key.
+  const int tok0 = a.causal && first >= w.prefix ? max(first - (w.lk - w.lq), 0) : 0;
+  const int rows = w.lq * a.group;
+  for (int r0 = tok0 * a.group; r0 < rows; r0 += kF32Step) {
+    __syncthreads();
+    for (int i = tid; i < kF32Step * (DP / 4); i += kF32Threads) {
+      const int r = i / (DP / 4), col = 4 * (i % (DP / 4)), row = r0 + r;
+      f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+      if (row < rows && col < a.d) {
+        const int64_t at = w.q0 + row / a.group;
+        const int head = hk * a.group + row % a.group;
+        x = load4(static_cast<const T*>(a.q.data) + at * a.q.ts + head * a.q.hs + col);
+        y = load4(static_cast<const T*>(a.dout.data) + at * a.dout.ts + head * a.dout.hs + col);
+      }
+      *reinterpret_cast<f32x4*>(&qs[r][col]) = x;
+      *reinterpret_cast<f32x4*>(&os[r][col]) = y;
+    }
+    if (tid < kF32Step) {
+      const int row = r0 + tid;
+      const int head = hk * a.group + row % a.group;
+      const int64_t at = static_cast<int64_t>(w.q0 + row / a.group) * a.heads + head;
+      row_lse[tid] = row < rows ? a.lse[at] : 0.0f;
+      row_delta[tid] = row < rows ? a.delta[at] : 0.0f;
+      row_slope[tid] = row < rows && a.slopes != nullptr ? a.slopes[head] : 0.0f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int qt = 0; qt < 2; ++qt) {
+      const f32x4 s = tile_dot<DP>(qs, 16 * qt, k, c, g);
+      const f32x4 dp = tile_dot<DP>(os, 16 * qt, v, c, g);
+      f32x4 p, ds;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 16 * qt + 4 * g + i, row = r0 + r;
+        const int tok = row / a.group;
+        const bool seen = valid && row < rows && key < keys_seen(a, w, tok);
+        float dcap;
+        const float x = score_f32(a, s[i], row_slope[r], tok + w.lk - w.lq - key, &dcap);
+        p[i] = seen ? __builtin_amdgcn_exp2f((x - row_lse[r]) * kLog2eF) : 0.0f;
+        ds[i] = seen ? p[i] * (dp[i] - row_delta[r]) * dcap : 0.0f;
+      }
+      tile_accumulate<DP>(dv, os, 16 * qt, p, c, g);
+      tile_accumulate<DP>(dk, qs, 16 * qt, ds, c, g);
+    }
+  }
+  if (!valid) return;
+  const int64_t out = (token * a.kv_heads + hk) * a.d;
+#pragma unroll
+  for (int t = 0; t < DP / 16; ++t) {
+    const int col = 16 * t + 4 * g;
+    if (col < a.d) {
+      store4(static_cast<T*>(a.dk) + out + col, dk[t] * a.scale);
+      store4(static_cast<T*>(a.dv) + out + col, dv[t]);
+    }
+  }
+}
+
+// Joins the splits of a row, one wavefront each.  The splits of the row's tile
+// follow from the lengths as in the kernel that wrote them.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(256) void k_heads_join(HeadsArgs a) {
+  const int chunk = split_chunk<ROWS>(a);
+  if (chunk == 0) return;
+  const int64_t out = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
+  const int lane = threadIdx.x % 64;
+  if (out >= static_cast<int64_t>(a.tokens_q) * a.heads) return;
+  const int token = static_cast<int>(out / a.heads);
+  DocTile w;
+  w.b = find_doc_of_token(a.cu_q, a.n, a.tokens_q, token);
+  doc_queries(a, &w);
+  doc_keys<true>(a, &w);
+  const int row = (token - w.q0) * a.group + static_cast<int>(out % a.heads) % a.group;
+  const int end =
+      keys_seen(a, w, (min(w.lq * a.group, (row / ROWS + 1) * ROWS) - 1) / a.group);
+  const int count = max(1, (end + chunk - 1) / chunk);
+  const int64_t step = static_cast<int64_t>(a.tokens_q) * a.heads;
+  float m = -INFINITY;
+  for (int s = 0; s < count; ++s) m = fmaxf(m, a.part_ml[2 * (s * step + out)]);
+  const float base = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f;
+  f32x4 acc = {0, 0, 0, 0};
+  for (int s = 0; s < count; ++s) {
+    const float* ml = a.part_ml + 2 * (s * step + out);
+    const float f = __builtin_amdgcn_exp2f((ml[0] - base) * kLog2eF);
+    l += ml[1] * f;
+    if (4 * lane < a.d)
+      acc += *reinterpret_cast<const f32x4*>(a.part_o + (s * step + out) * a.d + 4 * lane) * f;
+  }
+  const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
+  if (lane == 0 && a.lse != nullptr)
+    a.lse[out] = m == -INFINITY ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2F;
+  if (4 * lane < a.d) store4(static_cast<T*>(a.out) + out * a.d + 4 * lane, acc * inv);
+}
+
+}  // namespace smx

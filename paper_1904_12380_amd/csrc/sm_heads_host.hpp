@@ -1,0 +1,112 @@
+// Host-side checks shared by the entry points of attention_mi355x.h.
+#pragma once
+
+#include <cmath>
+
+#include "../../include/attention_mi355x.h"
+#include "sm_host.hpp"
+
+namespace smx_host {
+
+inline int dtype_size(int dtype) {
+  return dtype == SOFTMAX_F32 ? 4 : dtype == SOFTMAX_F16 || dtype == SOFTMAX_BF16 ? 2 : 0;
+}
+
+// log2 of a power of two up to 2^20, else -1.
+inline int log2_of(int64_t x) {
+  for (int i = 0; i <= 20; ++i)
+    if (x == int64_t(1) << i) return i;
+  return -1;
+}
+
+// extent += (count - 1) * stride without overflow; both not negative.
+inline bool add_extent(int64_t count, int64_t stride, int64_t* extent) {
+  int64_t x = 0;
+  return stride >= 0 && !__builtin_mul_overflow(count - 1, stride, &x) &&
+         !__builtin_add_overflow(*extent, x, extent);
+}
+
+// The layout rules of a tensor [tokens, heads, d]; its extent in bytes (0
+// when empty).
+inline bool heads_ok(const softmax_heads_t* t, int size, int64_t* bytes) {
+  *bytes = 0;
+  if (t == nullptr || t->tokens < 0 || t->heads < 0 || t->tokens > INT32_MAX ||
+      t->heads > INT32_MAX || t->d < 8 || t->d > SOFTMAX_HEADS_MAX_DIM || t->d % 8 != 0)
+    return false;
+  if (t->token_stride < 0 || t->head_stride < 0) return false;
+  if (t->tokens == 0 || t->heads == 0) return true;
+  const int64_t strip = 16 / size;
+  if (!aligned16(t->data) || t->token_stride % strip != 0 || t->head_stride % strip != 0)
+    return false;
+  int64_t extent = t->d;
+  if (!add_extent(t->tokens, t->token_stride, &extent) ||
+      !add_extent(t->heads, t->head_stride, &extent) || extent > INT64_MAX / size)
+    return false;
+  *bytes = extent * size;
+  return true;
+}
+
+inline bool cache_ok(const softmax_cache_t* t, int size, int64_t* bytes) {
+  *bytes = 0;
+  if (t == nullptr || t->blocks < 0 || t->blocks > INT32_MAX || log2_of(t->block_size) < 0 ||
+      t->heads < 0 || t->heads > INT32_MAX || t->d < 8 || t->d > SOFTMAX_HEADS_MAX_DIM ||
+      t->d % 8 != 0)
+    return false;
+  if (t->block_stride < 0 || t->token_stride < 0 || t->head_stride < 0) return false;
+  if (t->blocks == 0 || t->heads == 0) return true;
+  const int64_t strip = 16 / size;
+  if (!aligned16(t->data) || t->block_stride % strip != 0 || t->token_stride % strip != 0 ||
+      t->head_stride % strip != 0)
+    return false;
+  int64_t extent = t->d;
+  if (!add_extent(t->blocks, t->block_stride, &extent) ||
+      !add_extent(t->block_size, t->token_stride, &extent) ||
+      !add_extent(t->heads, t->head_stride, &extent) || extent > INT64_MAX / size)
+    return false;
+  *bytes = extent * size;
+  return true;
+}
+
+inline bool same_cache(const softmax_cache_t* a, const softmax_cache_t* b) {
+  return a->blocks == b->blocks && a->block_size == b->block_size && a->heads == b->heads &&
+         a->d == b->d;
+}
+
+inline bool score_ok(const softmax_score_t* s) {
+  return s != nullptr && std::isfinite(s->scale) && std::isfinite(s->cap) && s->cap >= 0.0f &&
+         (s->causal == 0 || s->causal == 1) && (s->causal == 1 || s->prefix == nullptr);
+}
+
+struct Range {
+  const void* p;
+  int64_t bytes;
+};
+
+// Every range is memory that the current device can use, and no output
+// overlaps an input or another output (`interleaved`: outputs may overlap
+// each other).  Empty ranges may be null.
+template <int NI, int NO>
+int check_ranges(const Range (&in)[NI], const Range (&out)[NO], bool interleaved = false) {
+  for (const Range& r : in)
+    if (r.bytes > 0 && r.p == nullptr) return SOFTMAX_ERR_INVALID_ARG;
+  for (int i = 0; i < NO; ++i) {
+    if (out[i].bytes > 0 && out[i].p == nullptr) return SOFTMAX_ERR_INVALID_ARG;
+    for (const Range& r : in)
+      if (ranges_overlap(out[i].p, out[i].bytes, r.p, r.bytes)) return SOFTMAX_ERR_INVALID_ARG;
+    for (int j = 0; j < i && !interleaved; ++j)
+      if (ranges_overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
+        return SOFTMAX_ERR_INVALID_ARG;
+  }
+  int dev = 0;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return fail_hip(e);
+  for (const Range& r : in)
+    if (r.bytes > 0)
+      if (const int rc = check_device_range(r.p, r.bytes, dev)) return rc;
+  for (const Range& r : out)
+    if (r.bytes > 0)
+      if (const int rc = check_device_range(r.p, r.bytes, dev)) return rc;
+  return SOFTMAX_OK;
+}
+
+}  // namespace smx_host
