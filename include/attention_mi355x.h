@@ -53,6 +53,7 @@ extern "C" {
 #define SOFTMAX_BF16 2
 
 #define SOFTMAX_HEADS_MAX_DIM 256
+#define SOFTMAX_HEADS_MAX_STRIDE 8388608 /* between tokens of softmax_heads_t */
 
 /* A tensor [tokens, heads, d] of a call's type. */
 typedef struct softmax_heads_t {

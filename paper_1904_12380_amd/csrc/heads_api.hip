@@ -8,6 +8,7 @@
 #include "sm_heads.hpp"
 #include "sm_heads_f32.hpp"
 #include "sm_heads_host.hpp"
+#include "sm_heads_mfma.hpp"
 
 namespace {
 
@@ -33,6 +34,7 @@ void set_shape(HeadsArgs* a, int64_t tokens_q, int64_t tokens_k, int64_t heads, 
   a->causal = s->causal;
   a->scale = s->scale;
   a->cap = s->cap;
+  a->exp_cap = s->cap > 0.0f ? 2.0f * kLog2eF / s->cap : 0.0f;
 }
 
 // Sizes that a call's index arithmetic holds.
@@ -61,12 +63,32 @@ const void* fwd_f32(int d) {
   return reinterpret_cast<const void*>(&k_heads_fwd_f32<T, 256, PAGED>);
 }
 
-template <bool PAGED>
-const void* fwd_fn(int dtype, int d) {
-  return dtype == SOFTMAX_F32   ? fwd_f32<float, PAGED>(d)
-         : dtype == SOFTMAX_F16 ? fwd_f32<f16, PAGED>(d)
-                                : fwd_f32<bf16, PAGED>(d);
+template <typename T, bool PAGED, bool SCORED>
+const void* fwd_16(int d) {
+  if (d <= 64) return reinterpret_cast<const void*>(&k_heads_fwd<T, 64, PAGED, SCORED>);
+  if (d <= 128) return reinterpret_cast<const void*>(&k_heads_fwd<T, 128, PAGED, SCORED>);
+  return reinterpret_cast<const void*>(&k_heads_fwd<T, 256, PAGED, SCORED>);
 }
+
+template <typename T, bool PAGED>
+const void* fwd_16(int d, bool scored) {
+  return scored ? fwd_16<T, PAGED, true>(d) : fwd_16<T, PAGED, false>(d);
+}
+
+// Scores are more than a dot product times a scale of ordinary size.
+bool scored(const HeadsArgs& a) {
+  return a.cap > 0.0f || a.slopes != nullptr || !(std::fabs(a.scale) > 1e-20f);
+}
+
+template <bool PAGED>
+const void* fwd_fn(int dtype, const HeadsArgs& a) {
+  return dtype == SOFTMAX_F32   ? fwd_f32<float, PAGED>(a.d)
+         : dtype == SOFTMAX_F16 ? fwd_16<f16, PAGED>(a.d, scored(a))
+                                : fwd_16<bf16, PAGED>(a.d, scored(a));
+}
+
+// Rows of a workgroup's tile in the forward kernels.
+int fwd_rows(int dtype) { return dtype == SOFTMAX_F32 ? kF32Rows : kTileRows; }
 
 const void* dq_fn(int dtype, int d) {
   return dtype == SOFTMAX_F32   ? SMX_FOR_WIDTH(d, k_heads_dq_f32, float)
@@ -82,8 +104,8 @@ const void* dkv_fn(int dtype, int d) {
 
 const void* join_fn(int dtype) {
   return dtype == SOFTMAX_F32 ? reinterpret_cast<const void*>(&k_heads_join<float, kF32Rows>)
-         : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_heads_join<f16, kF32Rows>)
-                                : reinterpret_cast<const void*>(&k_heads_join<bf16, kF32Rows>);
+         : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_heads_join<f16, kTileRows>)
+                                : reinterpret_cast<const void*>(&k_heads_join<bf16, kTileRows>);
 }
 
 // Splits of the keys to launch: enough that the call's tiles fill `target`
@@ -94,7 +116,7 @@ int64_t paged_splits(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t re
                      int64_t max_keys, int64_t target) {
   // Tiles that the requests have at least.
   const int64_t rows = tokens * (heads / kv_heads);
-  const int64_t tiles = std::max<int64_t>(1, std::max(rows / kF32Rows, std::min(requests, tokens)));
+  const int64_t tiles = std::max<int64_t>(1, std::max(rows / kTileRows, std::min(requests, tokens)));
   const int64_t wanted = ceil_div(target, tiles * kv_heads);
   return std::clamp<int64_t>(std::min(wanted, ceil_div(max_keys, kMinChunk)), 1, kMaxSplits);
 }
@@ -152,9 +174,9 @@ SOFTMAX_API int softmax_packed_attention_fwd(const softmax_heads_t* q, const sof
   a.lse = lse;
   a.cu_q = cu_q;
   a.cu_k = cu_k;
-  const int64_t slots = tile_slots(q->tokens * a.group, docs, kF32Rows);
+  const int64_t slots = tile_slots(q->tokens * a.group, docs, fwd_rows(dtype));
   const hipError_t e =
-      launch2(fwd_fn<false>(dtype, a.d), slots * a.kv_heads, 1, kF32Threads, &a, stream);
+      launch2(fwd_fn<false>(dtype, a), slots * a.kv_heads, 1, kF32Threads, &a, stream);
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
 }
 
@@ -301,9 +323,9 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
   a.target = static_cast<int>(target);
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = a.part_o + splits * rows * q->d;
-  const int64_t slots = tile_slots(q->tokens * a.group, requests, kF32Rows);
+  const int64_t slots = tile_slots(q->tokens * a.group, requests, fwd_rows(dtype));
   hipError_t e =
-      launch2(fwd_fn<true>(dtype, a.d), slots * a.kv_heads, splits, kF32Threads, &a, stream);
+      launch2(fwd_fn<true>(dtype, a), slots * a.kv_heads, splits, kF32Threads, &a, stream);
   if (e == hipSuccess && splits > 1)
     e = launch2(join_fn(dtype), ceil_div(rows, 4), 1, 256, &a, stream);
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);

@@ -62,6 +62,7 @@ struct HeadsArgs {
   int n, tokens_q, tokens_k, heads, kv_heads, group, d;
   int causal;
   float scale, cap;
+  float exp_cap;       // 2 log2 e / cap
 };
 
 __device__ __forceinline__ int clamp_i(int x, int lo, int hi) {

@@ -33,7 +33,9 @@ inline bool heads_ok(const softmax_heads_t* t, int size, int64_t* bytes) {
   if (t == nullptr || t->tokens < 0 || t->heads < 0 || t->tokens > INT32_MAX ||
       t->heads > INT32_MAX || t->d < 8 || t->d > SOFTMAX_HEADS_MAX_DIM || t->d % 8 != 0)
     return false;
-  if (t->token_stride < 0 || t->head_stride < 0) return false;
+  // A tile's offsets between its rows fit 31 bits.
+  if (t->token_stride < 0 || t->token_stride > SOFTMAX_HEADS_MAX_STRIDE || t->head_stride < 0)
+    return false;
   if (t->tokens == 0 || t->heads == 0) return true;
   const int64_t strip = 16 / size;
   if (!aligned16(t->data) || t->token_stride % strip != 0 || t->head_stride % strip != 0)
