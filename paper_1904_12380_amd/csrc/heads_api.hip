@@ -6,6 +6,7 @@
 
 #include "../../include/attention_mi355x.h"
 #include "sm_heads.hpp"
+#include "sm_heads_bwd.hpp"
 #include "sm_heads_f32.hpp"
 #include "sm_heads_host.hpp"
 #include "sm_heads_mfma.hpp"
@@ -51,56 +52,57 @@ hipError_t launch2(const void* fn, int64_t x, int64_t y, int block, HeadsArgs* a
 }
 
 // The instance of a head width: its columns padded to 64, 128 or 256.
-#define SMX_FOR_WIDTH(d, K, ...)                                            \
-  ((d) <= 64    ? reinterpret_cast<const void*>(&K<__VA_ARGS__, 64>)        \
-   : (d) <= 128 ? reinterpret_cast<const void*>(&K<__VA_ARGS__, 128>)       \
-                : reinterpret_cast<const void*>(&K<__VA_ARGS__, 256>))
-
-template <typename T, bool PAGED>
-const void* fwd_f32(int d) {
-  if (d <= 64) return reinterpret_cast<const void*>(&k_heads_fwd_f32<T, 64, PAGED>);
-  if (d <= 128) return reinterpret_cast<const void*>(&k_heads_fwd_f32<T, 128, PAGED>);
-  return reinterpret_cast<const void*>(&k_heads_fwd_f32<T, 256, PAGED>);
-}
-
-template <typename T, bool PAGED, bool SCORED>
-const void* fwd_16(int d) {
-  if (d <= 64) return reinterpret_cast<const void*>(&k_heads_fwd<T, 64, PAGED, SCORED>);
-  if (d <= 128) return reinterpret_cast<const void*>(&k_heads_fwd<T, 128, PAGED, SCORED>);
-  return reinterpret_cast<const void*>(&k_heads_fwd<T, 256, PAGED, SCORED>);
-}
-
-template <typename T, bool PAGED>
-const void* fwd_16(int d, bool scored) {
-  return scored ? fwd_16<T, PAGED, true>(d) : fwd_16<T, PAGED, false>(d);
-}
+#define SMX_BY_WIDTH(d, K, T, ...)                                                  \
+  ((d) <= 64    ? reinterpret_cast<const void*>(&K<T, 64 __VA_OPT__(, ) __VA_ARGS__>)  \
+   : (d) <= 128 ? reinterpret_cast<const void*>(&K<T, 128 __VA_OPT__(, ) __VA_ARGS__>) \
+                : reinterpret_cast<const void*>(&K<T, 256 __VA_OPT__(, ) __VA_ARGS__>))
 
 // Scores are more than a dot product times a scale of ordinary size.
 bool scored(const HeadsArgs& a) {
   return a.cap > 0.0f || a.slopes != nullptr || !(std::fabs(a.scale) > 1e-20f);
 }
 
+template <typename T, bool PAGED>
+const void* fwd_16(const HeadsArgs& a) {
+  return scored(a) ? SMX_BY_WIDTH(a.d, k_heads_fwd, T, PAGED, true)
+                   : SMX_BY_WIDTH(a.d, k_heads_fwd, T, PAGED, false);
+}
+
 template <bool PAGED>
 const void* fwd_fn(int dtype, const HeadsArgs& a) {
-  return dtype == SOFTMAX_F32   ? fwd_f32<float, PAGED>(a.d)
-         : dtype == SOFTMAX_F16 ? fwd_16<f16, PAGED>(a.d, scored(a))
-                                : fwd_16<bf16, PAGED>(a.d, scored(a));
+  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH(a.d, k_heads_fwd_f32, float, PAGED)
+         : dtype == SOFTMAX_F16 ? fwd_16<f16, PAGED>(a)
+                                : fwd_16<bf16, PAGED>(a);
 }
 
-// Rows of a workgroup's tile in the forward kernels.
-int fwd_rows(int dtype) { return dtype == SOFTMAX_F32 ? kF32Rows : kTileRows; }
-
-const void* dq_fn(int dtype, int d) {
-  return dtype == SOFTMAX_F32   ? SMX_FOR_WIDTH(d, k_heads_dq_f32, float)
-         : dtype == SOFTMAX_F16 ? SMX_FOR_WIDTH(d, k_heads_dq_f32, f16)
-                                : SMX_FOR_WIDTH(d, k_heads_dq_f32, bf16);
+template <typename T>
+const void* dq_16(const HeadsArgs& a) {
+  return scored(a) ? SMX_BY_WIDTH(a.d, k_heads_dq, T, true)
+                   : SMX_BY_WIDTH(a.d, k_heads_dq, T, false);
 }
 
-const void* dkv_fn(int dtype, int d) {
-  return dtype == SOFTMAX_F32   ? SMX_FOR_WIDTH(d, k_heads_dkv_f32, float)
-         : dtype == SOFTMAX_F16 ? SMX_FOR_WIDTH(d, k_heads_dkv_f32, f16)
-                                : SMX_FOR_WIDTH(d, k_heads_dkv_f32, bf16);
+template <typename T>
+const void* dkv_16(const HeadsArgs& a) {
+  return scored(a) ? SMX_BY_WIDTH(a.d, k_heads_dkv, T, true)
+                   : SMX_BY_WIDTH(a.d, k_heads_dkv, T, false);
 }
+
+const void* dq_fn(int dtype, const HeadsArgs& a) {
+  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH(a.d, k_heads_dq_f32, float)
+         : dtype == SOFTMAX_F16 ? dq_16<f16>(a)
+                                : dq_16<bf16>(a);
+}
+
+const void* dkv_fn(int dtype, const HeadsArgs& a) {
+  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH(a.d, k_heads_dkv_f32, float)
+         : dtype == SOFTMAX_F16 ? dkv_16<f16>(a)
+                                : dkv_16<bf16>(a);
+}
+
+// Rows (keys) of a workgroup's tile: the kernels' kF32Rows and kTileRows, with
+// kF32Threads = kTileThreads threads.
+int tile_rows(int dtype) { return dtype == SOFTMAX_F32 ? kF32Rows : kTileRows; }
+static_assert(kF32Threads == kTileThreads, "one launch shape");
 
 const void* join_fn(int dtype) {
   return dtype == SOFTMAX_F32 ? reinterpret_cast<const void*>(&k_heads_join<float, kF32Rows>)
@@ -174,15 +176,15 @@ SOFTMAX_API int softmax_packed_attention_fwd(const softmax_heads_t* q, const sof
   a.lse = lse;
   a.cu_q = cu_q;
   a.cu_k = cu_k;
-  const int64_t slots = tile_slots(q->tokens * a.group, docs, fwd_rows(dtype));
+  const int64_t slots = tile_slots(q->tokens * a.group, docs, tile_rows(dtype));
   const hipError_t e =
-      launch2(fwd_fn<false>(dtype, a), slots * a.kv_heads, 1, kF32Threads, &a, stream);
+      launch2(fwd_fn<false>(dtype, a), slots * a.kv_heads, 1, kTileThreads, &a, stream);
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
 }
 
 SOFTMAX_API int64_t softmax_packed_attention_bwd_workspace(int64_t tokens_q, int64_t heads) {
   if (tokens_q < 0 || heads < 0 || (heads > 0 && tokens_q > INT32_MAX / heads)) return -1;
-  return tokens_q * heads * 4;
+  return tokens_q * heads * 8;
 }
 
 SOFTMAX_API int softmax_packed_attention_bwd(const softmax_heads_t* dout,
@@ -240,15 +242,15 @@ SOFTMAX_API int softmax_packed_attention_bwd(const softmax_heads_t* dout,
   a.cu_q = cu_q;
   a.cu_k = cu_k;
   if (rows > 0) {
-    const int64_t slots = tile_slots(q->tokens * a.group, docs, kF32Rows);
+    const int64_t slots = tile_slots(q->tokens * a.group, docs, tile_rows(dtype));
     const hipError_t e =
-        launch2(dq_fn(dtype, a.d), slots * a.kv_heads, 1, kF32Threads, &a, stream);
+        launch2(dq_fn(dtype, a), slots * a.kv_heads, 1, kTileThreads, &a, stream);
     if (e != hipSuccess) return fail_hip(e);
   }
   if (krows > 0) {
-    const int64_t slots = tile_slots(k->tokens, docs, kF32Rows);
+    const int64_t slots = tile_slots(k->tokens, docs, tile_rows(dtype));
     const hipError_t e =
-        launch2(dkv_fn(dtype, a.d), slots * a.kv_heads, 1, kF32Threads, &a, stream);
+        launch2(dkv_fn(dtype, a), slots * a.kv_heads, 1, kTileThreads, &a, stream);
     if (e != hipSuccess) return fail_hip(e);
   }
   return SOFTMAX_OK;
@@ -323,9 +325,9 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
   a.target = static_cast<int>(target);
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = a.part_o + splits * rows * q->d;
-  const int64_t slots = tile_slots(q->tokens * a.group, requests, fwd_rows(dtype));
+  const int64_t slots = tile_slots(q->tokens * a.group, requests, tile_rows(dtype));
   hipError_t e =
-      launch2(fwd_fn<true>(dtype, a), slots * a.kv_heads, splits, kF32Threads, &a, stream);
+      launch2(fwd_fn<true>(dtype, a), slots * a.kv_heads, splits, kTileThreads, &a, stream);
   if (e == hipSuccess && splits > 1)
     e = launch2(join_fn(dtype), ceil_div(rows, 4), 1, 256, &a, stream);
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);

@@ -43,7 +43,7 @@ struct HeadsArgs {
   void* dk;
   void* dv;
   float* lse;        // written by the forward pass (may be null), read by the backward
-  float* delta;      // D of every query row (backward)
+  float* delta;      // D of every query row (backward); 16-bit types: pairs
   const int* cu_q;   // [n + 1]
   const int* cu_k;   // [n + 1]; paged: key_lens [n]
   const float* slopes;
