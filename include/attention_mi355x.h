@@ -110,8 +110,12 @@ SOFTMAX_API int softmax_packed_attention_fwd(const softmax_heads_t* q, const sof
                                              int64_t docs, const softmax_score_t* score,
                                              int dtype, hipStream_t stream);
 
-/* Bytes of workspace that softmax_packed_attention_bwd needs. */
-SOFTMAX_API int64_t softmax_packed_attention_bwd_workspace(int64_t tokens_q, int64_t heads);
+/* Bytes of workspace that softmax_packed_attention_bwd needs, or -1 for bad
+ * sizes: 8 per query row, and fp32 sums of dk and dv for up to 16 splits where
+ * there are few key tiles to fill the device. */
+SOFTMAX_API int64_t softmax_packed_attention_bwd_workspace(int64_t tokens_q, int64_t tokens_k,
+                                                           int64_t heads, int64_t kv_heads,
+                                                           int64_t d, int dtype);
 
 /*
  * softmax_packed_attention_bwd -- the gradients of softmax_packed_attention_fwd:

@@ -49,7 +49,7 @@ def declare(lib: ctypes.CDLL) -> None:
     for name, args, result in (
             ("packed_attention_fwd", [heads, heads, heads, _vp, _vp, _vp, _vp, _i64, score,
                                       ctypes.c_int, _vp], ctypes.c_int),
-            ("packed_attention_bwd_workspace", [_i64, _i64], _i64),
+            ("packed_attention_bwd_workspace", [_i64] * 5 + [ctypes.c_int], _i64),
             ("packed_attention_bwd", [heads] * 5 + [_vp] * 6 + [_i64, score, ctypes.c_int, _vp,
                                                                 _i64, _vp], ctypes.c_int),
             ("paged_attention_workspace", [_i64] * 6, _i64),
@@ -208,7 +208,8 @@ def softmax_packed_attention_bwd(dout, q, k, v, o, lse, cu_q, cu_k=None, *, caus
     dq = _output(dq, q.shape, q.dtype, q.device, "dq")
     dk = _output(dk, k.shape, q.dtype, q.device, "dk")
     dv = _output(dv, v.shape, q.dtype, q.device, "dv")
-    room = _fns.softmax_packed_attention_bwd_workspace(q.shape[0], q.shape[1])
+    room = _fns.softmax_packed_attention_bwd_workspace(aq.tokens, ak.tokens, aq.heads, ak.heads,
+                                                       aq.d, _dtypes[q.dtype])
     work = torch.empty(max(room, 0), dtype=torch.uint8, device=q.device)
     _on_stream(work, stream)
     _checked(_sm._run(fn, q.device, stream,

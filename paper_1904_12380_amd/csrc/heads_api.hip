@@ -52,10 +52,12 @@ hipError_t launch2(const void* fn, int64_t x, int64_t y, int block, HeadsArgs* a
 }
 
 // The instance of a head width: its columns padded to 64, 128 or 256.
-#define SMX_BY_WIDTH(d, K, T, ...)                                                  \
-  ((d) <= 64    ? reinterpret_cast<const void*>(&K<T, 64 __VA_OPT__(, ) __VA_ARGS__>)  \
-   : (d) <= 128 ? reinterpret_cast<const void*>(&K<T, 128 __VA_OPT__(, ) __VA_ARGS__>) \
-                : reinterpret_cast<const void*>(&K<T, 256 __VA_OPT__(, ) __VA_ARGS__>))
+#define SMX_FN(...) reinterpret_cast<const void*>(&__VA_ARGS__)
+#define SMX_BY_WIDTH(d, K, T, ...)                                                    \
+  ((d) <= 64 ? SMX_FN(K<T, 64, __VA_ARGS__>)                                          \
+             : (d) <= 128 ? SMX_FN(K<T, 128, __VA_ARGS__>) : SMX_FN(K<T, 256, __VA_ARGS__>))
+#define SMX_BY_WIDTH_F32(d, K)                                                        \
+  ((d) <= 64 ? SMX_FN(K<64>) : (d) <= 128 ? SMX_FN(K<128>) : SMX_FN(K<256>))
 
 // Scores are more than a dot product times a scale of ordinary size.
 bool scored(const HeadsArgs& a) {
@@ -70,7 +72,10 @@ const void* fwd_16(const HeadsArgs& a) {
 
 template <bool PAGED>
 const void* fwd_fn(int dtype, const HeadsArgs& a) {
-  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH(a.d, k_heads_fwd_f32, float, PAGED)
+  return dtype == SOFTMAX_F32
+             ? (a.d <= 64    ? SMX_FN(k_heads_fwd_f32<64, PAGED>)
+                : a.d <= 128 ? SMX_FN(k_heads_fwd_f32<128, PAGED>)
+                             : SMX_FN(k_heads_fwd_f32<256, PAGED>))
          : dtype == SOFTMAX_F16 ? fwd_16<f16, PAGED>(a)
                                 : fwd_16<bf16, PAGED>(a);
 }
@@ -88,15 +93,19 @@ const void* dkv_16(const HeadsArgs& a) {
 }
 
 const void* dq_fn(int dtype, const HeadsArgs& a) {
-  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH(a.d, k_heads_dq_f32, float)
+  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, k_heads_dq_f32)
          : dtype == SOFTMAX_F16 ? dq_16<f16>(a)
                                 : dq_16<bf16>(a);
 }
 
 const void* dkv_fn(int dtype, const HeadsArgs& a) {
-  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH(a.d, k_heads_dkv_f32, float)
+  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, k_heads_dkv_f32)
          : dtype == SOFTMAX_F16 ? dkv_16<f16>(a)
                                 : dkv_16<bf16>(a);
+}
+
+const void* sum_fn(int dtype) {
+  return dtype == SOFTMAX_F16 ? SMX_FN(k_heads_sum<f16>) : SMX_FN(k_heads_sum<bf16>);
 }
 
 // Rows (keys) of a workgroup's tile: the kernels' kF32Rows and kTileRows, with
@@ -125,6 +134,26 @@ int64_t paged_splits(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t re
 
 int64_t split_bytes(int64_t splits, int64_t tokens, int64_t heads, int64_t d) {
   return splits <= 1 ? 0 : splits * tokens * heads * (d + 2) * 4;
+}
+
+// Splits of a key tile's rows to launch in the backward pass of 16-bit types:
+// enough that the tiles of one long document make kKeyTarget workgroups, and
+// no more than its turns allow.
+constexpr int kKeyTarget = 2048;
+
+int64_t key_splits(int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv_heads,
+                   int dtype) {
+  if (dtype == SOFTMAX_F32) return 1;
+  const int64_t tiles = std::max<int64_t>(1, ceil_div(tokens_k, kTileRows) * kv_heads);
+  const int64_t turns = ceil_div(tokens_q, kTurnRows) * (heads / kv_heads);
+  return std::clamp<int64_t>(std::min(ceil_div(kKeyTarget, tiles), turns / kMinTurns), 1, 16);
+}
+
+// The backward pass' statistics of every row, in whole 16-byte strips, and
+// its split sums.
+int64_t stat_bytes(int64_t tokens_q, int64_t heads) { return (tokens_q * heads * 8 + 15) / 16 * 16; }
+int64_t part_bytes(int64_t splits, int64_t tokens_k, int64_t kv_heads, int64_t d) {
+  return splits <= 1 ? 0 : splits * tokens_k * kv_heads * d * 8;
 }
 
 // Workgroups that fill the device: two per CU.
@@ -182,9 +211,15 @@ SOFTMAX_API int softmax_packed_attention_fwd(const softmax_heads_t* q, const sof
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
 }
 
-SOFTMAX_API int64_t softmax_packed_attention_bwd_workspace(int64_t tokens_q, int64_t heads) {
-  if (tokens_q < 0 || heads < 0 || (heads > 0 && tokens_q > INT32_MAX / heads)) return -1;
-  return tokens_q * heads * 8;
+SOFTMAX_API int64_t softmax_packed_attention_bwd_workspace(int64_t tokens_q, int64_t tokens_k,
+                                                           int64_t heads, int64_t kv_heads,
+                                                           int64_t d, int dtype) {
+  if (tokens_q < 0 || tokens_k < 0 || heads < 0 || d < 8 || d > SOFTMAX_HEADS_MAX_DIM ||
+      dtype_size(dtype) == 0 || !sizes_ok(tokens_q, heads, kv_heads, 0) ||
+      !sizes_ok(tokens_k, heads, kv_heads, 0))
+    return -1;
+  return stat_bytes(tokens_q, heads) +
+         part_bytes(key_splits(tokens_q, tokens_k, heads, kv_heads, dtype), tokens_k, kv_heads, d);
 }
 
 SOFTMAX_API int softmax_packed_attention_bwd(const softmax_heads_t* dout,
@@ -208,7 +243,9 @@ SOFTMAX_API int softmax_packed_attention_bwd(const softmax_heads_t* dout,
       !aligned16(dv) || !aligned16(workspace))
     return SOFTMAX_ERR_INVALID_ARG;
   const int64_t rows = q->tokens * q->heads, krows = k->tokens * k->heads;
-  const int64_t need = softmax_packed_attention_bwd_workspace(q->tokens, q->heads);
+  const int64_t splits = key_splits(q->tokens, k->tokens, q->heads, k->heads, dtype);
+  const int64_t need =
+      stat_bytes(q->tokens, q->heads) + part_bytes(splits, k->tokens, k->heads, k->d);
   if (workspace_bytes < need) return SOFTMAX_ERR_INVALID_ARG;
   if (rows == 0 && krows == 0) return SOFTMAX_OK;
   const Range inputs[] = {{dout->data, db},
@@ -239,6 +276,9 @@ SOFTMAX_API int softmax_packed_attention_bwd(const softmax_heads_t* dout,
   a.dv = dv;
   a.lse = const_cast<float*>(lse);
   a.delta = static_cast<float*>(workspace);
+  a.part_o = a.delta + stat_bytes(q->tokens, q->heads) / 4;
+  a.splits = static_cast<int>(splits);
+  a.target = kKeyTarget;
   a.cu_q = cu_q;
   a.cu_k = cu_k;
   if (rows > 0) {
@@ -250,8 +290,12 @@ SOFTMAX_API int softmax_packed_attention_bwd(const softmax_heads_t* dout,
   if (krows > 0) {
     const int64_t slots = tile_slots(k->tokens, docs, tile_rows(dtype));
     const hipError_t e =
-        launch2(dkv_fn(dtype, a), slots * a.kv_heads, 1, kTileThreads, &a, stream);
+        launch2(dkv_fn(dtype, a), slots * a.kv_heads, splits, kTileThreads, &a, stream);
     if (e != hipSuccess) return fail_hip(e);
+    if (splits > 1) {
+      const hipError_t f = launch2(sum_fn(dtype), slots * a.kv_heads, 1, 256, &a, stream);
+      if (f != hipSuccess) return fail_hip(f);
+    }
   }
   return SOFTMAX_OK;
 }

@@ -172,7 +172,7 @@ __device__ __forceinline__ int split_chunk(const HeadsArgs& a) {
   int64_t chunk = (sum * a.kv_heads + a.target - 1) / a.target;
   chunk = max(chunk, (longest + a.splits - 1) / a.splits);
   chunk = max((chunk + 63) / 64 * 64, static_cast<int64_t>(kMinChunk));
-  return chunk >= longest ? 0 : static_cast<int>(chunk);
+  return __builtin_amdgcn_readfirstlane(chunk >= longest ? 0 : static_cast<int>(chunk));
 }
 
 // Keys [from, to) of split `split` of a tile that sees the first `end`; false

@@ -8,10 +8,13 @@
 // dK^T += Q^T dS.  Seven products instead of the five that one pass over both
 // would take, but every sum has one owner: no atomics, the same bits each time.
 //
-// The first kernel writes what the second needs of every row as a pair (lse
-// in powers of two, D), head by head, so that the second reads it by tokens.
+// The first kernel writes what the second needs of every row as a pair (-lse
+// / c, -D), head by head, so that the second reads it by tokens: the values
+// that its scores and dP start from, so that the shift and the difference cost
+// no instruction.
 #pragma once
 
+#include "sm_heads_f32.hpp"
 #include "sm_heads_mfma.hpp"
 
 namespace smx {
@@ -23,8 +26,8 @@ constexpr int kTwoPartKeys = 128;
 template <typename T, int DP>
 __device__ __forceinline__ f32x16 rows_dot(const TileReader<DP>& rd, const char SMX_LDS* tile,
                                            int row0,
-                                           const typename Vec8<T>::type (&b)[DP / 16]) {
-  f32x16 s = {};
+                                           const typename Vec8<T>::type (&b)[DP / 16],
+                                           f32x16 s = f32x16{}) {
 #pragma unroll
   for (int st = 0; st < DP / 16; ++st) s = mfma32(rd.template rows<T>(tile, row0, st), b[st], s);
   return s;
@@ -209,27 +212,99 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
   if (!valid) return;
   if (half == 0)
     reinterpret_cast<float2*>(a.delta)[static_cast<int64_t>(head) * a.tokens_q + token] =
-        make_float2(lse2, delta);
+        make_float2(-lse2 / c, -delta);
   store_columns<T, DP>(static_cast<T*>(a.out) + out * a.d, a.d, half, acc, a.scale);
 }
 
-template <typename T, int DP, bool SCORED>
-__global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(HeadsArgs a) {
-  __shared__ __attribute__((aligned(16))) char lds_bytes[tile_lds_bytes<DP>()];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][kTileKeys];  // [stage][lse, D][row]
-  char SMX_LDS* lds = (char SMX_LDS*)lds_bytes;
-  const int hk = blockIdx.x % a.kv_heads;
+// The turns of a key tile: 32 tokens of one head each, from the first token
+// that sees the tile's first key, head by head.
+constexpr int kTurnRows = 32;
+
+struct KeyTurns {
+  int tok0, tiles, turns;
+};
+
+__device__ __forceinline__ KeyTurns key_turns(const HeadsArgs& a, const DocTile& w, int first) {
+  KeyTurns k;
+  k.tok0 = a.causal && first >= w.prefix ? max(first - (w.lk - w.lq), 0) : 0;
+  k.tiles = k.tok0 < w.lq ? (w.lq - k.tok0 + kTurnRows - 1) / kTurnRows : 0;
+  k.turns = k.tiles * a.group;
+  return k;
+}
+
+// Turns per split, the same for the whole call: at least kMinTurns, such that
+// the longest document fits the launched splits and the call makes about
+// `target` workgroups.  0: not split.
+constexpr int kMinTurns = 32;
+
+__device__ __forceinline__ int split_turns(const HeadsArgs& a) {
+  if (a.splits <= 1) return 0;
+  int64_t sum = 0, longest = 0;
+  for (int b = static_cast<int>(__lane_id()); b < a.n; b += 64) {
+    const int lq = doc_start(a.cu_q, b + 1, a.tokens_q) - doc_start(a.cu_q, b, a.tokens_q);
+    const int lk = doc_start(a.cu_k, b + 1, a.tokens_k) - doc_start(a.cu_k, b, a.tokens_k);
+    if (lq <= 0 || lk <= 0) continue;
+    const int64_t turns = static_cast<int64_t>((lq + kTurnRows - 1) / kTurnRows) * a.group;
+    sum += turns * ((lk + kTileRows - 1) / kTileRows);
+    longest = max(longest, turns);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    sum += __shfl_xor(sum, o);
+    longest = max(longest, __shfl_xor(longest, o));
+  }
+  if (a.causal) sum /= 2;
+  int64_t chunk = (sum * a.kv_heads + a.target - 1) / a.target;
+  chunk = max(chunk, (longest + a.splits - 1) / a.splits);
+  chunk = max(chunk, static_cast<int64_t>(kMinTurns));
+  return __builtin_amdgcn_readfirstlane(chunk >= longest ? 0 : static_cast<int>(chunk));
+}
+
+// The keys' document and tile of a workgroup; keys past the last document are
+// one without queries.
+__device__ __forceinline__ DocTile key_tile(const HeadsArgs& a, int slot) {
   DocTile w;
-  w.b = find_doc<kTileRows>(a.cu_k, a.n, a.tokens_k, 1, blockIdx.x / a.kv_heads, &w.tile);
+  w.b = find_doc<kTileRows>(a.cu_k, a.n, a.tokens_k, 1, slot, &w.tile);
   doc_queries(a, &w);
   doc_keys<false>(a, &w);
-  if (w.b >= a.n) {  // keys past the last document
+  if (w.b >= a.n) {
     w.k0 = doc_start(a.cu_k, a.n, a.tokens_k);
     w.lk = a.tokens_k - w.k0;
     w.lq = 0;
   }
+  return w;
+}
+
+// LDS of k_heads_dkv: V of the key tile, and two stages of kTurnRows rows of Q
+// and dO.
+template <int DP>
+constexpr int kKeyLds = (kTileRows + 2 * 2 * kTurnRows) * DP * 2;
+
+// A wavefront's K operand stays in registers, its V operand in LDS: with both in
+// registers (64 at a width of 128, beside 128 of sums and 32 of scores) some
+// were spilled, and a reload from scratch waits for the next stage's loads.
+template <typename T, int DP, bool SCORED>
+__global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(HeadsArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds_bytes[kKeyLds<DP>];
+  // Of a stage's rows: -lse / c (what a row's scores start from; scored: -lse
+  // in powers of two), and -D (what dP starts from).
+  __shared__ __attribute__((aligned(16))) float stats[2][2][kTurnRows];
+  char SMX_LDS* lds = (char SMX_LDS*)lds_bytes;
+  const int hk = blockIdx.x % a.kv_heads;
+  const DocTile w = key_tile(a, blockIdx.x / a.kv_heads);
   const int first = w.tile * kTileRows;
   if (first >= w.lk) return;
+  const KeyTurns kt = key_turns(a, w, first);
+  const int chunk = split_turns(a);
+  int turn = 0, turns = kt.turns;
+  const bool split = chunk > 0 && kt.turns > chunk;
+  if (split) {
+    turn = static_cast<int>(blockIdx.y) * chunk;
+    turns = min(turns, turn + chunk);
+    if (turn >= turns) return;
+  } else if (blockIdx.y > 0) {
+    return;
+  }
 
   const int tid = threadIdx.x, lane = tid % 64, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -240,88 +315,111 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
   const float c = SCORED ? 1.0f : fabsf(a.scale) * kLog2eF;
 
   typedef typename Vec8<T>::type V;
-  V k[DP / 16], v[DP / 16];
+  V k[DP / 16];
   load_operand<T, DP>(k, static_cast<const T*>(a.k.data) + token * a.k.ts + hk * a.k.hs, valid,
                       half, a.d);
-  load_operand<T, DP>(v, static_cast<const T*>(a.v.data) + token * a.v.ts + hk * a.v.hs, valid,
-                      half, a.d);
+  const int d2 = 2 * a.d;
+  const char SMX_LDS* vt = lds + 32 * wave * DP * 2;
+  stage_packed<DP, 32 / Stager<DP, false>::kRows>(Stager<DP, false>(a.v, 0, w.k0, hk),
+                                                  lds + 32 * wave * DP * 2, first, 32 * wave, w.lk,
+                                                  d2);
   if (!SCORED && a.scale < 0.0f) {
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) k[i] = -k[i];
   }
   f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
 
-  const TileReader<DP> rd;
-  constexpr int kTile = kTileKeys * DP * 2;
-  constexpr int N = kTileKeys / 4 / Stager<DP, false>::kRows;
-  const int r0 = wave * (kTileKeys / 4), d2 = 2 * a.d;
-  // The first token that sees the workgroup's first key.
-  const int tok0 = a.causal && first >= w.prefix ? max(first - (w.lk - w.lq), 0) : 0;
-  const int tiles = tok0 < w.lq ? (w.lq - tok0 + kTileKeys - 1) / kTileKeys : 0;
-  const int turns = tiles * a.group;
+  const TileReader<DP> reader;
+  constexpr int kTile = kTurnRows * DP * 2;
+  constexpr int N = kTurnRows / 4 / Stager<DP, false>::kRows;
+  const int r0 = wave * (kTurnRows / 4);
+  char SMX_LDS* stages = lds + kTileRows * DP * 2;
 
-  float2 stat = {INFINITY, 0.0f};
-  auto stage = [&](int turn, int buf) {
-    const int head = hk * a.group + turn / tiles;
-    const int t0 = tok0 + turn % tiles * kTileKeys;
-    const Stager<DP, false> qs(a.q, 0, w.q0, head), os(a.dout, 0, w.q0, head);
-    char SMX_LDS* qt = lds + buf * 2 * kTile + r0 * DP * 2;
-    stage_packed<DP, N>(qs, qt, t0, r0, w.lq, d2);
-    stage_packed<DP, N>(os, qt + kTile, t0, r0, w.lq, d2);
-    if (wave == 0) {
-      stat = make_float2(INFINITY, 0.0f);
-      if (t0 + lane < w.lq)
+  float2 stat = {-INFINITY, 0.0f};
+  // The head and the first token of the turn to stage next, and of this one.
+  int next_head = hk * a.group, next_t0 = kt.tok0;
+  if (turn < turns) {
+    next_head += turn / kt.tiles;
+    next_t0 += turn % kt.tiles * kTurnRows;
+  }
+  auto stage = [&](int buf) {
+    const int head = next_head, t0 = next_t0;
+    next_t0 += kTurnRows;
+    if (next_t0 >= w.lq) {
+      next_t0 = kt.tok0;
+      ++next_head;
+    }
+    if (wave == 0) {  // before the stage's loads: waiting for it waits for no other
+      stat = make_float2(-INFINITY, 0.0f);
+      if (lane < kTurnRows && t0 + lane < w.lq)
         stat = reinterpret_cast<const float2*>(
             a.delta)[static_cast<int64_t>(head) * a.tokens_q + w.q0 + t0 + lane];
     }
+    const Stager<DP, false> qs(a.q, 0, w.q0, head), os(a.dout, 0, w.q0, head);
+    char SMX_LDS* qt = stages + buf * 2 * kTile + r0 * DP * 2;
+    stage_packed<DP, N>(qs, qt, t0, r0, w.lq, d2);
+    stage_packed<DP, N>(os, qt + kTile, t0, r0, w.lq, d2);
   };
   auto write_stats = [&](int buf) {
-    if (wave == 0) {
+    if (tid < kTurnRows) {
       stats[buf][0][lane] = stat.x;
       stats[buf][1][lane] = stat.y;
     }
   };
+  // Four rows' statistics for the registers 4 q .. 4 q + 3.
+  auto rows_stat = [&](const float (&x)[kTurnRows]) {
+    f32x16 r;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 y = *reinterpret_cast<const f32x4*>(&x[8 * q + 4 * half]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r[4 * q + j] = y[j];
+    }
+    return r;
+  };
 
-  if (turns > 0) {
-    stage(0, 0);
+  int this_head = next_head, this_t0 = next_t0;
+  if (turn < turns) {
+    stage(0);
     write_stats(0);
   }
   int buf = 0;
-  for (int turn = 0; turn < turns; ++turn, buf ^= 1) {
+  for (; turn < turns; ++turn, buf ^= 1) {
     staged();
     __syncthreads();
-    if (turn + 1 < turns) stage(turn + 1, buf ^ 1);
-    const int t0 = tok0 + turn % tiles * kTileKeys;
-    const char SMX_LDS* qt = lds + buf * 2 * kTile;
+    const int head = this_head, t0 = this_t0;
+    this_head = next_head;
+    this_t0 = next_t0;
+    if (turn + 1 < turns) stage(buf ^ 1);
+    const char SMX_LDS* qt = stages + buf * 2 * kTile;
     const char SMX_LDS* ot = qt + kTile;
-    const float slope =
-        SCORED && a.slopes != nullptr ? a.slopes[hk * a.group + turn / tiles] : 0.0f;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int t1 = t0 + 32 * h;
-      if (t1 >= w.lq || keys_seen(a, w, min(t1 + 31, w.lq - 1)) <= key0) continue;
-      const int lim_all = keys_seen(a, w, t1);
-      f32x16 s = rows_dot<T, DP>(rd, qt, 32 * h, k), dcap;
-      f32x16 dp = rows_dot<T, DP>(rd, ot, 32 * h, v);
+    const float slope = SCORED && a.slopes != nullptr ? a.slopes[head] : 0.0f;
+    if (keys_seen(a, w, min(t0 + kTurnRows, w.lq) - 1) > key0) {
+      const int lim_all = keys_seen(a, w, t0);
+      const TileReader<DP> rd = reader.fresh();
+      f32x16 s, dcap;
       if constexpr (SCORED) {
+        s = rows_dot<T, DP>(rd, qt, 0, k);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int tok = t1 + 8 * (i / 4) + 4 * half + i % 4;
+          const int r = 8 * (i / 4) + 4 * half + i % 4;
           float x;
-          s[i] = score16(a, s[i], slope, tok + w.lk - w.lq - key, &x);
+          s[i] = score16(a, s[i], slope, t0 + r + w.lk - w.lq - key, &x) + stats[buf][0][r];
           dcap[i] = x;
         }
+      } else {
+        s = rows_dot<T, DP>(rd, qt, 0, k, rows_stat(stats[buf][0]));
       }
+      f32x16 dp = rows_stat(stats[buf][1]);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = 32 * h + 8 * (i / 4) + 4 * half + i % 4;
-        s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -stats[buf][0][r]));
-        dp[i] -= stats[buf][1][r];
-      }
+      for (int st = 0; st < DP / 16; ++st)
+        dp = mfma32(rd.template rows<T>(ot, 0, st), rd.template rows<T>(vt, 0, st), dp);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
       if (lim_all < key0 + 32) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int tok = t1 + 8 * (i / 4) + 4 * half + i % 4;
+          const int tok = t0 + 8 * (i / 4) + 4 * half + i % 4;
           if (key >= keys_seen(a, w, tok)) s[i] = 0.0f;
         }
       }
@@ -331,15 +429,49 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
         if constexpr (SCORED) dp[i] *= dcap[i];
       }
       const bool two_parts = key0 < kTileKeys && lim_all <= kTwoPartKeys;
-      cols_accumulate<T, DP>(rd, ot, 32 * h, s, two_parts, dv);
-      cols_accumulate<T, DP>(rd, qt, 32 * h, dp, two_parts, dk);
+      cols_accumulate<T, DP>(rd, ot, 0, s, two_parts, dv);
+      cols_accumulate<T, DP>(rd, qt, 0, dp, two_parts, dk);
     }
     write_stats(buf ^ 1);
   }
   if (!valid) return;
-  const int64_t out = (token * a.kv_heads + hk) * a.d;
-  store_columns<T, DP>(static_cast<T*>(a.dk) + out, a.d, half, dk, a.scale);
-  store_columns<T, DP>(static_cast<T*>(a.dv) + out, a.d, half, dv, 1.0f);
+  const int64_t row = token * a.kv_heads + hk;
+  if (split) {
+    const int64_t rows = static_cast<int64_t>(a.tokens_k) * a.kv_heads;
+    float* p = a.part_o + ((2 * static_cast<int64_t>(blockIdx.y)) * rows + row) * a.d;
+    store_columns<float, DP>(p, a.d, half, dk, 1.0f);
+    store_columns<float, DP>(p + rows * a.d, a.d, half, dv, 1.0f);
+    return;
+  }
+  store_columns<T, DP>(static_cast<T*>(a.dk) + row * a.d, a.d, half, dk, a.scale);
+  store_columns<T, DP>(static_cast<T*>(a.dv) + row * a.d, a.d, half, dv, 1.0f);
+}
+
+// Sums the splits of a key tile's gradients.
+template <typename T>
+__global__ __launch_bounds__(256) void k_heads_sum(HeadsArgs a) {
+  const int hk = blockIdx.x % a.kv_heads;
+  const DocTile w = key_tile(a, blockIdx.x / a.kv_heads);
+  const int first = w.tile * kTileRows;
+  if (first >= w.lk) return;
+  const KeyTurns kt = key_turns(a, w, first);
+  const int chunk = split_turns(a);
+  if (chunk == 0 || kt.turns <= chunk) return;
+  const int count = (kt.turns + chunk - 1) / chunk;
+  const int64_t rows = static_cast<int64_t>(a.tokens_k) * a.kv_heads;
+  const int quads = a.d / 4, keys = min(w.lk - first, kTileRows);
+  for (int i = threadIdx.x; i < keys * quads; i += 256) {
+    const int64_t row = static_cast<int64_t>(w.k0 + first + i / quads) * a.kv_heads + hk;
+    const int64_t at = row * a.d + i % quads * 4;
+    f32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+    for (int s = 0; s < count; ++s) {
+      const float* p = a.part_o + 2 * static_cast<int64_t>(s) * rows * a.d + at;
+      k += *reinterpret_cast<const f32x4*>(p);
+      v += *reinterpret_cast<const f32x4*>(p + rows * a.d);
+    }
+    store4(static_cast<T*>(a.dk) + at, k * a.scale);
+    store4(static_cast<T*>(a.dv) + at, v);
+  }
 }
 
 }  // namespace smx

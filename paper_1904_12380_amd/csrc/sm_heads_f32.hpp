@@ -24,16 +24,8 @@ constexpr int kF32Rows = 64;   // rows (or keys) of a workgroup
 constexpr int kF32Step = 32;   // keys (or rows) of a staged tile
 constexpr int kF32Threads = 256;
 
-template <typename T>
-__device__ __forceinline__ f32x4 load4(const T* p) {
-  if constexpr (sizeof(T) == 4) {
-    return *reinterpret_cast<const f32x4*>(p);
-  } else {
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    const t4 v = *reinterpret_cast<const t4*>(p);
-    return f32x4{static_cast<float>(v[0]), static_cast<float>(v[1]), static_cast<float>(v[2]),
-                 static_cast<float>(v[3])};
-  }
+__device__ __forceinline__ f32x4 load4(const float* p) {
+  return *reinterpret_cast<const f32x4*>(p);
 }
 
 template <typename T>
@@ -66,8 +58,8 @@ __device__ __forceinline__ float score_f32(const HeadsArgs& a, float dot, float 
 
 // One row (of 16) of a register operand: element 4 t + j of the lane is
 // column 16 t + 4 (l / 16) + j of the row, 0 past d.
-template <typename T, int DP>
-__device__ __forceinline__ void load_row(f32x4 (&r)[DP / 16], const T* row, bool valid, int g,
+template <int DP>
+__device__ __forceinline__ void load_row(f32x4 (&r)[DP / 16], const float* row, bool valid, int g,
                                          int d) {
 #pragma unroll
   for (int t = 0; t < DP / 16; ++t) {
@@ -104,7 +96,7 @@ __device__ __forceinline__ void tile_accumulate(f32x4 (&acc)[DP / 16],
   }
 }
 
-template <typename T, int DP, bool PAGED>
+template <int DP, bool PAGED>
 __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) float ks[kF32Step][DP + 4];
   __shared__ __attribute__((aligned(16))) float vs[kF32Step][DP + 4];
@@ -135,7 +127,7 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
   const int64_t token = w.q0 + tok;
 
   f32x4 q[DP / 16];
-  load_row<T, DP>(q, static_cast<const T*>(a.q.data) + token * a.q.ts + head * a.q.hs, valid, g,
+  load_row<DP>(q, static_cast<const float*>(a.q.data) + token * a.q.ts + head * a.q.hs, valid, g,
                   a.d);
   f32x4 acc[DP / 16] = {};
   float m = -INFINITY, l = 0.0f;
@@ -157,8 +149,8 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
           vr = static_cast<int64_t>(w.k0 + j) * a.v.ts;
         }
         if (have && col < a.d) {
-          x = load4(static_cast<const T*>(a.k.data) + kr + hk * a.k.hs + col);
-          y = load4(static_cast<const T*>(a.v.data) + vr + hk * a.v.hs + col);
+          x = load4(static_cast<const float*>(a.k.data) + kr + hk * a.k.hs + col);
+          y = load4(static_cast<const float*>(a.v.data) + vr + hk * a.v.hs + col);
         }
       }
       *reinterpret_cast<f32x4*>(&ks[r][col]) = x;
@@ -220,11 +212,11 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
 #pragma unroll
   for (int t = 0; t < DP / 16; ++t)
     if (16 * t + 4 * g < a.d)
-      store4(static_cast<T*>(a.out) + out * a.d + 16 * t + 4 * g, acc[t] * inv);
+      store4(static_cast<float*>(a.out) + out * a.d + 16 * t + 4 * g, acc[t] * inv);
 }
 
 // D of every row and the gradient of the queries.
-template <typename T, int DP>
+template <int DP>
 __global__ __launch_bounds__(kF32Threads) void k_heads_dq_f32(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) float ks[kF32Step][DP + 4];
   __shared__ __attribute__((aligned(16))) float vs[kF32Step][DP + 4];
@@ -250,14 +242,14 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dq_f32(HeadsArgs a) {
   const int64_t token = w.q0 + tok, out = token * a.heads + head;
 
   f32x4 q[DP / 16], dout[DP / 16];
-  load_row<T, DP>(q, static_cast<const T*>(a.q.data) + token * a.q.ts + head * a.q.hs, valid, g,
+  load_row<DP>(q, static_cast<const float*>(a.q.data) + token * a.q.ts + head * a.q.hs, valid, g,
                   a.d);
-  load_row<T, DP>(dout, static_cast<const T*>(a.dout.data) + token * a.dout.ts + head * a.dout.hs,
+  load_row<DP>(dout, static_cast<const float*>(a.dout.data) + token * a.dout.ts + head * a.dout.hs,
                   valid, g, a.d);
   float delta = 0.0f;
   {
     f32x4 o[DP / 16];
-    load_row<T, DP>(o, static_cast<const T*>(a.o.data) + token * a.o.ts + head * a.o.hs, valid, g,
+    load_row<DP>(o, static_cast<const float*>(a.o.data) + token * a.o.ts + head * a.o.hs, valid, g,
                     a.d);
 #pragma unroll
     for (int t = 0; t < DP / 16; ++t)
@@ -276,8 +268,8 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dq_f32(HeadsArgs a) {
       f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
       if (j < to && col < a.d) {
         const int64_t at = w.k0 + j;
-        x = load4(static_cast<const T*>(a.k.data) + at * a.k.ts + hk * a.k.hs + col);
-        y = load4(static_cast<const T*>(a.v.data) + at * a.v.ts + hk * a.v.hs + col);
+        x = load4(static_cast<const float*>(a.k.data) + at * a.k.ts + hk * a.k.hs + col);
+        y = load4(static_cast<const float*>(a.v.data) + at * a.v.ts + hk * a.v.hs + col);
       }
       *reinterpret_cast<f32x4*>(&ks[r][col]) = x;
       *reinterpret_cast<f32x4*>(&vs[r][col]) = y;
@@ -303,12 +295,12 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dq_f32(HeadsArgs a) {
 #pragma unroll
   for (int t = 0; t < DP / 16; ++t)
     if (16 * t + 4 * g < a.d)
-      store4(static_cast<T*>(a.out) + out * a.d + 16 * t + 4 * g, acc[t] * a.scale);
+      store4(static_cast<float*>(a.out) + out * a.d + 16 * t + 4 * g, acc[t] * a.scale);
 }
 
 // The gradients of the keys and values: 64 keys per workgroup, against the
 // rows of their document that see any of them.
-template <typename T, int DP>
+template <int DP>
 __global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) float qs[kF32Step][DP + 4];
   __shared__ __attribute__((aligned(16))) float os[kF32Step][DP + 4];
@@ -333,9 +325,9 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
   const int64_t token = w.k0 + key;
 
   f32x4 k[DP / 16], v[DP / 16];
-  load_row<T, DP>(k, static_cast<const T*>(a.k.data) + token * a.k.ts + hk * a.k.hs, valid, g,
+  load_row<DP>(k, static_cast<const float*>(a.k.data) + token * a.k.ts + hk * a.k.hs, valid, g,
                   a.d);
-  load_row<T, DP>(v, static_cast<const T*>(a.v.data) + token * a.v.ts + hk * a.v.hs, valid, g,
+  load_row<DP>(v, static_cast<const float*>(a.v.data) + token * a.v.ts + hk * a.v.hs, valid, g,
                   a.d);
   f32x4 dk[DP / 16] = {}, dv[DP / 16] = {};
 
@@ -350,8 +342,8 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
       if (row < rows && col < a.d) {
         const int64_t at = w.q0 + row / a.group;
         const int head = hk * a.group + row % a.group;
-        x = load4(static_cast<const T*>(a.q.data) + at * a.q.ts + head * a.q.hs + col);
-        y = load4(static_cast<const T*>(a.dout.data) + at * a.dout.ts + head * a.dout.hs + col);
+        x = load4(static_cast<const float*>(a.q.data) + at * a.q.ts + head * a.q.hs + col);
+        y = load4(static_cast<const float*>(a.dout.data) + at * a.dout.ts + head * a.dout.hs + col);
       }
       *reinterpret_cast<f32x4*>(&qs[r][col]) = x;
       *reinterpret_cast<f32x4*>(&os[r][col]) = y;
@@ -390,8 +382,8 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
   for (int t = 0; t < DP / 16; ++t) {
     const int col = 16 * t + 4 * g;
     if (col < a.d) {
-      store4(static_cast<T*>(a.dk) + out + col, dk[t] * a.scale);
-      store4(static_cast<T*>(a.dv) + out + col, dv[t]);
+      store4(static_cast<float*>(a.dk) + out + col, dk[t] * a.scale);
+      store4(static_cast<float*>(a.dv) + out + col, dv[t]);
     }
   }
 }

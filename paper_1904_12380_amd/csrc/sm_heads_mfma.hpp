@@ -69,12 +69,14 @@ constexpr unsigned kFar = 0x80000000u;  // past every buffer
 // put a barrier between a stage's last read and its next load.
 typedef int s32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void load_lds(s32x4 rsrc, unsigned off, unsigned lds) {
+  lds = __builtin_amdgcn_readfirstlane(lds);
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                :
                : "v"(off), "s"(rsrc), "s"(lds)
                : "memory");
 }
 __device__ __forceinline__ void load_lds(const char* p, unsigned lds) {
+  lds = __builtin_amdgcn_readfirstlane(lds);
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                :
                : "v"(p), "s"(lds)
@@ -83,10 +85,20 @@ __device__ __forceinline__ void load_lds(const char* p, unsigned lds) {
 __device__ __forceinline__ unsigned lds_offset(const char SMX_LDS* p) {
   return static_cast<unsigned>(reinterpret_cast<uintptr_t>(p));
 }
-// Waits for all loads of this wavefront.
-__device__ __forceinline__ void staged() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-// Waits for this wavefront's reads of LDS.
-__device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// Waits for all loads of this wavefront (vmcnt(0)), in a form that tells the
+// compiler that its own have landed too: it would wait for them later, behind
+// the next stage's.
+__device__ __forceinline__ void staged() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70);
+  asm volatile("" ::: "memory");
+}
+// Waits for this wavefront's reads of LDS (lgkmcnt(0)).
+__device__ __forceinline__ void lds_read() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  asm volatile("" ::: "memory");
+}
 
 // What stages rows of K or V from memory into LDS.  A wavefront's instruction
 // moves 64 chunks of 16 bytes: kRows rows, lane l the chunk at place l % kChunks
@@ -115,22 +127,27 @@ struct Stager {
 };
 
 // Rows [r0, r0 + N * kRows) of the packed keys k0 .. into lds (uniform), zeros
-// past key `end` and past column d.
+// past key `end` and past column d.  Each instruction has a buffer of its own,
+// from its first row on, so that all share the lanes' offsets: as offsets from
+// one buffer they would take a register each, held across the loop.
 template <int DP, int N>
 __device__ __forceinline__ void stage_packed(const Stager<DP, false>& s, char SMX_LDS* lds, int k0,
                                              int r0, int end, int d2) {
   constexpr int kRows = Stager<DP, false>::kRows;
   const int64_t left = end - 1 - k0;
   const int64_t bytes = left < 0 ? 0 : left * s.ts2 + d2;
-  const uint64_t at = reinterpret_cast<uint64_t>(s.base + k0 * s.ts2);
-  const s32x4 rsrc = {static_cast<int>(at), static_cast<int>(at >> 32 & 0xffff),
-                      static_cast<int>(bytes < 0x7fffffff ? bytes : 0x7fffffff), 0x00027000};
-  const unsigned step = static_cast<unsigned>(s.ts2);
+  const int all = static_cast<int>(bytes < 0x7fffffff ? bytes : 0x7fffffff);
+  const int step = static_cast<int>(s.ts2);
 #pragma unroll
   for (int n = 0; n < N; ++n) {
+    const int skip = (r0 + n * kRows) * step;
+    const uint64_t at = reinterpret_cast<uint64_t>(s.base + k0 * s.ts2 + skip);
+    // Uniform, also where the compiler does not see it.
+    const s32x4 rsrc = {__builtin_amdgcn_readfirstlane(static_cast<int>(at)),
+                        __builtin_amdgcn_readfirstlane(static_cast<int>(at >> 32 & 0xffff)),
+                        __builtin_amdgcn_readfirstlane(max(all - skip, 0)), 0x00027000};
     const int col = s.column(n * kRows);
-    const unsigned off =
-        col < d2 ? (r0 + n * kRows + s.lane_row) * step + col : kFar;
+    const unsigned off = col < d2 ? s.lane_row * step + col : kFar;
     load_lds(rsrc, off, lds_offset(lds) + n * 1024);
   }
 }
@@ -180,6 +197,13 @@ __device__ __forceinline__ void load_operand(typename Vec8<T>::type (&r)[DP / 16
   }
 }
 
+// x itself, as a value that the compiler cannot see through: what is built
+// from it is built where it is used, not held in registers across a loop.
+__device__ __forceinline__ int opaque(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Reads of a staged tile.  `rows`: chunk 2 s + l / 32 of row l % 32, at LDS
 // bytes rows.at ^ (32 s); `cols`: transposed reads, of the columns 32 t.
 template <int DP>
@@ -194,6 +218,14 @@ struct TileReader {
     const int i = lane % 16, cr = 4 * half + i / 4;
     const int chunk = 2 * (lane / 16 % 2) + (i % 4) / 2;
     col_at = cr * DP * 2 + 16 * (chunk ^ swz(cr)) + 8 * (i % 2);
+  }
+
+  // The same reader with addresses built anew.
+  __device__ __forceinline__ TileReader fresh() const {
+    TileReader r = *this;
+    r.row_at = opaque(row_at);
+    r.col_at = opaque(col_at);
+    return r;
   }
 
   // A operand: rows row0 + l % 32 (row0 a multiple of 8), columns of step s.
