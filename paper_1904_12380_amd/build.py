@@ -19,7 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIBDIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIBDIR, "libsoftmax_mi355x.so")
 SOURCES = [os.path.join(CSRC, name) for name in (
-    "softmax_api.hip", "attention_api.hip", "heads_api.hip", "cache_api.hip")]
+    "softmax_api.hip", "attention_api.hip", "heads_api.hip", "heads_fwd_f16.hip",
+    "heads_fwd_bf16.hip", "heads_bwd_f16.hip", "heads_bwd_bf16.hip", "cache_api.hip")]
 PROBE_SOURCE = os.path.join(ROOT, "tests", "native", "long_rows_probe.hip")
 PROBE_LIB = os.path.join(ROOT, "tests", "native", "liblong_rows_probe.so")
 

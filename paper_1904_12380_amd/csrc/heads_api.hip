@@ -9,6 +9,7 @@
 #include "sm_heads_bwd.hpp"
 #include "sm_heads_f32.hpp"
 #include "sm_heads_host.hpp"
+#include "sm_heads_launch.hpp"
 #include "sm_heads_mfma.hpp"
 
 namespace {
@@ -51,57 +52,45 @@ hipError_t launch2(const void* fn, int64_t x, int64_t y, int block, HeadsArgs* a
                          dim3(block), args, 0, s);
 }
 
-// The instance of a head width: its columns padded to 64, 128 or 256.
-#define SMX_FN(...) reinterpret_cast<const void*>(&__VA_ARGS__)
-#define SMX_BY_WIDTH(d, K, T, ...)                                                    \
-  ((d) <= 64 ? SMX_FN(K<T, 64, __VA_ARGS__>)                                          \
-             : (d) <= 128 ? SMX_FN(K<T, 128, __VA_ARGS__>) : SMX_FN(K<T, 256, __VA_ARGS__>))
-#define SMX_BY_WIDTH_F32(d, K)                                                        \
-  ((d) <= 64 ? SMX_FN(K<64>) : (d) <= 128 ? SMX_FN(K<128>) : SMX_FN(K<256>))
-
-// Scores are more than a dot product times a scale of ordinary size.
-bool scored(const HeadsArgs& a) {
-  return a.cap > 0.0f || a.slopes != nullptr || !(std::fabs(a.scale) > 1e-20f);
-}
-
-template <typename T, bool PAGED>
-const void* fwd_16(const HeadsArgs& a) {
-  return scored(a) ? SMX_BY_WIDTH(a.d, k_heads_fwd, T, PAGED, true)
-                   : SMX_BY_WIDTH(a.d, k_heads_fwd, T, PAGED, false);
-}
-
 template <bool PAGED>
-const void* fwd_fn(int dtype, const HeadsArgs& a) {
-  return dtype == SOFTMAX_F32
-             ? (a.d <= 64    ? SMX_FN(k_heads_fwd_f32<64, PAGED>)
-                : a.d <= 128 ? SMX_FN(k_heads_fwd_f32<128, PAGED>)
-                             : SMX_FN(k_heads_fwd_f32<256, PAGED>))
-         : dtype == SOFTMAX_F16 ? fwd_16<f16, PAGED>(a)
-                                : fwd_16<bf16, PAGED>(a);
+const void* fwd_f32(const HeadsArgs& a) {
+  return a.d <= 64    ? SMX_FN(k_heads_fwd_f32<64, PAGED>)
+         : a.d <= 128 ? SMX_FN(k_heads_fwd_f32<128, PAGED>)
+                      : SMX_FN(k_heads_fwd_f32<256, PAGED>);
 }
 
-template <typename T>
-const void* dq_16(const HeadsArgs& a) {
-  return scored(a) ? SMX_BY_WIDTH(a.d, k_heads_dq, T, true)
-                   : SMX_BY_WIDTH(a.d, k_heads_dq, T, false);
+const void* packed_fn(int dtype, const HeadsArgs& a) {
+  return dtype == SOFTMAX_F32   ? fwd_f32<false>(a)
+         : dtype == SOFTMAX_F16 ? heads_fwd_f16(a, kPacked)
+                                : heads_fwd_bf16(a, kPacked);
 }
 
-template <typename T>
-const void* dkv_16(const HeadsArgs& a) {
-  return scored(a) ? SMX_BY_WIDTH(a.d, k_heads_dkv, T, true)
-                   : SMX_BY_WIDTH(a.d, k_heads_dkv, T, false);
+const void* paged_fn(int dtype, const HeadsArgs& a) {
+  const int where = 1 << a.log_block >= kGroup ? kBlocks : kSmallBlocks;
+  return dtype == SOFTMAX_F32   ? fwd_f32<true>(a)
+         : dtype == SOFTMAX_F16 ? heads_fwd_f16(a, where)
+                                : heads_fwd_bf16(a, where);
 }
+
+#define SMX_BY_WIDTH_F32(d, K) \
+  ((d) <= 64 ? SMX_FN(K<64>) : (d) <= 128 ? SMX_FN(K<128>) : SMX_FN(K<256>))
 
 const void* dq_fn(int dtype, const HeadsArgs& a) {
   return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, k_heads_dq_f32)
-         : dtype == SOFTMAX_F16 ? dq_16<f16>(a)
-                                : dq_16<bf16>(a);
+         : dtype == SOFTMAX_F16 ? heads_dq_f16(a)
+                                : heads_dq_bf16(a);
 }
 
 const void* dkv_fn(int dtype, const HeadsArgs& a) {
   return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, k_heads_dkv_f32)
-         : dtype == SOFTMAX_F16 ? dkv_16<f16>(a)
-                                : dkv_16<bf16>(a);
+         : dtype == SOFTMAX_F16 ? heads_dkv_f16(a)
+                                : heads_dkv_bf16(a);
+}
+
+const void* join_fn(int dtype) {
+  return dtype == SOFTMAX_F32   ? SMX_FN(k_heads_join<float, kF32Rows>)
+         : dtype == SOFTMAX_F16 ? SMX_FN(k_heads_join<f16, kTileRows>)
+                                : SMX_FN(k_heads_join<bf16, kTileRows>);
 }
 
 const void* sum_fn(int dtype) {
@@ -112,12 +101,6 @@ const void* sum_fn(int dtype) {
 // kF32Threads = kTileThreads threads.
 int tile_rows(int dtype) { return dtype == SOFTMAX_F32 ? kF32Rows : kTileRows; }
 static_assert(kF32Threads == kTileThreads, "one launch shape");
-
-const void* join_fn(int dtype) {
-  return dtype == SOFTMAX_F32 ? reinterpret_cast<const void*>(&k_heads_join<float, kF32Rows>)
-         : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_heads_join<f16, kTileRows>)
-                                : reinterpret_cast<const void*>(&k_heads_join<bf16, kTileRows>);
-}
 
 // Splits of the keys to launch: enough that the call's tiles fill `target`
 // workgroups, no more than the longest request has chunks of, at most 64.
@@ -207,7 +190,7 @@ SOFTMAX_API int softmax_packed_attention_fwd(const softmax_heads_t* q, const sof
   a.cu_k = cu_k;
   const int64_t slots = tile_slots(q->tokens * a.group, docs, tile_rows(dtype));
   const hipError_t e =
-      launch2(fwd_fn<false>(dtype, a), slots * a.kv_heads, 1, kTileThreads, &a, stream);
+      launch2(packed_fn(dtype, a), slots * a.kv_heads, 1, kTileThreads, &a, stream);
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
 }
 
@@ -371,7 +354,7 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
   a.part_ml = a.part_o + splits * rows * q->d;
   const int64_t slots = tile_slots(q->tokens * a.group, requests, tile_rows(dtype));
   hipError_t e =
-      launch2(fwd_fn<true>(dtype, a), slots * a.kv_heads, splits, kTileThreads, &a, stream);
+      launch2(paged_fn(dtype, a), slots * a.kv_heads, splits, kTileThreads, &a, stream);
   if (e == hipSuccess && splits > 1)
     e = launch2(join_fn(dtype), ceil_div(rows, 4), 1, 256, &a, stream);
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);

@@ -1,0 +1,20 @@
+// Instances of the attention forward kernel for f16.
+#include "sm_heads_launch.hpp"
+#include "sm_heads_mfma.hpp"
+
+namespace smx {
+
+template <int WHERE>
+static const void* fwd(const HeadsArgs& a) {
+  switch (score_mode(a)) {
+    case kPlain: return SMX_BY_WIDTH(a.d, k_heads_fwd, f16, WHERE, kPlain);
+    case kBias: return SMX_BY_WIDTH(a.d, k_heads_fwd, f16, WHERE, kBias);
+    default: return SMX_BY_WIDTH(a.d, k_heads_fwd, f16, WHERE, kCap);
+  }
+}
+
+const void* heads_fwd_f16(const HeadsArgs& a, int where) {
+  return where == kPacked ? fwd<kPacked>(a) : where == kBlocks ? fwd<kBlocks>(a) : fwd<kSmallBlocks>(a);
+}
+
+}  // namespace smx

@@ -19,10 +19,6 @@
 
 namespace smx {
 
-// Weights and score gradients are taken in two 16-bit parts for the first 64
-// keys of a document where rows see at most this many keys.
-constexpr int kTwoPartKeys = 128;
-
 template <typename T, int DP>
 __device__ __forceinline__ f32x16 rows_dot(const TileReader<DP>& rd, const char SMX_LDS* tile,
                                            int row0,
@@ -76,7 +72,7 @@ __device__ __forceinline__ void store_columns(T* p, int d, int half, const f32x1
     }
 }
 
-template <typename T, int DP, bool SCORED>
+template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) char lds_bytes[tile_lds_bytes<DP>()];
   char SMX_LDS* lds = (char SMX_LDS*)lds_bytes;
@@ -106,8 +102,8 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
     lim_all = keys_seen(a, w, (row0 + 32 * wave) / a.group);
     lim_any = keys_seen(a, w, (min(rows, row0 + 32 * wave + 32) - 1) / a.group);
   }
-  const float slope = SCORED && a.slopes != nullptr ? a.slopes[head] : 0.0f;
-  const float c = SCORED ? 1.0f : fabsf(a.scale) * kLog2eF;
+  const Scoring<MODE> sc(a, MODE != kPlain && a.slopes != nullptr ? a.slopes[head] : 0.0f);
+  const float c = sc.unit();
 
   typedef typename Vec8<T>::type V;
   V q[DP / 16], dout[DP / 16];
@@ -134,32 +130,31 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
     lse2 = a.lse[out] * kLog2eF;
     if (lse2 == -INFINITY) lse2 = INFINITY;
   }
-  if (!SCORED && a.scale < 0.0f) {
+  if (MODE == kPlain && a.scale < 0.0f) {
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) q[i] = -q[i];
   }
   f32x16 acc[DP / 32] = {};
 
-  const Stager<DP, false> ks(a.k, 0, w.k0, hk), vs(a.v, 0, w.k0, hk);
   const TileReader<DP> rd;
   constexpr int kTile = kTileKeys * DP * 2;
-  constexpr int N = kTileKeys / 4 / Stager<DP, false>::kRows;
-  const int r0 = wave * (kTileKeys / 4), d2 = 2 * a.d;
+  const int r0 = wave * kGroup;
+  const KeySource<DP, kPacked, 1> keys(a, w, hk, to);
   auto stage = [&](int k0, int buf) {
     char SMX_LDS* kt = lds + buf * 2 * kTile + r0 * DP * 2;
-    stage_packed<DP, N>(ks, kt, k0, r0, to, d2);
-    stage_packed<DP, N>(vs, kt + kTile, k0, r0, to, d2);
+    keys.stage(a, keys.k, kt, k0 + r0);
+    keys.stage(a, keys.v, kt + kTile, k0 + r0);
   };
 
-  // Weights, and the scores' gradient over (dP - D), of 32 keys.
-  auto weights = [&](f32x16& s, f32x16& dcap, int k0) {
-    if constexpr (SCORED) {
+  // Weights of 32 keys from dot products; cap: what its derivative takes.
+  auto weights = [&](f32x16& s, f32x16& cap, int k0) {
+    if constexpr (MODE != kPlain) {
+      const float dist = static_cast<float>(pos - k0 - 4 * half);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int j = k0 + 8 * (i / 4) + 4 * half + i % 4;
-        float x;
-        s[i] = score16(a, s[i], slope, pos - j, &x);
-        dcap[i] = x;
+        float r = 0.0f;
+        s[i] = sc.score(s[i], dist - (8 * (i / 4) + i % 4), &r);
+        cap[i] = r;
       }
     }
 #pragma unroll
@@ -187,9 +182,9 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
       float sum = 0.0f;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        f32x16 s = rows_dot<T, DP>(rd, kt, 32 * h, q), dcap;
+        f32x16 s = rows_dot<T, DP>(rd, kt, 32 * h, q), cap;
         const f32x16 dp = rows_dot<T, DP>(rd, vt, 32 * h, dout);
-        weights(s, dcap, 32 * h);
+        weights(s, cap, 32 * h);
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum = __builtin_fmaf(s[i], dp[i], sum);
       }
@@ -198,13 +193,13 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      f32x16 s = rows_dot<T, DP>(rd, kt, 32 * h, q), dcap;
+      f32x16 s = rows_dot<T, DP>(rd, kt, 32 * h, q), cap;
       f32x16 dp = rows_dot<T, DP>(rd, vt, 32 * h, dout);
-      weights(s, dcap, k0 + 32 * h);
+      weights(s, cap, k0 + 32 * h);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         dp[i] = s[i] * (dp[i] - delta);
-        if constexpr (SCORED) dp[i] *= dcap[i];
+        if constexpr (MODE == kCap) dp[i] *= sc.derivative(cap[i]);
       }
       cols_accumulate<T, DP>(rd, kt, 32 * h, dp, two_parts, acc);
     }
@@ -283,7 +278,7 @@ constexpr int kKeyLds = (kTileRows + 2 * 2 * kTurnRows) * DP * 2;
 // A wavefront's K operand stays in registers, its V operand in LDS: with both in
 // registers (64 at a width of 128, beside 128 of sums and 32 of scores) some
 // were spilled, and a reload from scratch waits for the next stage's loads.
-template <typename T, int DP, bool SCORED>
+template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) char lds_bytes[kKeyLds<DP>];
   // Of a stage's rows: -lse / c (what a row's scores start from; scored: -lse
@@ -312,7 +307,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
   const int key = key0 + lane % 32;
   const bool valid = key < w.lk;
   const int64_t token = w.k0 + key;
-  const float c = SCORED ? 1.0f : fabsf(a.scale) * kLog2eF;
+  const float c = Scoring<MODE>(a, 0.0f).unit();
 
   typedef typename Vec8<T>::type V;
   V k[DP / 16];
@@ -320,10 +315,9 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
                       half, a.d);
   const int d2 = 2 * a.d;
   const char SMX_LDS* vt = lds + 32 * wave * DP * 2;
-  stage_packed<DP, 32 / Stager<DP, false>::kRows>(Stager<DP, false>(a.v, 0, w.k0, hk),
-                                                  lds + 32 * wave * DP * 2, first, 32 * wave, w.lk,
-                                                  d2);
-  if (!SCORED && a.scale < 0.0f) {
+  Stager<DP>(a.v, 0, w.k0, hk)
+      .template packed<32 / Stager<DP>::kRows>(lds + 32 * wave * DP * 2, key0, w.lk, d2);
+  if (MODE == kPlain && a.scale < 0.0f) {
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) k[i] = -k[i];
   }
@@ -331,7 +325,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
 
   const TileReader<DP> reader;
   constexpr int kTile = kTurnRows * DP * 2;
-  constexpr int N = kTurnRows / 4 / Stager<DP, false>::kRows;
+  constexpr int N = kTurnRows / 4 / Stager<DP>::kRows;
   const int r0 = wave * (kTurnRows / 4);
   char SMX_LDS* stages = lds + kTileRows * DP * 2;
 
@@ -355,10 +349,9 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
         stat = reinterpret_cast<const float2*>(
             a.delta)[static_cast<int64_t>(head) * a.tokens_q + w.q0 + t0 + lane];
     }
-    const Stager<DP, false> qs(a.q, 0, w.q0, head), os(a.dout, 0, w.q0, head);
     char SMX_LDS* qt = stages + buf * 2 * kTile + r0 * DP * 2;
-    stage_packed<DP, N>(qs, qt, t0, r0, w.lq, d2);
-    stage_packed<DP, N>(os, qt + kTile, t0, r0, w.lq, d2);
+    Stager<DP>(a.q, 0, w.q0, head).template packed<N>(qt, t0 + r0, w.lq, d2);
+    Stager<DP>(a.dout, 0, w.q0, head).template packed<N>(qt + kTile, t0 + r0, w.lq, d2);
   };
   auto write_stats = [&](int buf) {
     if (tid < kTurnRows) {
@@ -393,19 +386,20 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
     if (turn + 1 < turns) stage(buf ^ 1);
     const char SMX_LDS* qt = stages + buf * 2 * kTile;
     const char SMX_LDS* ot = qt + kTile;
-    const float slope = SCORED && a.slopes != nullptr ? a.slopes[head] : 0.0f;
     if (keys_seen(a, w, min(t0 + kTurnRows, w.lq) - 1) > key0) {
       const int lim_all = keys_seen(a, w, t0);
       const TileReader<DP> rd = reader.fresh();
-      f32x16 s, dcap;
-      if constexpr (SCORED) {
+      f32x16 s, cap;
+      if constexpr (MODE != kPlain) {
+        const Scoring<MODE> sc(a, a.slopes != nullptr ? a.slopes[head] : 0.0f);
+        const float dist = static_cast<float>(t0 + 4 * half + w.lk - w.lq - key);
         s = rows_dot<T, DP>(rd, qt, 0, k);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int r = 8 * (i / 4) + 4 * half + i % 4;
-          float x;
-          s[i] = score16(a, s[i], slope, t0 + r + w.lk - w.lq - key, &x) + stats[buf][0][r];
-          dcap[i] = x;
+          const int r = 8 * (i / 4) + i % 4;
+          float x = 0.0f;
+          s[i] = sc.score(s[i], dist + r, &x) + stats[buf][0][r + 4 * half];
+          cap[i] = x;
         }
       } else {
         s = rows_dot<T, DP>(rd, qt, 0, k, rows_stat(stats[buf][0]));
@@ -426,7 +420,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         dp[i] *= s[i];
-        if constexpr (SCORED) dp[i] *= dcap[i];
+        if constexpr (MODE == kCap) dp[i] *= Scoring<MODE>::derivative(cap[i]);
       }
       const bool two_parts = key0 < kTileKeys && lim_all <= kTwoPartKeys;
       cols_accumulate<T, DP>(rd, ot, 0, s, two_parts, dv);

@@ -100,10 +100,16 @@ __device__ __forceinline__ void lds_read() {
   asm volatile("" ::: "memory");
 }
 
-// What stages rows of K or V from memory into LDS.  A wavefront's instruction
-// moves 64 chunks of 16 bytes: kRows rows, lane l the chunk at place l % kChunks
-// of row l / kChunks.
-template <int DP, bool PAGED>
+// Where keys lie: in packed tensors; in cache blocks of at least kGroup rows,
+// so that the rows that one wavefront stages for a group share a block; in
+// smaller blocks, where every lane looks its row's block up.
+constexpr int kPacked = 0, kBlocks = 1, kSmallBlocks = 2;
+constexpr int kGroup = 16;
+
+// What stages rows from memory into LDS.  A wavefront's instruction moves 64
+// chunks of 16 bytes: kRows rows, lane l the chunk at place l % kChunks of row
+// l / kChunks.
+template <int DP>
 struct Stager {
   static constexpr int kChunks = DP / 8;
   static constexpr int kRows = 64 / kChunks;  // per instruction
@@ -124,64 +130,127 @@ struct Stager {
   // Column byte of the lane's chunk for the instruction whose first row has
   // the low bits `low` (a constant).
   __device__ __forceinline__ int column(int low) const { return 16 * (lane_chunk ^ swz(low)); }
+
+  // N instructions' rows from `at` on into lds (uniform), of which `bytes` are
+  // there: zeros past them and past column d.  Each instruction has a buffer
+  // of its own, from its first row on, so that all share the lanes' offsets:
+  // as offsets from one buffer they would take a register each, held across
+  // the loop.
+  template <int N>
+  __device__ __forceinline__ void rows(const char* at, int bytes, char SMX_LDS* lds,
+                                       int d2) const {
+    const int step = static_cast<int>(ts2);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int skip = n * kRows * step;
+      const uint64_t p = reinterpret_cast<uint64_t>(at + skip);
+      // Uniform, also where the compiler does not see it.
+      const s32x4 rsrc = {__builtin_amdgcn_readfirstlane(static_cast<int>(p)),
+                          __builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32 & 0xffff)),
+                          __builtin_amdgcn_readfirstlane(max(bytes - skip, 0)), 0x00027000};
+      const int col = column(n * kRows);
+      const unsigned off = col < d2 ? lane_row * step + col : kFar;
+      load_lds(rsrc, off, lds_offset(lds) + n * 1024);
+    }
+  }
+
+  // Rows j, j + 1, .. of packed keys that end at `end`.
+  template <int N>
+  __device__ __forceinline__ void packed(char SMX_LDS* lds, int j, int end, int d2) const {
+    const int64_t left = end - 1 - j;
+    const int64_t bytes = left < 0 ? 0 : left * ts2 + d2;
+    rows<N>(base + j * ts2, static_cast<int>(bytes < 0x7fffffff ? bytes : 0x7fffffff), lds, d2);
+  }
 };
 
-// Rows [r0, r0 + N * kRows) of the packed keys k0 .. into lds (uniform), zeros
-// past key `end` and past column d.  Each instruction has a buffer of its own,
-// from its first row on, so that all share the lanes' offsets: as offsets from
-// one buffer they would take a register each, held across the loop.
-template <int DP, int N>
-__device__ __forceinline__ void stage_packed(const Stager<DP, false>& s, char SMX_LDS* lds, int k0,
-                                             int r0, int end, int d2) {
-  constexpr int kRows = Stager<DP, false>::kRows;
-  const int64_t left = end - 1 - k0;
-  const int64_t bytes = left < 0 ? 0 : left * s.ts2 + d2;
-  const int all = static_cast<int>(bytes < 0x7fffffff ? bytes : 0x7fffffff);
-  const int step = static_cast<int>(s.ts2);
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int skip = (r0 + n * kRows) * step;
-    const uint64_t at = reinterpret_cast<uint64_t>(s.base + k0 * s.ts2 + skip);
-    // Uniform, also where the compiler does not see it.
-    const s32x4 rsrc = {__builtin_amdgcn_readfirstlane(static_cast<int>(at)),
-                        __builtin_amdgcn_readfirstlane(static_cast<int>(at >> 32 & 0xffff)),
-                        __builtin_amdgcn_readfirstlane(max(all - skip, 0)), 0x00027000};
-    const int col = s.column(n * kRows);
-    const unsigned off = col < d2 ? s.lane_row * step + col : kFar;
-    load_lds(rsrc, off, lds_offset(lds) + n * 1024);
-  }
-}
+// Keys of one request or document as a wavefront stages them, in groups of
+// kGroup rows.  For blocks, the ids of the groups to stage next are looked up
+// a stage ahead.
+template <int DP, int WHERE, int GROUPS>
+struct KeySource {
+  static constexpr int kRows = Stager<DP>::kRows;
+  static constexpr int kPer = kGroup / kRows;  // instructions of a group
+  Stager<DP> k, v;
+  int end, d2;
+  const int* table;
+  int ids[WHERE == kSmallBlocks ? GROUPS * kPer : GROUPS];
 
-// Block ids of the rows that a lane stages: rows r0 + n * kRows + lane_row of
-// the keys k0 ..; -1 past `end` and for entries outside the cache.
-template <int DP, int N>
-__device__ __forceinline__ void page_ids(const HeadsArgs& a, const Stager<DP, true>& s, int b,
-                                         int k0, int r0, int end, int (&ids)[N]) {
-  const int* table = a.table + static_cast<int64_t>(b) * a.width;
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int j = k0 + r0 + n * Stager<DP, true>::kRows + s.lane_row;
-    int id = -1;
-    if (j < end) id = table[j >> a.log_block];
-    ids[n] = static_cast<unsigned>(id) < static_cast<uint64_t>(a.blocks) ? id : -1;
+  __device__ __forceinline__ KeySource(const HeadsArgs& a, const DocTile& w, int hk, int to)
+      : k(a.k, a.k_bs, w.k0, hk), v(a.v, a.v_bs, w.k0, hk), end(to), d2(2 * a.d) {
+    table = WHERE == kPacked ? nullptr : a.table + static_cast<int64_t>(w.b) * a.width;
   }
-}
 
-template <int DP, int N>
-__device__ __forceinline__ void stage_paged(const HeadsArgs& a, const Stager<DP, true>& s,
-                                            char SMX_LDS* lds, int k0, int r0, int d2,
-                                            const int (&ids)[N]) {
-  const int mask = (1 << a.log_block) - 1;
+  // Looks the blocks of rows j .. up: -1 past the end and outside the cache.
+  __device__ __forceinline__ void look_up(const HeadsArgs& a, int j) {
+    if constexpr (WHERE == kBlocks) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int j = k0 + r0 + n * Stager<DP, true>::kRows + s.lane_row;
-    const int col = s.column(n * Stager<DP, true>::kRows);
-    const char* p = s.base + static_cast<int64_t>(ids[n]) * s.bs2 +
-                    static_cast<int64_t>(j & mask) * s.ts2 + col;
-    if (ids[n] < 0 || col >= d2) p = reinterpret_cast<const char*>(&g_heads_zero);
-    load_lds(p, lds_offset(lds) + n * 1024);
+      for (int g = 0; g < GROUPS; ++g) {
+        const int at = j + g * kGroup;
+        int id = -1;
+        if (at < end) id = table[at >> a.log_block];
+        ids[g] = static_cast<unsigned>(id) < static_cast<uint64_t>(a.blocks) ? id : -1;
+      }
+    } else if constexpr (WHERE == kSmallBlocks) {
+#pragma unroll
+      for (int n = 0; n < GROUPS * kPer; ++n) {
+        const int at = j + n * kRows + k.lane_row;
+        int id = -1;
+        if (at < end) id = table[at >> a.log_block];
+        ids[n] = static_cast<unsigned>(id) < static_cast<uint64_t>(a.blocks) ? id : -1;
+      }
+    }
   }
-}
+
+  // Rows of the groups that were looked up and are not there, a bit each.
+  __device__ __forceinline__ unsigned absent() const {
+    unsigned mask = 0;
+    if constexpr (WHERE == kBlocks) {
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g)
+        if (ids[g] < 0) mask |= 0xffffu << (g * kGroup);
+    } else if constexpr (WHERE == kSmallBlocks) {
+#pragma unroll
+      for (int n = 0; n < GROUPS * kPer; ++n) {
+        const uint64_t lanes = __ballot(ids[n] < 0);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+          mask |= static_cast<unsigned>(lanes >> (r * Stager<DP>::kChunks) & 1)
+                  << (n * kRows + r);
+      }
+    }
+    return mask;
+  }
+
+  // Rows j .. (looked up before) of K or V.
+  __device__ __forceinline__ void stage(const HeadsArgs& a, const Stager<DP>& s,
+                                        char SMX_LDS* lds, int j) const {
+    if constexpr (WHERE == kPacked) {
+      s.template packed<GROUPS * kPer>(lds, j, end, d2);
+    } else if constexpr (WHERE == kBlocks) {
+      const int mask = (1 << a.log_block) - 1;
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) {
+        const int at = j + g * kGroup;
+        const int count = ids[g] < 0 ? 0 : min(end - at, kGroup);
+        const char* p = s.base + static_cast<int64_t>(max(ids[g], 0)) * s.bs2 +
+                        static_cast<int64_t>(at & mask) * s.ts2;
+        s.template rows<kPer>(p, count > 0 ? (count - 1) * static_cast<int>(s.ts2) + d2 : 0,
+                              lds + g * kGroup * DP * 2, d2);
+      }
+    } else {
+      const int mask = (1 << a.log_block) - 1;
+#pragma unroll
+      for (int n = 0; n < GROUPS * kPer; ++n) {
+        const int at = j + n * kRows + s.lane_row;
+        const int col = s.column(n * kRows);
+        const char* p = s.base + static_cast<int64_t>(ids[n]) * s.bs2 +
+                        static_cast<int64_t>(at & mask) * s.ts2 + col;
+        if (ids[n] < 0 || col >= d2) p = reinterpret_cast<const char*>(&g_heads_zero);
+        load_lds(p, lds_offset(lds) + n * 1024);
+      }
+    }
+  }
+};
 
 // The lane's row of Q (or of dO) as the B operand of DP / 16 steps: columns 16 s + 8
 // (l / 32) + j, 0 past d and for rows that are not there.
@@ -269,25 +338,46 @@ __device__ __forceinline__ typename Vec8<T>::type pack8_rest(const f32x16& x, in
   return r;
 }
 
-// The score of a dot product in units of 1 / log2 e, and the derivative of the
-// cap.  tanh(y) = 1 - 2 / (e^2y + 1): within 2e-7, which the weights' rounding
-// to 16 bits covers (up to caps of 1000).
-__device__ __forceinline__ float score16(const HeadsArgs& a, float dot, float slope, int dist,
-                                         float* dcap) {
-  float x = dot * a.scale;
-  *dcap = 1.0f;
-  if (a.cap > 0.0f) {
-    const float e = __builtin_amdgcn_exp2f(x * a.exp_cap);  // e^(2 x / cap)
-    const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
-    x = a.cap * t;
-    *dcap = 1.0f - t * t;
+// How scores are formed (a template argument): scaled, with a bias, or with a
+// cap and a bias (of slope 0 where there is none).
+constexpr int kPlain = 0, kBias = 1, kCap = 2;
+
+// Scores in powers of two from dot products.  tanh(y) = 1 - 2 r with r = 1 /
+// (e^2y + 1), so that the capped score is one fma of r, and the cap's
+// derivative 1 - tanh^2 is 4 r (1 - r).  Within 2e-7 of the cap, which the
+// weights' rounding to 16 bits covers (up to caps of 1000).
+template <int MODE>
+struct Scoring {
+  float c;       // scale in powers of two (kCap: of e^2y)
+  float cap2;    // the cap in powers of two
+  float slope2;  // the slope in powers of two
+
+  __device__ __forceinline__ Scoring(const HeadsArgs& a, float slope) {
+    c = MODE == kPlain ? fabsf(a.scale) * kLog2eF
+        : MODE == kBias ? a.scale * kLog2eF : a.scale * a.exp_cap;
+    cap2 = a.cap * kLog2eF;
+    slope2 = slope * kLog2eF;
   }
-  return (x - slope * static_cast<float>(abs(dist))) * kLog2eF;
-}
+  // The score of a dot product at a distance; *r: for the derivative.
+  __device__ __forceinline__ float score(float dot, float dist, float* r) const {
+    if constexpr (MODE == kBias) return __builtin_fmaf(dot, c, -slope2 * fabsf(dist));
+    *r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(dot * c) + 1.0f);
+    return __builtin_fmaf(*r, -2.0f * cap2, __builtin_fmaf(-slope2, fabsf(dist), cap2));
+  }
+  __device__ __forceinline__ static float derivative(float r) {
+    return __builtin_fmaf(-4.0f * r, r, 4.0f * r);
+  }
+  // Powers of two per unit of what score() (kPlain: the dot product) gives.
+  __device__ __forceinline__ float unit() const { return MODE == kPlain ? c : 1.0f; }
+};
 
 // Scores below every real one, of keys that a row does not see: finite, so
 // that products with the scale stay ordered.
 constexpr float kUnseen = -3.0e38f;
+
+// Weights and score gradients are taken in two 16-bit parts for the first 64
+// keys of a document where rows see at most this many keys.
+constexpr int kTwoPartKeys = 128;
 
 // A running maximum is moved (and the sums rescaled) when a score passes it by
 // this many powers of two: weights then stay below 2^8, and most tiles
@@ -301,18 +391,16 @@ struct RowState {
   f32x16 acc[DP / 32];
   float m, l;        // m in units of the scores, times c in powers of two
   float c;           // powers of two per unit of score
-  float slope;
   int pos, lim;
   int lim_all, lim_any;  // keys that every row, and any row, of the wavefront sees
 };
 
 // Scores of KT * 32 keys from k0, staged at ktile, their softmax and the
 // product with the values at vtile.
-template <typename T, int DP, bool SCORED, int KT>
-__device__ __forceinline__ void attend(const HeadsArgs& a, RowState<T, DP>& w,
+template <typename T, int DP, int MODE, int KT>
+__device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>& w,
                                        const TileReader<DP>& rd, const char SMX_LDS* ktile,
-                                       const char SMX_LDS* vtile, int k0,
-                                       uint64_t absent) {
+                                       const char SMX_LDS* vtile, int k0, uint64_t absent) {
   typedef typename Vec8<T>::type V;
   const int half = static_cast<int>(__lane_id()) / 32;
   f32x16 s[KT] = {};
@@ -322,14 +410,14 @@ __device__ __forceinline__ void attend(const HeadsArgs& a, RowState<T, DP>& w,
     for (int kt = 0; kt < KT; ++kt)
       s[kt] = mfma32(rd.template rows<T>(ktile, 32 * kt, st), w.q[st], s[kt]);
   }
-  if constexpr (SCORED) {
+  if constexpr (MODE != kPlain) {
+    const float dist = static_cast<float>(w.pos - k0 - 4 * half);
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int j = k0 + 32 * kt + 8 * (i / 4) + 4 * half + i % 4;
-        float dcap;
-        s[kt][i] = score16(a, s[kt][i], w.slope, w.pos - j, &dcap);
+        float r;
+        s[kt][i] = sc.score(s[kt][i], dist - (32 * kt + 8 * (i / 4) + i % 4), &r);
       }
   }
   if (k0 + 32 * KT > w.lim_all || absent != 0) {
@@ -374,7 +462,9 @@ __device__ __forceinline__ void attend(const HeadsArgs& a, RowState<T, DP>& w,
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
       w.acc[t] = mfma32(rd.template cols<T>(vtile, 16 * u, t), p[u], w.acc[t]);
-  if (k0 == 0) {  // a document's first keys: what the weights' rounding left
+  // A document's first keys: what the weights' rounding left, where rows see
+  // few keys to average it.
+  if (k0 == 0 && w.lim_all <= kTwoPartKeys) {
 #pragma unroll
     for (int u = 0; u < 2 * KT; ++u) p[u] = pack8_rest<T>(s[u / 2], 8 * (u % 2), p[u]);
 #pragma unroll
@@ -385,9 +475,12 @@ __device__ __forceinline__ void attend(const HeadsArgs& a, RowState<T, DP>& w,
   }
 }
 
-template <typename T, int DP, bool PAGED, bool SCORED>
+template <typename T, int DP, int WHERE, int MODE>
 __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) char lds_bytes[tile_lds_bytes<DP>()];
+  // Rows of a stage that no block holds, a bit each, 16 from each wavefront.
+  __shared__ __attribute__((aligned(8))) unsigned short absent_rows[2][4];
+  constexpr bool PAGED = WHERE != kPacked;
   char SMX_LDS* lds = (char SMX_LDS*)lds_bytes;
   const int hk = blockIdx.x % a.kv_heads;
   const int slot = static_cast<int>(gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads);
@@ -424,96 +517,77 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
     st.lim_all = any ? min(keys_seen(a, w, first / a.group), to) : 0;
     st.lim_any = any ? min(keys_seen(a, w, last / a.group), to) : 0;
   }
-  st.slope = SCORED && a.slopes != nullptr ? a.slopes[head] : 0.0f;
-  st.c = SCORED ? 1.0f : fabsf(a.scale) * kLog2eF;
+  const Scoring<MODE> sc(a, MODE != kPlain && a.slopes != nullptr ? a.slopes[head] : 0.0f);
+  st.c = sc.unit();
   st.m = kUnseen;
   st.l = 0.0f;
   load_operand<T, DP>(st.q, static_cast<const T*>(a.q.data) + token * a.q.ts + head * a.q.hs,
                       valid, half, a.d);
-  if (!SCORED && a.scale < 0.0f) {  // the sign into q
+  if (MODE == kPlain && a.scale < 0.0f) {  // the sign into q
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) st.q[i] = -st.q[i];
   }
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) st.acc[t] = f32x16{};
 
-  const Stager<DP, PAGED> ks(a.k, a.k_bs, w.k0, hk), vs(a.v, a.v_bs, w.k0, hk);
   const TileReader<DP> rd;
-  const int d2 = 2 * a.d;
   constexpr int kRowBytes = DP * 2;
-  constexpr int kRows = Stager<DP, PAGED>::kRows;
 
   if (!few) {
     constexpr int kTile = kTileKeys * kRowBytes;
-    constexpr int N = kTileKeys / 4 / kRows;  // instructions of a wavefront per tile
-    const int r0 = wave * (kTileKeys / 4);
-    int ids[N];
-    if constexpr (PAGED) page_ids<DP, N>(a, ks, w.b, from, r0, to, ids);
+    static_assert(kTileKeys == 4 * kGroup, "a group for each wavefront");
+    KeySource<DP, WHERE, 1> keys(a, w, hk, to);
+    const int r0 = wave * kGroup;
     auto stage = [&](int k0, int buf) {
       char SMX_LDS* kt = lds + buf * 2 * kTile + r0 * kRowBytes;
+      keys.stage(a, keys.k, kt, k0 + r0);
+      keys.stage(a, keys.v, kt + kTile, k0 + r0);
       if constexpr (PAGED) {
-        stage_paged<DP, N>(a, ks, kt, k0, r0, d2, ids);
-        stage_paged<DP, N>(a, vs, kt + kTile, k0, r0, d2, ids);
-      } else {
-        stage_packed<DP, N>(ks, kt, k0, r0, to, d2);
-        stage_packed<DP, N>(vs, kt + kTile, k0, r0, to, d2);
+        absent_rows[buf][wave] = static_cast<unsigned short>(keys.absent());
+        keys.look_up(a, k0 + kTileKeys + r0);
       }
     };
-    if (from < to) stage(from, 0);
+    if (from < to) {
+      keys.look_up(a, from + r0);
+      stage(from, 0);
+    }
     int buf = 0;
     for (int k0 = from; k0 < to; k0 += kTileKeys, buf ^= 1) {
-      // Rows of this tile that hold no key, from the table.
-      uint64_t absent = 0;
-      if constexpr (PAGED) {
-        const int j = k0 + lane;
-        int id = 0;
-        if (j < to) id = a.table[static_cast<int64_t>(w.b) * a.width + (j >> a.log_block)];
-        absent = __ballot(static_cast<unsigned>(id) >= static_cast<uint64_t>(a.blocks));
-        page_ids<DP, N>(a, ks, w.b, k0 + kTileKeys, r0, to, ids);
-      }
       staged();
       __syncthreads();
-      if (k0 + kTileKeys < to) stage(k0 + kTileKeys, buf ^ 1);
-      if (k0 < st.lim_any)
-        attend<T, DP, SCORED, 2>(a, st, rd, lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile, k0,
-                                 absent);
-    }
-  } else {
-    constexpr int kKeys = 32;
-    constexpr int N = kKeys / kRows;
-    char SMX_LDS* kt = lds + wave * (2 * kKeys * kRowBytes);
-    char SMX_LDS* vt = kt + kKeys * kRowBytes;
-    int ids[N];
-    auto stage = [&](const Stager<DP, PAGED>& s, char SMX_LDS* at, int k0) {
-      if constexpr (PAGED)
-        stage_paged<DP, N>(a, s, at, k0, 0, d2, ids);
-      else
-        stage_packed<DP, N>(s, at, k0, 0, to, d2);
-    };
-    int k0 = from + wave * kKeys;
-    if constexpr (PAGED) page_ids<DP, N>(a, ks, w.b, k0, 0, to, ids);
-    if (k0 < to) {
-      stage(ks, kt, k0);
-      stage(vs, vt, k0);
-    }
-    for (; k0 < to; k0 += 4 * kKeys) {
       uint64_t absent = 0;
       if constexpr (PAGED) {
-        const int j = k0 + lane % 32;
-        int id = 0;
-        if (j < to) id = a.table[static_cast<int64_t>(w.b) * a.width + (j >> a.log_block)];
-        absent = __ballot(static_cast<unsigned>(id) >= static_cast<uint64_t>(a.blocks)) &
-                 0xffffffffu;
+        const uint2 m = *reinterpret_cast<const uint2*>(absent_rows[buf]);
+        absent = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(m.y)) << 32 |
+                 static_cast<unsigned>(__builtin_amdgcn_readfirstlane(m.x));
       }
+      if (k0 + kTileKeys < to) stage(k0 + kTileKeys, buf ^ 1);
+      if (k0 < st.lim_any)
+        attend<T, DP, MODE, 2>(sc, st, rd, lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile,
+                               k0, absent);
+    }
+  } else {
+    constexpr int kKeys = 2 * kGroup;
+    KeySource<DP, WHERE, 2> keys(a, w, hk, to);
+    char SMX_LDS* kt = lds + wave * (2 * kKeys * kRowBytes);
+    char SMX_LDS* vt = kt + kKeys * kRowBytes;
+    int k0 = from + wave * kKeys;
+    uint64_t absent = 0;
+    auto stage = [&](int j) {
+      keys.stage(a, keys.k, kt, j);
+      keys.stage(a, keys.v, vt, j);
+      absent = keys.absent();
+      keys.look_up(a, j + 4 * kKeys);
+    };
+    if (k0 < to) {
+      keys.look_up(a, k0);
+      stage(k0);
+    }
+    for (; k0 < to; k0 += 4 * kKeys) {
       staged();
-      attend<T, DP, SCORED, 1>(a, st, rd, kt, vt, k0, absent);
-      const int next = k0 + 4 * kKeys;
-      if constexpr (PAGED) page_ids<DP, N>(a, ks, w.b, next, 0, to, ids);
+      attend<T, DP, MODE, 1>(sc, st, rd, kt, vt, k0, absent);
       lds_read();
-      if (next < to) {
-        stage(ks, kt, next);
-        stage(vs, vt, next);
-      }
+      if (k0 + 4 * kKeys < to) stage(k0 + 4 * kKeys);
     }
   }
 
