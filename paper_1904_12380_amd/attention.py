@@ -115,6 +115,12 @@ def _cache(t, name: str, like) -> _Cache:
 
 def _vector(t, name: str, dtype, count, device) -> int:
     """Pointer of a contiguous vector (count None: any length)."""
+    try:
+        if t.dtype is dtype and t.device == device and t.dim() == 1 and t.is_contiguous() and \
+                (count is None or t.numel() == count):
+            return t.data_ptr()
+    except AttributeError:
+        pass  # no tensor: said below
     _tensor(t, name, 1)
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
@@ -334,9 +340,9 @@ def softmax_cache_slots(context_lens, new_lens, block_table, free_blocks, free_c
                        count, block_size, at, at + 4 * (n + 1), slots.data_ptr(), total,
                        at + 4 * (2 * n + 1), at + 4 * (2 * n + 2))),
              "softmax_cache_slots")
-    return {"table": block_table, "cu_q": sums[:n + 1], "key_lens": sums[n + 1:2 * n + 1],
-            "slots": slots, "free_count": sums[2 * n + 1:2 * n + 2],
-            "missing": sums[2 * n + 2:]}
+    cu_q, key_lens, left, missing = torch.split_with_sizes(sums, (n + 1, n, 1, 1))
+    return {"table": block_table, "cu_q": cu_q, "key_lens": key_lens, "slots": slots,
+            "free_count": left, "missing": missing}
 
 
 def softmax_cache_append(k, v, k_cache, v_cache, slots, *, stream=None) -> None:

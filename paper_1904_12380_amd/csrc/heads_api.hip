@@ -88,9 +88,9 @@ const void* dkv_fn(int dtype, const HeadsArgs& a) {
 }
 
 const void* join_fn(int dtype) {
-  return dtype == SOFTMAX_F32   ? SMX_FN(k_heads_join<float, kF32Rows>)
-         : dtype == SOFTMAX_F16 ? SMX_FN(k_heads_join<f16, kTileRows>)
-                                : SMX_FN(k_heads_join<bf16, kTileRows>);
+  return dtype == SOFTMAX_F32   ? SMX_FN(k_heads_join<float>)
+         : dtype == SOFTMAX_F16 ? SMX_FN(k_heads_join<f16>)
+                                : SMX_FN(k_heads_join<bf16>);
 }
 
 const void* sum_fn(int dtype) {
@@ -116,7 +116,7 @@ int64_t paged_splits(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t re
 }
 
 int64_t split_bytes(int64_t splits, int64_t tokens, int64_t heads, int64_t d) {
-  return splits <= 1 ? 0 : splits * tokens * heads * (d + 2) * 4;
+  return splits <= 1 ? 0 : 16 + splits * tokens * heads * (d * 4 + 16);
 }
 
 // Splits of a key tile's rows to launch in the backward pass of 16-bit types:
@@ -350,8 +350,9 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
   a.cu_k = key_lens;
   a.splits = static_cast<int>(splits);
   a.target = static_cast<int>(target);
-  a.part_o = static_cast<float*>(workspace);
-  a.part_ml = a.part_o + splits * rows * q->d;
+  a.part_head = static_cast<int*>(workspace);
+  a.part_stat = reinterpret_cast<SplitStat*>(a.part_head + 4);
+  a.part_o = reinterpret_cast<float*>(a.part_stat + splits * rows);
   const int64_t slots = tile_slots(q->tokens * a.group, requests, tile_rows(dtype));
   hipError_t e =
       launch2(paged_fn(dtype, a), slots * a.kv_heads, splits, kTileThreads, &a, stream);

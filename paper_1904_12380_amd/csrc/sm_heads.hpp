@@ -37,6 +37,13 @@ struct HeadsView {
   int64_t ts, hs;  // strides in elements between tokens and heads
 };
 
+// A row's maximum (natural units) and sum over one split of its keys, and the
+// number of its splits.
+struct SplitStat {
+  float m, l;
+  int count, pad;
+};
+
 struct HeadsArgs {
   HeadsView q, k, v, o, dout;
   void* out;         // o of the forward pass, or dq
@@ -55,8 +62,9 @@ struct HeadsArgs {
   int64_t max_keys;    // table width times block size
   int width, log_block;
   // Splits of the keys (paged).
-  float* part_o;       // [splits, tokens, heads, d]
-  float* part_ml;      // [splits, tokens, heads, 2]
+  int* part_head;        // keys per split, 0: not split
+  SplitStat* part_stat;  // [splits, tokens, heads]
+  float* part_o;         // [splits, tokens, heads, d]
   int splits;
   int target;          // workgroups that fill the device
   int n, tokens_q, tokens_k, heads, kv_heads, group, d;
@@ -150,7 +158,7 @@ __device__ __forceinline__ int keys_seen(const HeadsArgs& a, const DocTile& w, i
 // keys of all of its tiles of ROWS rows over the workgroups that fill the
 // device, in whole tiles of 64 keys, at least kMinChunk, and such that the
 // longest request fits the launched splits.  0: not split.  Every wavefront of
-// a call computes the same from the lengths.
+// a call computes the same from the lengths; the first notes it for the join.
 constexpr int kMinChunk = 256;
 
 template <int ROWS>
@@ -172,7 +180,13 @@ __device__ __forceinline__ int split_chunk(const HeadsArgs& a) {
   int64_t chunk = (sum * a.kv_heads + a.target - 1) / a.target;
   chunk = max(chunk, (longest + a.splits - 1) / a.splits);
   chunk = max((chunk + 63) / 64 * 64, static_cast<int64_t>(kMinChunk));
-  return __builtin_amdgcn_readfirstlane(chunk >= longest ? 0 : static_cast<int>(chunk));
+  const int n = __builtin_amdgcn_readfirstlane(chunk >= longest ? 0 : static_cast<int>(chunk));
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.part_head[0] = n;
+  return n;
+}
+
+__device__ __forceinline__ int split_count(int end, int chunk) {
+  return max(1, (end + chunk - 1) / chunk);
 }
 
 // Keys [from, to) of split `split` of a tile that sees the first `end`; false

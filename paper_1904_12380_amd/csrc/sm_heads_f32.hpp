@@ -109,8 +109,8 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
   doc_queries(a, &w);
   doc_keys<PAGED>(a, &w);
   const int rows = w.lq * a.group;
-  if (w.tile * kF32Rows >= rows) return;
   const int chunk = PAGED ? split_chunk<kF32Rows>(a) : 0;
+  if (w.tile * kF32Rows >= rows) return;
 
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
   const int c = lane % 16, g = lane / 16;
@@ -121,8 +121,9 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
   const int pos = tok + w.lk - w.lq;
   const int lim = valid ? keys_seen(a, w, tok) : 0;
   const int last_tok = (min(rows, (w.tile + 1) * kF32Rows) - 1) / a.group;
+  const int seen = keys_seen(a, w, last_tok);
   int from, to;
-  if (!split_range(keys_seen(a, w, last_tok), chunk, split, &from, &to)) return;
+  if (!split_range(seen, chunk, split, &from, &to)) return;
   const float slope = a.slopes != nullptr ? a.slopes[head] : 0.0f;
   const int64_t token = w.q0 + tok;
 
@@ -196,10 +197,7 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
   const int64_t out = token * a.heads + head;
   if (chunk > 0) {
     const int64_t at = split * static_cast<int64_t>(a.tokens_q) * a.heads + out;
-    if (g == 0) {
-      a.part_ml[2 * at] = m;
-      a.part_ml[2 * at + 1] = l;
-    }
+    if (g == 0) a.part_stat[at] = {m, l, split_count(seen, chunk), 0};
 #pragma unroll
     for (int t = 0; t < DP / 16; ++t)
       if (16 * t + 4 * g < a.d)
@@ -388,41 +386,40 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
   }
 }
 
-// Joins the splits of a row, one wavefront each.  The splits of the row's tile
-// follow from the lengths as in the kernel that wrote them.
-template <typename T, int ROWS>
+// Joins the splits of a row, one wavefront each, its lanes over the splits'
+// statistics and then over the columns (up to 128 of them twice, for two splits
+// at a time).
+template <typename T>
 __global__ __launch_bounds__(256) void k_heads_join(HeadsArgs a) {
-  const int chunk = split_chunk<ROWS>(a);
-  if (chunk == 0) return;
-  const int64_t out = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
+  if (a.part_head[0] == 0) return;
+  const int64_t rows = static_cast<int64_t>(a.tokens_q) * a.heads;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
   const int lane = threadIdx.x % 64;
-  if (out >= static_cast<int64_t>(a.tokens_q) * a.heads) return;
-  const int token = static_cast<int>(out / a.heads);
-  DocTile w;
-  w.b = find_doc_of_token(a.cu_q, a.n, a.tokens_q, token);
-  doc_queries(a, &w);
-  doc_keys<true>(a, &w);
-  const int row = (token - w.q0) * a.group + static_cast<int>(out % a.heads) % a.group;
-  const int end =
-      keys_seen(a, w, (min(w.lq * a.group, (row / ROWS + 1) * ROWS) - 1) / a.group);
-  const int count = max(1, (end + chunk - 1) / chunk);
-  const int64_t step = static_cast<int64_t>(a.tokens_q) * a.heads;
-  float m = -INFINITY;
-  for (int s = 0; s < count; ++s) m = fmaxf(m, a.part_ml[2 * (s * step + out)]);
-  const float base = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f;
+  if (row >= rows) return;
+  const SplitStat* stats = a.part_stat + row;
+  const int count = __builtin_amdgcn_readfirstlane(stats->count);
+  SplitStat mine = {-INFINITY, 0.0f, 0, 0};
+  if (lane < count) mine = stats[lane * rows];
+  const float m = seg_max<64>(mine.m);
+  const float weight = __builtin_amdgcn_exp2f((mine.m - (m == -INFINITY ? 0.0f : m)) * kLog2eF);
+  const float l = seg_sum<64>(mine.l * weight);
+  const int pair = a.d <= 128 ? lane / 32 : 0, step = a.d <= 128 ? 2 : 1;
+  const int col = 4 * (a.d <= 128 ? lane % 32 : lane);
   f32x4 acc = {0, 0, 0, 0};
-  for (int s = 0; s < count; ++s) {
-    const float* ml = a.part_ml + 2 * (s * step + out);
-    const float f = __builtin_amdgcn_exp2f((ml[0] - base) * kLog2eF);
-    l += ml[1] * f;
-    if (4 * lane < a.d)
-      acc += *reinterpret_cast<const f32x4*>(a.part_o + (s * step + out) * a.d + 4 * lane) * f;
+#pragma unroll 4
+  for (int s = 0; s < count; s += step) {
+    const int at = s + pair;
+    const float f = __shfl(weight, at);
+    if (at < count && col < a.d)
+      acc += *reinterpret_cast<const f32x4*>(a.part_o + (at * rows + row) * a.d + col) * f;
   }
+  if (step == 2)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] += half32_partner(acc[j]);
   const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
   if (lane == 0 && a.lse != nullptr)
-    a.lse[out] = m == -INFINITY ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2F;
-  if (4 * lane < a.d) store4(static_cast<T*>(a.out) + out * a.d + 4 * lane, acc * inv);
+    a.lse[row] = m == -INFINITY ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2F;
+  if (pair == 0 && col < a.d) store4(static_cast<T*>(a.out) + row * a.d + col, acc * inv);
 }
 
 }  // namespace smx

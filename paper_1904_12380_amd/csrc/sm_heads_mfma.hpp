@@ -491,13 +491,13 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
   doc_keys<PAGED>(a, &w);
   const int rows = w.lq * a.group;
   const int row0 = w.tile * kTileRows;
-  if (row0 >= rows) return;
   const int chunk = PAGED ? split_chunk<kTileRows>(a) : 0;
+  if (row0 >= rows) return;
   const int tile_rows = min(rows - row0, kTileRows);
   const bool few = tile_rows <= 32;
+  const int seen = keys_seen(a, w, (row0 + tile_rows - 1) / a.group);
   int from, to;
-  if (!split_range(keys_seen(a, w, (row0 + tile_rows - 1) / a.group), chunk, split, &from, &to))
-    return;
+  if (!split_range(seen, chunk, split, &from, &to)) return;
 
   const int lane = threadIdx.x % 64, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -647,10 +647,8 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
   const bool writes_stats = half == 0 && (!few || wave == 0);
   if (chunk > 0) {
     const int64_t at = split * static_cast<int64_t>(a.tokens_q) * a.heads + out;
-    if (writes_stats) {
-      a.part_ml[2 * at] = some ? m * st.c * kLn2F : -INFINITY;
-      a.part_ml[2 * at + 1] = l;
-    }
+    if (writes_stats)
+      a.part_stat[at] = {some ? m * st.c * kLn2F : -INFINITY, l, split_count(seen, chunk), 0};
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
