@@ -139,6 +139,10 @@ int64_t part_bytes(int64_t splits, int64_t tokens_k, int64_t kv_heads, int64_t d
   return splits <= 1 ? 0 : splits * tokens_k * kv_heads * d * 8;
 }
 
+// Workgroups of a join, each of four rows at a time: one that finds nothing
+// to join ends at once, but 8192 of them take 12 us to do so.
+constexpr int64_t kJoinGrid = 2048;
+
 // Workgroups that fill the device: two per CU.
 int fill_target(int64_t* target) {
   int dev = 0, cus = 0;
@@ -357,7 +361,8 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
   hipError_t e =
       launch2(paged_fn(dtype, a), slots * a.kv_heads, splits, kTileThreads, &a, stream);
   if (e == hipSuccess && splits > 1)
-    e = launch2(join_fn(dtype), ceil_div(rows, 4), 1, 256, &a, stream);
+    e = launch2(join_fn(dtype), std::min<int64_t>(ceil_div(rows, 4), kJoinGrid), 1, 256, &a,
+                stream);
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
 }
 

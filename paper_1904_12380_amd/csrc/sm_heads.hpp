@@ -13,7 +13,7 @@
 // workgroup slots from floor(s(b) / T) + b on.  Slots of different documents
 // never meet: floor((s + l) / T) + 1 >= floor(s / T) + ceil(l / T).  A slot's
 // document is the last whose first slot is not past it, found by 64-way
-// search (one step for up to 64 documents).  Tokens past the last document
+// search (one step for fewer than 64 documents).  Tokens past the last document
 // are a document of their own, without keys.
 #pragma once
 
@@ -108,44 +108,96 @@ __device__ __forceinline__ int last_at_most(int n, int t, F base) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// The document of slot t, where the documents' rows are `group` per token and
-// a tile has T of them.
-template <int T>
-__device__ __forceinline__ int find_doc(const int* cu, int n, int tokens, int group, int t,
-                                        int* tile) {
-  auto base = [&](int b) {
-    return static_cast<int>(static_cast<int64_t>(doc_start(cu, b, tokens)) * group / T) + b;
-  };
-  const int b = last_at_most(n, t, base);
-  *tile = __builtin_amdgcn_readfirstlane(t - base(b));
-  return b;
-}
-
-// The document of a token.
-__device__ __forceinline__ int find_doc_of_token(const int* cu, int n, int tokens, int token) {
-  return last_at_most(n, token, [&](int b) { return doc_start(cu, b, tokens); });
-}
+// The documents that a wavefront's lanes hold, lane b document b: with fewer
+// than 64 of them everything about a workgroup's own and about the whole call
+// follows from one load of the sums, with no load behind another.
+struct DocLanes {
+  int q0, lq, k0, lk;
+  bool live;  // a document (lane n: the tokens past the last one)
+};
 
 template <bool PAGED>
-__device__ __forceinline__ void doc_keys(const HeadsArgs& a, DocTile* w) {
-  const int b = w->b;
-  if (b >= a.n) {
-    w->k0 = 0;
-    w->lk = 0;
-  } else if constexpr (PAGED) {
-    w->k0 = 0;
-    w->lk = static_cast<int>(min(static_cast<int64_t>(max(a.cu_k[b], 0)), a.max_keys));
-  } else {
-    w->k0 = doc_start(a.cu_k, b, a.tokens_k);
-    w->lk = max(doc_start(a.cu_k, b + 1, a.tokens_k) - w->k0, 0);
+__device__ __forceinline__ DocLanes load_docs(const HeadsArgs& a, int b) {
+  DocLanes x = {0, 0, 0, 0, b < a.n};
+  if (b > a.n) return x;
+  x.q0 = doc_start(a.cu_q, b, a.tokens_q);
+  x.lq = max((x.live ? doc_start(a.cu_q, b + 1, a.tokens_q) : a.tokens_q) - x.q0, 0);
+  if constexpr (PAGED) {
+    if (x.live) x.lk = static_cast<int>(min(static_cast<int64_t>(max(a.cu_k[b], 0)), a.max_keys));
+  } else if (x.live) {
+    x.k0 = doc_start(a.cu_k, b, a.tokens_k);
+    x.lk = max(doc_start(a.cu_k, b + 1, a.tokens_k) - x.k0, 0);
   }
-  w->prefix = a.prefix != nullptr && b < a.n ? clamp_i(a.prefix[b], 0, w->lk) : 0;
+  return x;
 }
 
-__device__ __forceinline__ void doc_queries(const HeadsArgs& a, DocTile* w) {
-  w->q0 = doc_start(a.cu_q, w->b, a.tokens_q);
-  const int end = w->b >= a.n ? a.tokens_q : doc_start(a.cu_q, w->b + 1, a.tokens_q);
-  w->lq = max(end - w->q0, 0);
+// The document and tile of workgroup slot t, for tiles of T rows (`group` per
+// token) or, BY_KEYS, of T keys.  `mine`: the lanes' documents, where the call
+// has fewer than 64.
+template <int T, bool PAGED, bool BY_KEYS>
+__device__ __forceinline__ DocTile find_tile(const HeadsArgs& a, const DocLanes& mine, int t) {
+  const int* cu = BY_KEYS ? a.cu_k : a.cu_q;
+  const int tokens = BY_KEYS ? a.tokens_k : a.tokens_q;
+  const int group = BY_KEYS ? 1 : a.group;
+  auto first = [&](int start, int b) {
+    return static_cast<int>(static_cast<int64_t>(start) * group / T) + b;
+  };
+  DocTile w;
+  if (a.n < 64) {
+    const int lane = static_cast<int>(__lane_id());
+    // The tokens past the last document have queries but no keys, and the
+    // keys past it no queries.
+    const int start = !BY_KEYS ? mine.q0 : lane < a.n ? mine.k0 : 0;
+    int base = first(start, lane);
+    if (BY_KEYS && lane == a.n) base = first(doc_start(cu, a.n, tokens), lane);
+    const uint64_t at = __ballot(lane <= a.n && base <= t);
+    w.b = at == 0 ? 0 : 63 - __builtin_clzll(at);
+    w.q0 = __builtin_amdgcn_readlane(mine.q0, w.b);
+    w.lq = __builtin_amdgcn_readlane(mine.lq, w.b);
+    w.k0 = __builtin_amdgcn_readlane(mine.k0, w.b);
+    w.lk = __builtin_amdgcn_readlane(mine.lk, w.b);
+    w.tile = t - __builtin_amdgcn_readlane(base, w.b);
+  } else {
+    w.b = last_at_most(a.n, t, [&](int b) { return first(doc_start(cu, b, tokens), b); });
+    const DocLanes x = load_docs<PAGED>(a, w.b);
+    w.q0 = __builtin_amdgcn_readfirstlane(x.q0);
+    w.lq = __builtin_amdgcn_readfirstlane(x.lq);
+    w.k0 = __builtin_amdgcn_readfirstlane(x.k0);
+    w.lk = __builtin_amdgcn_readfirstlane(x.lk);
+    w.tile = t - first(doc_start(cu, w.b, tokens), w.b);
+  }
+  if (BY_KEYS && w.b >= a.n) {
+    w.k0 = doc_start(a.cu_k, a.n, a.tokens_k);
+    w.lk = a.tokens_k - w.k0;
+    w.lq = 0;
+  }
+  w.prefix = a.prefix != nullptr && w.b < a.n ? clamp_i(a.prefix[w.b], 0, w.lk) : 0;
+  return w;
+}
+
+// Sums f(document) over the call's documents, and takes the largest of g
+// (both below 2^53 and 2^24; every wavefront of a call gets the same).
+template <bool PAGED, typename F, typename G>
+__device__ __forceinline__ void over_docs(const HeadsArgs& a, const DocLanes& mine, F f, G g,
+                                          double* sum, float* most) {
+  double s = 0.0;
+  float m = 0.0f;
+  const int lane = static_cast<int>(__lane_id());
+  if (a.n < 64) {
+    if (mine.live && mine.lq > 0) {
+      s = f(mine);
+      m = g(mine);
+    }
+  } else {
+    for (int b = lane; b < a.n; b += 64) {
+      const DocLanes x = load_docs<PAGED>(a, b);
+      if (x.lq <= 0) continue;
+      s += f(x);
+      m = fmaxf(m, g(x));
+    }
+  }
+  *sum = wave_sum64(s);
+  *most = seg_max<64>(m);
 }
 
 // Keys that the query `tok` of a document sees: those before this one.
@@ -162,25 +214,21 @@ __device__ __forceinline__ int keys_seen(const HeadsArgs& a, const DocTile& w, i
 constexpr int kMinChunk = 256;
 
 template <int ROWS>
-__device__ __forceinline__ int split_chunk(const HeadsArgs& a) {
+__device__ __forceinline__ int split_chunk(const HeadsArgs& a, const DocLanes& mine) {
   if (a.splits <= 1) return 0;
-  int64_t sum = 0, longest = 0;
-  for (int b = static_cast<int>(__lane_id()); b < a.n; b += 64) {
-    const int64_t lk = min(static_cast<int64_t>(max(a.cu_k[b], 0)), a.max_keys);
-    const int lq = doc_start(a.cu_q, b + 1, a.tokens_q) - doc_start(a.cu_q, b, a.tokens_q);
-    if (lq <= 0) continue;
-    sum += lk * ((lq * a.group + ROWS - 1) / ROWS);
-    longest = max(longest, lk);
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    sum += __shfl_xor(sum, o);
-    longest = max(longest, __shfl_xor(longest, o));
-  }
-  int64_t chunk = (sum * a.kv_heads + a.target - 1) / a.target;
-  chunk = max(chunk, (longest + a.splits - 1) / a.splits);
+  double sum;
+  float longest;  // rounded up to the fp32 above
+  over_docs<true>(
+      a, mine,
+      [&](const DocLanes& x) {
+        return static_cast<double>(x.lk) * ((x.lq * a.group + ROWS - 1) / ROWS);
+      },
+      [](const DocLanes& x) { return __int2float_ru(x.lk); }, &sum, &longest);
+  const int64_t all = static_cast<int64_t>(sum) * a.kv_heads;
+  const int64_t most = static_cast<int64_t>(longest);
+  int64_t chunk = max((all + a.target - 1) / a.target, (most + a.splits - 1) / a.splits);
   chunk = max((chunk + 63) / 64 * 64, static_cast<int64_t>(kMinChunk));
-  const int n = __builtin_amdgcn_readfirstlane(chunk >= longest ? 0 : static_cast<int>(chunk));
+  const int n = __builtin_amdgcn_readfirstlane(chunk >= most ? 0 : static_cast<int>(chunk));
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.part_head[0] = n;
   return n;
 }

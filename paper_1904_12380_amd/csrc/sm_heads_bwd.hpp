@@ -78,10 +78,8 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
   char SMX_LDS* lds = (char SMX_LDS*)lds_bytes;
   const int hk = blockIdx.x % a.kv_heads;
   const int slot = static_cast<int>(gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads);
-  DocTile w;
-  w.b = find_doc<kTileRows>(a.cu_q, a.n, a.tokens_q, a.group, slot, &w.tile);
-  doc_queries(a, &w);
-  doc_keys<false>(a, &w);
+  const DocTile w =
+      find_tile<kTileRows, false, false>(a, load_docs<false>(a, threadIdx.x % 64), slot);
   const int rows = w.lq * a.group;
   const int row0 = w.tile * kTileRows;
   if (row0 >= rows) return;
@@ -232,42 +230,24 @@ __device__ __forceinline__ KeyTurns key_turns(const HeadsArgs& a, const DocTile&
 // `target` workgroups.  0: not split.
 constexpr int kMinTurns = 32;
 
-__device__ __forceinline__ int split_turns(const HeadsArgs& a) {
+__device__ __forceinline__ int split_turns(const HeadsArgs& a, const DocLanes& mine) {
   if (a.splits <= 1) return 0;
-  int64_t sum = 0, longest = 0;
-  for (int b = static_cast<int>(__lane_id()); b < a.n; b += 64) {
-    const int lq = doc_start(a.cu_q, b + 1, a.tokens_q) - doc_start(a.cu_q, b, a.tokens_q);
-    const int lk = doc_start(a.cu_k, b + 1, a.tokens_k) - doc_start(a.cu_k, b, a.tokens_k);
-    if (lq <= 0 || lk <= 0) continue;
-    const int64_t turns = static_cast<int64_t>((lq + kTurnRows - 1) / kTurnRows) * a.group;
-    sum += turns * ((lk + kTileRows - 1) / kTileRows);
-    longest = max(longest, turns);
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    sum += __shfl_xor(sum, o);
-    longest = max(longest, __shfl_xor(longest, o));
-  }
-  if (a.causal) sum /= 2;
-  int64_t chunk = (sum * a.kv_heads + a.target - 1) / a.target;
-  chunk = max(chunk, (longest + a.splits - 1) / a.splits);
+  auto turns = [&](const DocLanes& x) {
+    return x.lk > 0 ? (x.lq + kTurnRows - 1) / kTurnRows * a.group : 0;
+  };
+  double sum;
+  float longest;
+  over_docs<false>(
+      a, mine,
+      [&](const DocLanes& x) {
+        return static_cast<double>(turns(x)) * ((x.lk + kTileRows - 1) / kTileRows);
+      },
+      [&](const DocLanes& x) { return __int2float_ru(turns(x)); }, &sum, &longest);
+  const int64_t all = static_cast<int64_t>(a.causal ? sum / 2 : sum) * a.kv_heads;
+  const int64_t most = static_cast<int64_t>(longest);
+  int64_t chunk = max((all + a.target - 1) / a.target, (most + a.splits - 1) / a.splits);
   chunk = max(chunk, static_cast<int64_t>(kMinTurns));
-  return __builtin_amdgcn_readfirstlane(chunk >= longest ? 0 : static_cast<int>(chunk));
-}
-
-// The keys' document and tile of a workgroup; keys past the last document are
-// one without queries.
-__device__ __forceinline__ DocTile key_tile(const HeadsArgs& a, int slot) {
-  DocTile w;
-  w.b = find_doc<kTileRows>(a.cu_k, a.n, a.tokens_k, 1, slot, &w.tile);
-  doc_queries(a, &w);
-  doc_keys<false>(a, &w);
-  if (w.b >= a.n) {
-    w.k0 = doc_start(a.cu_k, a.n, a.tokens_k);
-    w.lk = a.tokens_k - w.k0;
-    w.lq = 0;
-  }
-  return w;
+  return __builtin_amdgcn_readfirstlane(chunk >= most ? 0 : static_cast<int>(chunk));
 }
 
 // LDS of k_heads_dkv: V of the key tile, and two stages of kTurnRows rows of Q
@@ -286,11 +266,12 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
   __shared__ __attribute__((aligned(16))) float stats[2][2][kTurnRows];
   char SMX_LDS* lds = (char SMX_LDS*)lds_bytes;
   const int hk = blockIdx.x % a.kv_heads;
-  const DocTile w = key_tile(a, blockIdx.x / a.kv_heads);
+  const DocLanes docs = load_docs<false>(a, threadIdx.x % 64);
+  const DocTile w = find_tile<kTileRows, false, true>(a, docs, blockIdx.x / a.kv_heads);
   const int first = w.tile * kTileRows;
   if (first >= w.lk) return;
   const KeyTurns kt = key_turns(a, w, first);
-  const int chunk = split_turns(a);
+  const int chunk = split_turns(a, docs);
   int turn = 0, turns = kt.turns;
   const bool split = chunk > 0 && kt.turns > chunk;
   if (split) {
@@ -445,11 +426,12 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
 template <typename T>
 __global__ __launch_bounds__(256) void k_heads_sum(HeadsArgs a) {
   const int hk = blockIdx.x % a.kv_heads;
-  const DocTile w = key_tile(a, blockIdx.x / a.kv_heads);
+  const DocLanes docs = load_docs<false>(a, threadIdx.x % 64);
+  const DocTile w = find_tile<kTileRows, false, true>(a, docs, blockIdx.x / a.kv_heads);
   const int first = w.tile * kTileRows;
   if (first >= w.lk) return;
   const KeyTurns kt = key_turns(a, w, first);
-  const int chunk = split_turns(a);
+  const int chunk = split_turns(a, docs);
   if (chunk == 0 || kt.turns <= chunk) return;
   const int count = (kt.turns + chunk - 1) / chunk;
   const int64_t rows = static_cast<int64_t>(a.tokens_k) * a.kv_heads;

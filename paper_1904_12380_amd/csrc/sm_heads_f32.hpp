@@ -104,12 +104,10 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
   const int hk = blockIdx.x % a.kv_heads;
   const int slot = static_cast<int>(gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads);
   const int split = blockIdx.y;
-  DocTile w;
-  w.b = find_doc<kF32Rows>(a.cu_q, a.n, a.tokens_q, a.group, slot, &w.tile);
-  doc_queries(a, &w);
-  doc_keys<PAGED>(a, &w);
+  const DocLanes docs = load_docs<PAGED>(a, threadIdx.x % 64);
+  const int chunk = PAGED ? split_chunk<kF32Rows>(a, docs) : 0;
+  const DocTile w = find_tile<kF32Rows, PAGED, false>(a, docs, slot);
   const int rows = w.lq * a.group;
-  const int chunk = PAGED ? split_chunk<kF32Rows>(a) : 0;
   if (w.tile * kF32Rows >= rows) return;
 
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
@@ -220,10 +218,8 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dq_f32(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) float vs[kF32Step][DP + 4];
   const int hk = blockIdx.x % a.kv_heads;
   const int slot = static_cast<int>(gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads);
-  DocTile w;
-  w.b = find_doc<kF32Rows>(a.cu_q, a.n, a.tokens_q, a.group, slot, &w.tile);
-  doc_queries(a, &w);
-  doc_keys<false>(a, &w);
+  const DocTile w =
+      find_tile<kF32Rows, false, false>(a, load_docs<false>(a, threadIdx.x % 64), slot);
   const int rows = w.lq * a.group;
   if (w.tile * kF32Rows >= rows) return;
 
@@ -304,15 +300,8 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) float os[kF32Step][DP + 4];
   __shared__ float row_lse[kF32Step], row_delta[kF32Step], row_slope[kF32Step];
   const int hk = blockIdx.x % a.kv_heads;
-  DocTile w;
-  w.b = find_doc<kF32Rows>(a.cu_k, a.n, a.tokens_k, 1, blockIdx.x / a.kv_heads, &w.tile);
-  doc_queries(a, &w);
-  doc_keys<false>(a, &w);
-  if (w.b >= a.n) {  // keys past the last document
-    w.k0 = doc_start(a.cu_k, a.n, a.tokens_k);
-    w.lk = a.tokens_k - w.k0;
-    w.lq = 0;
-  }
+  const DocTile w = find_tile<kF32Rows, false, true>(a, load_docs<false>(a, threadIdx.x % 64),
+                                                     blockIdx.x / a.kv_heads);
   if (w.tile * kF32Rows >= w.lk) return;
 
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
@@ -390,16 +379,10 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
 // statistics and then over the columns (up to 128 of them twice, for two splits
 // at a time).
 template <typename T>
-__global__ __launch_bounds__(256) void k_heads_join(HeadsArgs a) {
-  if (a.part_head[0] == 0) return;
-  const int64_t rows = static_cast<int64_t>(a.tokens_q) * a.heads;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 64;
-  const int lane = threadIdx.x % 64;
-  if (row >= rows) return;
-  const SplitStat* stats = a.part_stat + row;
-  const int count = __builtin_amdgcn_readfirstlane(stats->count);
-  SplitStat mine = {-INFINITY, 0.0f, 0, 0};
-  if (lane < count) mine = stats[lane * rows];
+__device__ __forceinline__ void join_row(const HeadsArgs& a, int64_t rows, int64_t row, int lane,
+                                         SplitStat mine) {
+  const int count = __builtin_amdgcn_readfirstlane(mine.count);
+  if (lane >= count) mine = {-INFINITY, 0.0f, 0, 0};
   const float m = seg_max<64>(mine.m);
   const float weight = __builtin_amdgcn_exp2f((mine.m - (m == -INFINITY ? 0.0f : m)) * kLog2eF);
   const float l = seg_sum<64>(mine.l * weight);
@@ -420,6 +403,20 @@ __global__ __launch_bounds__(256) void k_heads_join(HeadsArgs a) {
   if (lane == 0 && a.lse != nullptr)
     a.lse[row] = m == -INFINITY ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2F;
   if (pair == 0 && col < a.d) store4(static_cast<T*>(a.out) + row * a.d + col, acc * inv);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_heads_join(HeadsArgs a) {
+  const int64_t rows = static_cast<int64_t>(a.tokens_q) * a.heads;
+  const int lane = threadIdx.x % 64;
+  const int chunk = a.part_head[0];
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 64; row < rows;
+       row += static_cast<int64_t>(gridDim.x) * 4) {
+    // All launched splits' places, before the row's own number is known.
+    SplitStat mine = a.part_stat[min(lane, a.splits - 1) * rows + row];
+    if (chunk == 0) return;
+    join_row<T>(a, rows, row, lane, mine);
+  }
 }
 
 }  // namespace smx

@@ -485,13 +485,11 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
   const int hk = blockIdx.x % a.kv_heads;
   const int slot = static_cast<int>(gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads);
   const int split = blockIdx.y;
-  DocTile w;
-  w.b = find_doc<kTileRows>(a.cu_q, a.n, a.tokens_q, a.group, slot, &w.tile);
-  doc_queries(a, &w);
-  doc_keys<PAGED>(a, &w);
+  const DocLanes docs = load_docs<PAGED>(a, threadIdx.x % 64);
+  const int chunk = PAGED ? split_chunk<kTileRows>(a, docs) : 0;
+  const DocTile w = find_tile<kTileRows, PAGED, false>(a, docs, slot);
   const int rows = w.lq * a.group;
   const int row0 = w.tile * kTileRows;
-  const int chunk = PAGED ? split_chunk<kTileRows>(a) : 0;
   if (row0 >= rows) return;
   const int tile_rows = min(rows - row0, kTileRows);
   const bool few = tile_rows <= 32;
