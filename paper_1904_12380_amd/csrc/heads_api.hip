@@ -106,13 +106,23 @@ static_assert(kF32Threads == kTileThreads, "one launch shape");
 // workgroups, no more than the longest request has chunks of, at most 64.
 constexpr int64_t kMaxSplits = 64;
 
-int64_t paged_splits(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t requests,
-                     int64_t max_keys, int64_t target) {
+struct PagedSplits {
+  int64_t splits;  // launched
+  int64_t target;  // workgroups that a call aims at
+};
+
+PagedSplits paged_splits(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t requests,
+                         int64_t max_keys, int64_t cus) {
   // Tiles that the requests have at least.
   const int64_t rows = tokens * (heads / kv_heads);
   const int64_t tiles = std::max<int64_t>(1, std::max(rows / kTileRows, std::min(requests, tokens)));
+  // Single tokens are bound by the keys that they read, and their lengths
+  // differ: four times the resident workgroups even them out, and their split
+  // sums are small.  Chunks' are not: what is resident.
+  const int64_t target = (rows <= 32 * requests ? 8 : 2) * cus;
   const int64_t wanted = ceil_div(target, tiles * kv_heads);
-  return std::clamp<int64_t>(std::min(wanted, ceil_div(max_keys, kMinChunk)), 1, kMaxSplits);
+  return {std::clamp<int64_t>(std::min(wanted, ceil_div(max_keys, kMinChunk)), 1, kMaxSplits),
+          target};
 }
 
 int64_t split_bytes(int64_t splits, int64_t tokens, int64_t heads, int64_t d) {
@@ -143,13 +153,12 @@ int64_t part_bytes(int64_t splits, int64_t tokens_k, int64_t kv_heads, int64_t d
 // to join ends at once, but 8192 of them take 12 us to do so.
 constexpr int64_t kJoinGrid = 2048;
 
-// Workgroups that fill the device: two per CU.
-int fill_target(int64_t* target) {
-  int dev = 0, cus = 0;
+int current_cus(int64_t* cus) {
+  int dev = 0, n = 0;
   const hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return fail_hip(e);
-  const int rc = device_cus(dev, &cus);
-  *target = 2 * cus;
+  const int rc = device_cus(dev, &n);
+  *cus = n;
   return rc;
 }
 
@@ -293,9 +302,9 @@ SOFTMAX_API int64_t softmax_paged_attention_workspace(int64_t tokens, int64_t he
   if (tokens < 0 || heads < 0 || d < 8 || d > SOFTMAX_HEADS_MAX_DIM || max_keys < 0 ||
       !sizes_ok(tokens, heads, kv_heads, requests))
     return -1;
-  int64_t target = 0;
-  if (fill_target(&target) != SOFTMAX_OK) return -1;
-  return split_bytes(paged_splits(tokens, heads, kv_heads, requests, max_keys, target), tokens,
+  int64_t cus = 0;
+  if (current_cus(&cus) != SOFTMAX_OK) return -1;
+  return split_bytes(paged_splits(tokens, heads, kv_heads, requests, max_keys, cus).splits, tokens,
                      heads, d);
 }
 
@@ -315,12 +324,12 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
       !aligned16(workspace))
     return SOFTMAX_ERR_INVALID_ARG;
   if (qb == 0) return SOFTMAX_OK;
-  int64_t target = 0;
-  int rc = fill_target(&target);
+  int64_t cus = 0;
+  int rc = current_cus(&cus);
   if (rc != SOFTMAX_OK) return rc;
   const int64_t max_keys = table_width * k->block_size;
-  const int64_t splits =
-      paged_splits(q->tokens, q->heads, k->heads, requests, max_keys, target);
+  const auto [splits, target] =
+      paged_splits(q->tokens, q->heads, k->heads, requests, max_keys, cus);
   const int64_t need = split_bytes(splits, q->tokens, q->heads, q->d);
   if (workspace_bytes < need) return SOFTMAX_ERR_INVALID_ARG;
   const int64_t rows = q->tokens * q->heads;

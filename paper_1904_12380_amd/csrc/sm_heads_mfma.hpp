@@ -93,6 +93,13 @@ __device__ __forceinline__ void staged() {
   __builtin_amdgcn_s_waitcnt(0x0f70);
   asm volatile("" ::: "memory");
 }
+// Waits for all but this wavefront's last N loads.
+template <int N>
+__device__ __forceinline__ void staged_but() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+  asm volatile("" ::: "memory");
+}
 // Waits for this wavefront's reads of LDS (lgkmcnt(0)).
 __device__ __forceinline__ void lds_read() {
   asm volatile("" ::: "memory");
@@ -396,11 +403,13 @@ struct RowState {
 };
 
 // Scores of KT * 32 keys from k0, staged at ktile, their softmax and the
-// product with the values at vtile.
-template <typename T, int DP, int MODE, int KT>
+// product with the values at vtile.  scored() runs when the keys have been
+// read, ready() before the values are.
+template <typename T, int DP, int MODE, int KT, typename F, typename G>
 __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>& w,
                                        const TileReader<DP>& rd, const char SMX_LDS* ktile,
-                                       const char SMX_LDS* vtile, int k0, uint64_t absent) {
+                                       const char SMX_LDS* vtile, int k0, uint64_t absent,
+                                       F scored, G ready) {
   typedef typename Vec8<T>::type V;
   const int half = static_cast<int>(__lane_id()) / 32;
   f32x16 s[KT] = {};
@@ -410,6 +419,7 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
     for (int kt = 0; kt < KT; ++kt)
       s[kt] = mfma32(rd.template rows<T>(ktile, 32 * kt, st), w.q[st], s[kt]);
   }
+  scored();
   if constexpr (MODE != kPlain) {
     const float dist = static_cast<float>(w.pos - k0 - 4 * half);
 #pragma unroll
@@ -454,6 +464,7 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
     }
     w.l += part[0] + part[1];
   }
+  ready();
   V p[2 * KT];
 #pragma unroll
   for (int u = 0; u < 2 * KT; ++u) p[u] = pack8<T>(s[u / 2], 8 * (u % 2));
@@ -562,30 +573,49 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
       if (k0 + kTileKeys < to) stage(k0 + kTileKeys, buf ^ 1);
       if (k0 < st.lim_any)
         attend<T, DP, MODE, 2>(sc, st, rd, lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile,
-                               k0, absent);
+                               k0, absent, [] {}, [] {});
     }
   } else {
     constexpr int kKeys = 2 * kGroup;
     KeySource<DP, WHERE, 2> keys(a, w, hk, to);
     char SMX_LDS* kt = lds + wave * (2 * kKeys * kRowBytes);
     char SMX_LDS* vt = kt + kKeys * kRowBytes;
+    // Each wavefront has one buffer for keys and one for values, and loads
+    // each anew as soon as it has been read: the next keys during the softmax
+    // and the value product, the next values during the next scores.  Loads
+    // past the end read nothing, and keep the count of those in flight.
+    constexpr int kLoads = 2 * KeySource<DP, WHERE, 2>::kPer;
     int k0 = from + wave * kKeys;
-    uint64_t absent = 0;
-    auto stage = [&](int j) {
-      keys.stage(a, keys.k, kt, j);
-      keys.stage(a, keys.v, vt, j);
-      absent = keys.absent();
-      keys.look_up(a, j + 4 * kKeys);
-    };
+    unsigned absent = 0;
     if (k0 < to) {
       keys.look_up(a, k0);
-      stage(k0);
-    }
-    for (; k0 < to; k0 += 4 * kKeys) {
+      keys.stage(a, keys.k, kt, k0);
+      keys.stage(a, keys.v, vt, k0);
+      for (; k0 < to; k0 += 4 * kKeys) {
+        const int next = k0 + 4 * kKeys;
+        absent = keys.absent();
+        if constexpr (WHERE != kSmallBlocks) {
+          staged_but<kLoads>();
+          attend<T, DP, MODE, 1>(
+              sc, st, rd, kt, vt, k0, absent,
+              [&] {
+                lds_read();
+                keys.look_up(a, next);
+                keys.stage(a, keys.k, kt, next);
+              },
+              [&] { staged_but<kLoads>(); });
+          lds_read();
+          keys.stage(a, keys.v, vt, next);
+        } else {  // lanes look up blocks: loads between the stages' own
+          staged();
+          attend<T, DP, MODE, 1>(sc, st, rd, kt, vt, k0, absent, [] {}, [] {});
+          lds_read();
+          keys.look_up(a, next);
+          keys.stage(a, keys.k, kt, next);
+          keys.stage(a, keys.v, vt, next);
+        }
+      }
       staged();
-      attend<T, DP, MODE, 1>(sc, st, rd, kt, vt, k0, absent);
-      lds_read();
-      if (k0 + 4 * kKeys < to) stage(k0 + 4 * kKeys);
     }
   }
 
