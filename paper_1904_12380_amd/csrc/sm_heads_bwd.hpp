@@ -26,6 +26,7 @@ __device__ __forceinline__ f32x16 rows_dot(const TileReader<DP>& rd, const char 
                                            f32x16 s = f32x16{}) {
 #pragma unroll
   for (int st = 0; st < DP / 16; ++st) s = mfma32(rd.template rows<T>(tile, row0, st), b[st], s);
+  interleave<DP / 16, 1>();
   return s;
 }
 
@@ -45,6 +46,7 @@ __device__ __forceinline__ void cols_accumulate(const TileReader<DP>& rd,
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
       acc[t] = mfma32(rd.template cols<T>(tile, row0 + 16 * u, t), hi[u], acc[t]);
+  interleave<2 * DP / 32, 2>();
   if (two_parts) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -389,6 +391,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
 #pragma unroll
       for (int st = 0; st < DP / 16; ++st)
         dp = mfma32(rd.template rows<T>(ot, 0, st), rd.template rows<T>(vt, 0, st), dp);
+      interleave<DP / 16, 2, 2>();
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * c);
       if (lim_all < key0 + 32) {

@@ -345,6 +345,21 @@ __device__ __forceinline__ typename Vec8<T>::type pack8_rest(const f32x16& x, in
   return r;
 }
 
+// Orders a run of `reads` reads of LDS (`per` for each operand) and `ops`
+// matrix ops that take them: AHEAD operands are read ahead, so that the reads'
+// latency passes during earlier matrix ops.  (The compiler by itself waits for
+// each read right before its use.)
+template <int OPS, int PER, int AHEAD = 4>
+__device__ __forceinline__ void interleave() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * PER, 0);
+#pragma unroll
+  for (int i = 0; i < OPS - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
 // How scores are formed (a template argument): scaled, with a bias, or with a
 // cap and a bias (of slope 0 where there is none).
 constexpr int kPlain = 0, kBias = 1, kCap = 2;
@@ -419,6 +434,7 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
     for (int kt = 0; kt < KT; ++kt)
       s[kt] = mfma32(rd.template rows<T>(ktile, 32 * kt, st), w.q[st], s[kt]);
   }
+  interleave<KT * DP / 16, 1>();
   scored();
   if constexpr (MODE != kPlain) {
     const float dist = static_cast<float>(w.pos - k0 - 4 * half);
@@ -473,6 +489,7 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
       w.acc[t] = mfma32(rd.template cols<T>(vtile, 16 * u, t), p[u], w.acc[t]);
+  interleave<2 * KT * DP / 32, 2>();
   // A document's first keys: what the weights' rounding left, where rows see
   // few keys to average it.
   if (k0 == 0 && w.lim_all <= kTwoPartKeys) {
@@ -591,6 +608,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
       keys.look_up(a, k0);
       keys.stage(a, keys.k, kt, k0);
       keys.stage(a, keys.v, vt, k0);
+      staged();  // q too
       for (; k0 < to; k0 += 4 * kKeys) {
         const int next = k0 + 4 * kKeys;
         absent = keys.absent();
