@@ -333,8 +333,9 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
             a.delta)[static_cast<int64_t>(head) * a.tokens_q + w.q0 + t0 + lane];
     }
     char SMX_LDS* qt = stages + buf * 2 * kTile + r0 * DP * 2;
-    Stager<DP>(a.q, 0, w.q0, head).template packed<N>(qt, t0 + r0, w.lq, d2);
-    Stager<DP>(a.dout, 0, w.q0, head).template packed<N>(qt + kTile, t0 + r0, w.lq, d2);
+    Stager<DP>(a.q, 0, w.q0, head).template packed<N>(qt, t0 + r0, w.lq, d2, r0);
+    Stager<DP>(a.dout, 0, w.q0, head).template packed<N>(qt + kTile, t0 + r0, w.lq, d2,
+                                                                     r0);
   };
   auto write_stats = [&](int buf) {
     if (tid < kTurnRows) {

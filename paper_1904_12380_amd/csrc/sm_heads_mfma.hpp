@@ -11,9 +11,9 @@
 // lanes read 4 rows of 16 columns, and each gets one column).
 //
 // LDS holds rows of the padded head width in 16-byte chunks, chunk c of row r
-// at place c ^ swz(r): reads of 8 rows at one chunk (K) and of 4 rows at 4
-// consecutive chunks (V, transposed) then touch all banks.  Tiles go from
-// memory to LDS without registers.
+// at place c ^ swz(r): reads of 16 rows at one chunk (K) and of 4 rows at 4
+// consecutive chunks (V, transposed) then touch each of the 64 banks once.
+// Tiles go from memory to LDS without registers.
 //
 // A tile of up to 32 rows (single tokens of grouped heads, ends of chunks) is
 // taken by all four wavefronts over different keys; a larger one by one
@@ -50,9 +50,17 @@ constexpr int kTileRows = 128;
 constexpr int kTileKeys = 64;
 constexpr int kTileThreads = 256;
 
-// The swizzle of row r's chunks: its low three bits, the lowest on top, so
-// that neighbouring rows lie 64 bytes apart.  swz(a ^ b) = swz(a) ^ swz(b).
-__host__ __device__ constexpr int swz(int r) { return (r & 1) << 2 | (r >> 1 & 3); }
+// The swizzle of row r's chunks.  Rows of 256 bytes or more start at the same
+// bank: 16 rows at one chunk need 16 places, and 4 rows at 4 consecutive chunks
+// 4 places that lie 64 bytes apart.  Of rows of 128 bytes two share the banks.
+// swz(a ^ b) = swz(a) ^ swz(b).
+template <int DP>
+__host__ __device__ constexpr int swz(int r) {
+  return DP >= 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 3);
+}
+// Bytes of a row over which places are permuted.
+template <int DP>
+constexpr int kSwzSpan = DP >= 128 ? 256 : 128;
 
 // LDS of one workgroup: two stages of kTileKeys rows of K and V.
 template <int DP>
@@ -131,21 +139,23 @@ struct Stager {
     base = static_cast<const char*>(v.data) + first * ts2 + hk * v.hs * 2;
     const int lane = static_cast<int>(__lane_id());
     lane_row = lane / kChunks;
-    lane_chunk = (lane % kChunks) ^ swz(lane_row);
+    lane_chunk = (lane % kChunks) ^ swz<DP>(lane_row);
   }
 
   // Column byte of the lane's chunk for the instruction whose first row has
-  // the low bits `low` (a constant).
-  __device__ __forceinline__ int column(int low) const { return 16 * (lane_chunk ^ swz(low)); }
+  // the low bits `low`.
+  __device__ __forceinline__ int column(int low) const {
+    return 16 * (lane_chunk ^ swz<DP>(low));
+  }
 
-  // N instructions' rows from `at` on into lds (uniform), of which `bytes` are
-  // there: zeros past them and past column d.  Each instruction has a buffer
+  // N instructions' rows from `at` on into lds (uniform, a row with the low
+  // bits `low`), of which `bytes` are there: zeros past them and past column d.  Each instruction has a buffer
   // of its own, from its first row on, so that all share the lanes' offsets:
   // as offsets from one buffer they would take a register each, held across
   // the loop.
   template <int N>
-  __device__ __forceinline__ void rows(const char* at, int bytes, char SMX_LDS* lds,
-                                       int d2) const {
+  __device__ __forceinline__ void rows(const char* at, int bytes, char SMX_LDS* lds, int d2,
+                                       int low = 0) const {
     const int step = static_cast<int>(ts2);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -155,7 +165,7 @@ struct Stager {
       const s32x4 rsrc = {__builtin_amdgcn_readfirstlane(static_cast<int>(p)),
                           __builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32 & 0xffff)),
                           __builtin_amdgcn_readfirstlane(max(bytes - skip, 0)), 0x00027000};
-      const int col = column(n * kRows);
+      const int col = column(n * kRows) ^ 16 * swz<DP>(low);
       const unsigned off = col < d2 ? lane_row * step + col : kFar;
       load_lds(rsrc, off, lds_offset(lds) + n * 1024);
     }
@@ -163,10 +173,12 @@ struct Stager {
 
   // Rows j, j + 1, .. of packed keys that end at `end`.
   template <int N>
-  __device__ __forceinline__ void packed(char SMX_LDS* lds, int j, int end, int d2) const {
+  __device__ __forceinline__ void packed(char SMX_LDS* lds, int j, int end, int d2,
+                                         int low = 0) const {
     const int64_t left = end - 1 - j;
     const int64_t bytes = left < 0 ? 0 : left * ts2 + d2;
-    rows<N>(base + j * ts2, static_cast<int>(bytes < 0x7fffffff ? bytes : 0x7fffffff), lds, d2);
+    rows<N>(base + j * ts2, static_cast<int>(bytes < 0x7fffffff ? bytes : 0x7fffffff), lds, d2,
+            low);
   }
 };
 
@@ -280,20 +292,20 @@ __device__ __forceinline__ int opaque(int x) {
   return x;
 }
 
-// Reads of a staged tile.  `rows`: chunk 2 s + l / 32 of row l % 32, at LDS
-// bytes rows.at ^ (32 s); `cols`: transposed reads, of the columns 32 t.
+// Reads of a staged tile: rows as they lie, and columns, transposed.
 template <int DP>
 struct TileReader {
+  static constexpr int kSpan = kSwzSpan<DP>;
   int row_at;   // byte of row l % 32, chunk l / 32
   int col_at;   // byte of the transposed read at rows 4 (l / 32) .., column 0
 
   __device__ __forceinline__ TileReader() {
     const int lane = static_cast<int>(__lane_id()), half = lane / 32;
     const int r = lane % 32;
-    row_at = r * DP * 2 + 16 * (half ^ swz(r));
+    row_at = r * DP * 2 + 16 * (half ^ swz<DP>(r));
     const int i = lane % 16, cr = 4 * half + i / 4;
     const int chunk = 2 * (lane / 16 % 2) + (i % 4) / 2;
-    col_at = cr * DP * 2 + 16 * (chunk ^ swz(cr)) + 8 * (i % 2);
+    col_at = cr * DP * 2 + 16 * (chunk ^ swz<DP>(cr)) + 8 * (i % 2);
   }
 
   // The same reader with addresses built anew.
@@ -304,13 +316,13 @@ struct TileReader {
     return r;
   }
 
-  // A operand: rows row0 + l % 32 (row0 a multiple of 8), columns of step s.
+  // A operand: rows row0 + l % 32 (row0 a multiple of 32), columns of step s.
   template <typename T>
   __device__ __forceinline__ typename Vec8<T>::type rows(const char SMX_LDS* tile, int row0,
                                                          int s) const {
     typedef typename Vec8<T>::type V;
-    return *reinterpret_cast<const V SMX_LDS*>(tile + row0 * DP * 2 + (row_at ^ (s % 4 * 32)) +
-                                               s / 4 * 128);
+    return *reinterpret_cast<const V SMX_LDS*>(tile + row0 * DP * 2 + (row_at ^ 32 * s % kSpan) +
+                                               32 * s / kSpan * kSpan);
   }
 
   // A operand: columns 32 t + l % 32 of the rows row0 + 4 (l / 32) + j % 4 + 8
@@ -318,10 +330,11 @@ struct TileReader {
   template <typename T>
   __device__ __forceinline__ typename Vec8<T>::type cols(const char SMX_LDS* tile, int row0,
                                                          int t) const {
-    const char SMX_LDS* p = tile + row0 * DP * 2 + (col_at ^ (t % 2 * 64)) + t / 2 * 128;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 SMX_LDS*)(p));
+    const char SMX_LDS* p = tile + row0 * DP * 2 + 64 * t / kSpan * kSpan;
+    const int lo_at = col_at ^ 64 * t % kSpan, hi_at = lo_at ^ 16 * swz<DP>(8);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 SMX_LDS*)(p + lo_at));
     const s16x4 hi =
-        __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 SMX_LDS*)(p + 8 * DP * 2));
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 SMX_LDS*)(p + 8 * DP * 2 + hi_at));
     const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     return __builtin_bit_cast(typename Vec8<T>::type, both);
   }
