@@ -58,19 +58,19 @@ __device__ __forceinline__ void cols_accumulate(const TileReader<DP>& rd,
   }
 }
 
-template <typename T, int DP>
-__device__ __forceinline__ void store_columns(T* p, int d, int half, const f32x16 (&acc)[DP / 32],
-                                              float f) {
-  typedef T t4 __attribute__((ext_vector_type(4)));
+// The lane's row, of fp32 sums.
+template <int DP>
+__device__ __forceinline__ void store_sums(float* p, int d, int half,
+                                           const f32x16 (&acc)[DP / 32]) {
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int col = 32 * t + 8 * i + 4 * half;
-      t4 x;
+      f32x4 x;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = static_cast<T>(acc[t][4 * i + j] * f);
-      if (col < d) *reinterpret_cast<t4*>(p + col) = x;
+      for (int j = 0; j < 4; ++j) x[j] = acc[t][4 * i + j];
+      if (col < d) *reinterpret_cast<f32x4*>(p + col) = x;
     }
 }
 
@@ -204,11 +204,12 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
       cols_accumulate<T, DP>(rd, kt, 32 * h, dp, two_parts, acc);
     }
   }
-  if (!valid) return;
-  if (half == 0)
+  if (valid && half == 0)
     reinterpret_cast<float2*>(a.delta)[static_cast<int64_t>(head) * a.tokens_q + token] =
         make_float2(-lse2 / c, -delta);
-  store_columns<T, DP>(static_cast<T*>(a.out) + out * a.d, a.d, half, acc, a.scale);
+  __syncthreads();
+  store_rows<T, DP>(lds + wave * 32 * DP * 2, acc, a.scale, static_cast<T*>(a.out),
+                    valid ? static_cast<int>(out) : -1, a.d);
 }
 
 // The turns of a key tile: 32 tokens of one head each, from the first token
@@ -413,17 +414,21 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
     }
     write_stats(buf ^ 1);
   }
-  if (!valid) return;
   const int64_t row = token * a.kv_heads + hk;
   if (split) {
+    if (!valid) return;
     const int64_t rows = static_cast<int64_t>(a.tokens_k) * a.kv_heads;
     float* p = a.part_o + ((2 * static_cast<int64_t>(blockIdx.y)) * rows + row) * a.d;
-    store_columns<float, DP>(p, a.d, half, dk, 1.0f);
-    store_columns<float, DP>(p + rows * a.d, a.d, half, dv, 1.0f);
+    store_sums<DP>(p, a.d, half, dk);
+    store_sums<DP>(p + rows * a.d, a.d, half, dv);
     return;
   }
-  store_columns<T, DP>(static_cast<T*>(a.dk) + row * a.d, a.d, half, dk, a.scale);
-  store_columns<T, DP>(static_cast<T*>(a.dv) + row * a.d, a.d, half, dv, 1.0f);
+  // The wavefront's own V has landed (also without a turn) and been read: its
+  // place turns the rows.
+  staged();
+  const int index = valid ? static_cast<int>(row) : -1;
+  store_rows<T, DP>(lds + 32 * wave * DP * 2, dk, a.scale, static_cast<T*>(a.dk), index, a.d);
+  store_rows<T, DP>(lds + 32 * wave * DP * 2, dv, 1.0f, static_cast<T*>(a.dv), index, a.d);
 }
 
 // Sums the splits of a key tile's gradients.

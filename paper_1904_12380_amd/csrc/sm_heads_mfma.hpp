@@ -271,6 +271,25 @@ struct KeySource {
   }
 };
 
+// A wavefront's 32 rows from memory to lds, lane r's row at base + its offset in
+// bytes (negative: a row of zeros), which whole chunks at a time: a lane's own
+// loads of its row would take 32 bytes of each of 32 rows at once.
+template <int DP>
+__device__ __forceinline__ void stage_rows(const char* base, int64_t offset, char SMX_LDS* lds,
+                                           int d2) {
+  constexpr int kChunks = DP / 8, kRows = 64 / kChunks;
+  const int lane = static_cast<int>(__lane_id()), row0 = lane / kChunks;
+#pragma unroll
+  for (int n = 0; n < 32 / kRows; ++n) {
+    const int row = n * kRows + row0;
+    const int col = 16 * (lane % kChunks ^ swz<DP>(row));
+    const int64_t off = __shfl(offset, row);
+    const char* p = base + off + col;
+    if (off < 0 || col >= d2) p = reinterpret_cast<const char*>(&g_heads_zero);
+    load_lds(p, lds_offset(lds) + n * 1024);
+  }
+}
+
 // The lane's row of Q (or of dO) as the B operand of DP / 16 steps: columns 16 s + 8
 // (l / 32) + j, 0 past d and for rows that are not there.
 template <typename T, int DP>
@@ -516,6 +535,38 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
   }
 }
 
+// A wavefront's 32 rows, a lane's at l % 32 in acc (D of transposed products),
+// times f: rounded, turned in LDS (32 * DP * 2 bytes of the wavefront's own) and
+// written as whole rows, row r at base + index * d for lane r's index (-1: not
+// written).  Straight from the lanes every store would write 16 bytes of each of
+// 32 rows: 2.4 us of a workgroup's 10 at one or two key tiles.
+template <typename T, int DP>
+__device__ __forceinline__ void store_rows(char SMX_LDS* lds, const f32x16 (&acc)[DP / 32],
+                                           float f, T* base, int index, int d) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  constexpr int kChunks = DP / 8, kRows = 64 / kChunks;
+  const int lane = static_cast<int>(__lane_id()), half = lane / 32, r = lane % 32;
+#pragma unroll
+  for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      t4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = static_cast<T>(acc[t][4 * i + j] * f);
+      *(t4 SMX_LDS*)(lds + r * DP * 2 + 16 * ((4 * t + i) ^ swz<DP>(r)) + 8 * half) = x;
+    }
+  const int row0 = lane / kChunks, chunk = lane % kChunks;
+#pragma unroll
+  for (int n = 0; n < 32 / kRows; ++n) {
+    const int row = n * kRows + row0;
+    const s32x4 x =
+        *(const s32x4 SMX_LDS*)(lds + row * DP * 2 + 16 * (chunk ^ swz<DP>(row)));
+    const int at = __shfl(index, row);
+    if (at >= 0 && 8 * chunk < d)
+      *reinterpret_cast<s32x4*>(base + static_cast<int64_t>(at) * d + 8 * chunk) = x;
+  }
+}
+
 template <typename T, int DP, int WHERE, int MODE>
 __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) char lds_bytes[tile_lds_bytes<DP>()];
@@ -560,17 +611,27 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
   st.c = sc.unit();
   st.m = kUnseen;
   st.l = 0.0f;
-  load_operand<T, DP>(st.q, static_cast<const T*>(a.q.data) + token * a.q.ts + head * a.q.hs,
-                      valid, half, a.d);
-  if (MODE == kPlain && a.scale < 0.0f) {  // the sign into q
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) st.q[i] = -st.q[i];
-  }
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t) st.acc[t] = f32x16{};
 
   const TileReader<DP> rd;
   constexpr int kRowBytes = DP * 2;
+  // The wavefront's rows of Q, by way of its quarter of the second stage.
+  auto load_q = [&] {
+    char SMX_LDS* at = lds + tile_lds_bytes<DP>() / 2 + wave * 32 * kRowBytes;
+    const int64_t offset = 2 * (token * a.q.ts + head * a.q.hs);
+    stage_rows<DP>(static_cast<const char*>(a.q.data), valid ? offset : -1, at, 2 * a.d);
+    return at;
+  };
+  auto read_q = [&](const char SMX_LDS* at) {
+    staged();
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+      st.q[i] = rd.template rows<T>(at, 0, i);
+      if (MODE == kPlain && a.scale < 0.0f) st.q[i] = -st.q[i];  // the sign into q
+    }
+    lds_read();
+  };
 
   if (!few) {
     constexpr int kTile = kTileKeys * kRowBytes;
@@ -587,8 +648,10 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
       }
     };
     if (from < to) {
+      const char SMX_LDS* q = load_q();
       keys.look_up(a, from + r0);
       stage(from, 0);
+      read_q(q);
     }
     int buf = 0;
     for (int k0 = from; k0 < to; k0 += kTileKeys, buf ^= 1) {
@@ -602,7 +665,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
       }
       if (k0 + kTileKeys < to) stage(k0 + kTileKeys, buf ^ 1);
       if (k0 < st.lim_any)
-        attend<T, DP, MODE, 2>(sc, st, rd, lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile,
+        attend<T, DP, MODE, 2>(sc, st, PAGED ? rd.fresh() : rd, lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile,
                                k0, absent, [] {}, [] {});
     }
   } else {
@@ -619,16 +682,22 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
     unsigned absent = 0;
     if (k0 < to) {
       keys.look_up(a, k0);
+      load_operand<T, DP>(st.q, static_cast<const T*>(a.q.data) + token * a.q.ts + head * a.q.hs,
+                          valid, half, a.d);
       keys.stage(a, keys.k, kt, k0);
       keys.stage(a, keys.v, vt, k0);
       staged();  // q too
+      if (MODE == kPlain && a.scale < 0.0f) {
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) st.q[i] = -st.q[i];
+      }
       for (; k0 < to; k0 += 4 * kKeys) {
         const int next = k0 + 4 * kKeys;
         absent = keys.absent();
         if constexpr (WHERE != kSmallBlocks) {
           staged_but<kLoads>();
           attend<T, DP, MODE, 1>(
-              sc, st, rd, kt, vt, k0, absent,
+              sc, st, rd.fresh(), kt, vt, k0, absent,
               [&] {
                 lds_read();
                 keys.look_up(a, next);
@@ -639,7 +708,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
           keys.stage(a, keys.v, vt, next);
         } else {  // lanes look up blocks: loads between the stages' own
           staged();
-          attend<T, DP, MODE, 1>(sc, st, rd, kt, vt, k0, absent, [] {}, [] {});
+          attend<T, DP, MODE, 1>(sc, st, rd.fresh(), kt, vt, k0, absent, [] {}, [] {});
           lds_read();
           keys.look_up(a, next);
           keys.stage(a, keys.k, kt, next);
@@ -700,11 +769,11 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
         for (int j = 0; j < 4; ++j) st.acc[t][4 * i + j] = x[j];
       }
   }
-  if (!valid) return;
   const bool some = m > kUnseen;
   const int64_t out = token * a.heads + head;
-  const bool writes_stats = half == 0 && (!few || wave == 0);
+  const bool writes_stats = valid && half == 0 && (!few || wave == 0);
   if (chunk > 0) {
+    if (!valid) return;
     const int64_t at = split * static_cast<int64_t>(a.tokens_q) * a.heads + out;
     if (writes_stats)
       a.part_stat[at] = {some ? m * st.c * kLn2F : -INFINITY, l, split_count(seen, chunk), 0};
@@ -725,13 +794,20 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
   const float inv = some ? 1.0f / l : 0.0f;
   if (writes_stats && a.lse != nullptr)
     a.lse[out] = some ? (m * st.c + __builtin_amdgcn_logf(l)) * kLn2F : -INFINITY;
+  if (!few) {
+    __syncthreads();  // the last tile has been read: its place turns the rows
+    store_rows<T, DP>(lds + wave * 32 * kRowBytes, st.acc, inv, static_cast<T*>(a.out),
+                      valid ? static_cast<int>(out) : -1, a.d);
+    return;
+  }
+  if (!valid) return;
   T* o = static_cast<T*>(a.out) + out * a.d;
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int col = 32 * t + 8 * i + 4 * half;
-      if (col < a.d && (!few || i == wave)) {
+      if (col < a.d && i == wave) {
         typedef T t4 __attribute__((ext_vector_type(4)));
         t4 x;
 #pragma unroll
