@@ -212,18 +212,22 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
                     valid ? static_cast<int>(out) : -1, a.d);
 }
 
-// The turns of a key tile: 32 tokens of one head each, from the first token
-// that sees the tile's first key, head by head.
+// The turns of a key tile: 32 tokens of one head each, head by head, each from
+// the document's last tokens down to the first that sees the tile's first
+// key.  Workgroups of different key tiles then read the same rows at the same
+// time, and these come from the L2: in ascending order each would start at
+// rows of its own.
 constexpr int kTurnRows = 32;
 
 struct KeyTurns {
-  int tok0, tiles, turns;
+  int last, tiles, turns;  // last token tile; token tiles of a head; turns
 };
 
 __device__ __forceinline__ KeyTurns key_turns(const HeadsArgs& a, const DocTile& w, int first) {
   KeyTurns k;
-  k.tok0 = a.causal && first >= w.prefix ? max(first - (w.lk - w.lq), 0) : 0;
-  k.tiles = k.tok0 < w.lq ? (w.lq - k.tok0 + kTurnRows - 1) / kTurnRows : 0;
+  const int tok0 = a.causal && first >= w.prefix ? max(first - (w.lk - w.lq), 0) : 0;
+  k.last = (w.lq + kTurnRows - 1) / kTurnRows - 1;
+  k.tiles = tok0 < w.lq ? k.last + 1 - tok0 / kTurnRows : 0;
   k.turns = k.tiles * a.group;
   return k;
 }
@@ -253,6 +257,19 @@ __device__ __forceinline__ int split_turns(const HeadsArgs& a, const DocLanes& m
   return __builtin_amdgcn_readfirstlane(chunk >= most ? 0 : static_cast<int>(chunk));
 }
 
+// Splits of a tile's turns: enough for the chunk, and so many that they begin
+// with heads (a divisor of the group, or a multiple of it), which keeps the
+// tiles' workgroups at the same rows.
+__device__ __forceinline__ int turn_splits(const HeadsArgs& a, int turns, int chunk) {
+  if (chunk == 0 || turns <= chunk) return 1;
+  int count = (turns + chunk - 1) / chunk;
+  if (count >= a.group)
+    count = (count + a.group - 1) / a.group * a.group;
+  else
+    while (a.group % count != 0) ++count;
+  return min(count, a.splits);
+}
+
 // LDS of k_heads_dkv: V of the key tile, and two stages of kTurnRows rows of Q
 // and dO.
 template <int DP>
@@ -275,15 +292,12 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
   if (first >= w.lk) return;
   const KeyTurns kt = key_turns(a, w, first);
   const int chunk = split_turns(a, docs);
-  int turn = 0, turns = kt.turns;
-  const bool split = chunk > 0 && kt.turns > chunk;
-  if (split) {
-    turn = static_cast<int>(blockIdx.y) * chunk;
-    turns = min(turns, turn + chunk);
-    if (turn >= turns) return;
-  } else if (blockIdx.y > 0) {
-    return;
-  }
+  const int splits = turn_splits(a, kt.turns, chunk);
+  const bool split = splits > 1;
+  if (static_cast<int>(blockIdx.y) >= splits) return;
+  const int per = (kt.turns + splits - 1) / splits;
+  int turn = static_cast<int>(blockIdx.y) * per;
+  const int turns = min(kt.turns, turn + per);
 
   const int tid = threadIdx.x, lane = tid % 64, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -315,16 +329,17 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
 
   float2 stat = {-INFINITY, 0.0f};
   // The head and the first token of the turn to stage next, and of this one.
-  int next_head = hk * a.group, next_t0 = kt.tok0;
+  const int top = kt.last * kTurnRows, bottom = (kt.last + 1 - kt.tiles) * kTurnRows;
+  int next_head = hk * a.group, next_t0 = top;
   if (turn < turns) {
     next_head += turn / kt.tiles;
-    next_t0 += turn % kt.tiles * kTurnRows;
+    next_t0 -= turn % kt.tiles * kTurnRows;
   }
   auto stage = [&](int buf) {
     const int head = next_head, t0 = next_t0;
-    next_t0 += kTurnRows;
-    if (next_t0 >= w.lq) {
-      next_t0 = kt.tok0;
+    next_t0 -= kTurnRows;
+    if (next_t0 < bottom) {
+      next_t0 = top;
       ++next_head;
     }
     if (wave == 0) {  // before the stage's loads: waiting for it waits for no other
@@ -440,9 +455,8 @@ __global__ __launch_bounds__(256) void k_heads_sum(HeadsArgs a) {
   const int first = w.tile * kTileRows;
   if (first >= w.lk) return;
   const KeyTurns kt = key_turns(a, w, first);
-  const int chunk = split_turns(a, docs);
-  if (chunk == 0 || kt.turns <= chunk) return;
-  const int count = (kt.turns + chunk - 1) / chunk;
+  const int count = turn_splits(a, kt.turns, split_turns(a, docs));
+  if (count == 1) return;
   const int64_t rows = static_cast<int64_t>(a.tokens_k) * a.kv_heads;
   const int quads = a.d / 4, keys = min(w.lk - first, kTileRows);
   for (int i = threadIdx.x; i < keys * quads; i += 256) {
