@@ -52,37 +52,40 @@ hipError_t launch2(const void* fn, int64_t x, int64_t y, int block, HeadsArgs* a
                          dim3(block), args, 0, s);
 }
 
-template <bool PAGED>
-const void* fwd_f32(const HeadsArgs& a) {
-  return a.d <= 64    ? SMX_FN(k_heads_fwd_f32<64, PAGED>)
-         : a.d <= 128 ? SMX_FN(k_heads_fwd_f32<128, PAGED>)
-                      : SMX_FN(k_heads_fwd_f32<256, PAGED>);
-}
+// The fp32 instance of a head width: its columns padded to a multiple of 32
+// up to 128 (a matrix op takes 4), then to 192 or 256.
+#define SMX_BY_WIDTH_F32(d, ...)                                                   \
+  ((d) <= 32    ? SMX_FN(__VA_ARGS__(32))                                          \
+   : (d) <= 64  ? SMX_FN(__VA_ARGS__(64))                                          \
+   : (d) <= 96  ? SMX_FN(__VA_ARGS__(96))                                          \
+   : (d) <= 128 ? SMX_FN(__VA_ARGS__(128))                                         \
+   : (d) <= 192 ? SMX_FN(__VA_ARGS__(192)) : SMX_FN(__VA_ARGS__(256)))
+#define SMX_FWD_PACKED(DP) k_heads_fwd_f32<DP, false>
+#define SMX_FWD_PAGED(DP) k_heads_fwd_f32<DP, true>
+#define SMX_DQ(DP) k_heads_dq_f32<DP>
+#define SMX_DKV(DP) k_heads_dkv_f32<DP>
 
 const void* packed_fn(int dtype, const HeadsArgs& a) {
-  return dtype == SOFTMAX_F32   ? fwd_f32<false>(a)
+  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, SMX_FWD_PACKED)
          : dtype == SOFTMAX_F16 ? heads_fwd_f16(a, kPacked)
                                 : heads_fwd_bf16(a, kPacked);
 }
 
 const void* paged_fn(int dtype, const HeadsArgs& a) {
   const int where = 1 << a.log_block >= kGroup ? kBlocks : kSmallBlocks;
-  return dtype == SOFTMAX_F32   ? fwd_f32<true>(a)
+  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, SMX_FWD_PAGED)
          : dtype == SOFTMAX_F16 ? heads_fwd_f16(a, where)
                                 : heads_fwd_bf16(a, where);
 }
 
-#define SMX_BY_WIDTH_F32(d, K) \
-  ((d) <= 64 ? SMX_FN(K<64>) : (d) <= 128 ? SMX_FN(K<128>) : SMX_FN(K<256>))
-
 const void* dq_fn(int dtype, const HeadsArgs& a) {
-  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, k_heads_dq_f32)
+  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, SMX_DQ)
          : dtype == SOFTMAX_F16 ? heads_dq_f16(a)
                                 : heads_dq_bf16(a);
 }
 
 const void* dkv_fn(int dtype, const HeadsArgs& a) {
-  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, k_heads_dkv_f32)
+  return dtype == SOFTMAX_F32   ? SMX_BY_WIDTH_F32(a.d, SMX_DKV)
          : dtype == SOFTMAX_F16 ? heads_dkv_f16(a)
                                 : heads_dkv_bf16(a);
 }

@@ -402,6 +402,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
           cap[i] = x;
         }
       } else {
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
         s = rows_dot<T, DP>(rd, qt, 0, k, rows_stat(stats[buf][0]));
       }
       f32x16 dp = rows_stat(stats[buf][1]);

@@ -96,6 +96,33 @@ __device__ __forceinline__ void tile_accumulate(f32x4 (&acc)[DP / 16],
   }
 }
 
+// A thread's share of the next tile's two tensors, loaded into registers
+// during the products of this one: f(row, column, x, y) loads four columns
+// of one row of each.
+template <int DP>
+struct NextTile {
+  static constexpr int kShare = kF32Step * DP / 4 / kF32Threads;
+  f32x4 x[kShare], y[kShare];
+
+  template <typename F>
+  __device__ __forceinline__ void load(F f) {
+#pragma unroll
+    for (int n = 0; n < kShare; ++n) {
+      const int i = static_cast<int>(threadIdx.x) + n * kF32Threads;
+      x[n] = y[n] = f32x4{0, 0, 0, 0};
+      f(i / (DP / 4), 4 * (i % (DP / 4)), x[n], y[n]);
+    }
+  }
+  __device__ __forceinline__ void store(float (*xs)[DP + 4], float (*ys)[DP + 4]) const {
+#pragma unroll
+    for (int n = 0; n < kShare; ++n) {
+      const int i = static_cast<int>(threadIdx.x) + n * kF32Threads;
+      *reinterpret_cast<f32x4*>(&xs[i / (DP / 4)][4 * (i % (DP / 4))]) = x[n];
+      *reinterpret_cast<f32x4*>(&ys[i / (DP / 4)][4 * (i % (DP / 4))]) = y[n];
+    }
+  }
+};
+
 template <int DP, bool PAGED>
 __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) float ks[kF32Step][DP + 4];
@@ -131,32 +158,32 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
   f32x4 acc[DP / 16] = {};
   float m = -INFINITY, l = 0.0f;
 
+  NextTile<DP> next;
+  auto load = [&](int k0) {
+    next.load([&](int r, int col, f32x4& x, f32x4& y) {
+      const int j = k0 + r;
+      if (j >= to || col >= a.d) return;
+      int64_t kr, vr;
+      if constexpr (PAGED) {
+        kr = paged_row(a, w.b, j, a.k_bs, a.k.ts);
+        vr = paged_row(a, w.b, j, a.v_bs, a.v.ts);
+        if (kr < 0) return;
+      } else {
+        kr = static_cast<int64_t>(w.k0 + j) * a.k.ts;
+        vr = static_cast<int64_t>(w.k0 + j) * a.v.ts;
+      }
+      x = load4(static_cast<const float*>(a.k.data) + kr + hk * a.k.hs + col);
+      y = load4(static_cast<const float*>(a.v.data) + vr + hk * a.v.hs + col);
+    });
+  };
+  load(from);
   for (int k0 = from; k0 < to; k0 += kF32Step) {
     __syncthreads();
-    for (int i = tid; i < kF32Step * (DP / 4); i += kF32Threads) {
-      const int r = i / (DP / 4), col = 4 * (i % (DP / 4)), j = k0 + r;
-      f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-      bool have = j < to;
-      if (have) {
-        int64_t kr, vr;
-        if constexpr (PAGED) {
-          kr = paged_row(a, w.b, j, a.k_bs, a.k.ts);
-          vr = paged_row(a, w.b, j, a.v_bs, a.v.ts);
-          have = kr >= 0;
-        } else {
-          kr = static_cast<int64_t>(w.k0 + j) * a.k.ts;
-          vr = static_cast<int64_t>(w.k0 + j) * a.v.ts;
-        }
-        if (have && col < a.d) {
-          x = load4(static_cast<const float*>(a.k.data) + kr + hk * a.k.hs + col);
-          y = load4(static_cast<const float*>(a.v.data) + vr + hk * a.v.hs + col);
-        }
-      }
-      *reinterpret_cast<f32x4*>(&ks[r][col]) = x;
-      *reinterpret_cast<f32x4*>(&vs[r][col]) = y;
-      if (col == 0) held[r] = have;
-    }
+    next.store(ks, vs);
+    if (PAGED && tid < kF32Step)
+      held[tid] = k0 + tid < to && paged_row(a, w.b, k0 + tid, a.k_bs, a.k.ts) >= 0;
     __syncthreads();
+    load(k0 + kF32Step);
     f32x4 s[2];
     float top = -INFINITY;
 #pragma unroll
@@ -167,7 +194,7 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
         const int r = 16 * kt + 4 * g + i, j = k0 + r;
         float dcap;
         const float x = score_f32(a, s[kt][i], slope, pos - j, &dcap);
-        s[kt][i] = j < lim && held[r] ? x : -INFINITY;
+        s[kt][i] = j < lim && (!PAGED || held[r]) ? x : -INFINITY;
         top = fmaxf(top, s[kt][i]);
       }
     }
@@ -255,20 +282,21 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dq_f32(HeadsArgs a) {
   if (valid && g == 0) a.delta[out] = delta;
   f32x4 acc[DP / 16] = {};
 
+  NextTile<DP> next;
+  auto load = [&](int k0) {
+    next.load([&](int r, int col, f32x4& x, f32x4& y) {
+      if (k0 + r >= to || col >= a.d) return;
+      const int64_t at = w.k0 + k0 + r;
+      x = load4(static_cast<const float*>(a.k.data) + at * a.k.ts + hk * a.k.hs + col);
+      y = load4(static_cast<const float*>(a.v.data) + at * a.v.ts + hk * a.v.hs + col);
+    });
+  };
+  load(0);
   for (int k0 = 0; k0 < to; k0 += kF32Step) {
     __syncthreads();
-    for (int i = tid; i < kF32Step * (DP / 4); i += kF32Threads) {
-      const int r = i / (DP / 4), col = 4 * (i % (DP / 4)), j = k0 + r;
-      f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-      if (j < to && col < a.d) {
-        const int64_t at = w.k0 + j;
-        x = load4(static_cast<const float*>(a.k.data) + at * a.k.ts + hk * a.k.hs + col);
-        y = load4(static_cast<const float*>(a.v.data) + at * a.v.ts + hk * a.v.hs + col);
-      }
-      *reinterpret_cast<f32x4*>(&ks[r][col]) = x;
-      *reinterpret_cast<f32x4*>(&vs[r][col]) = y;
-    }
+    next.store(ks, vs);
     __syncthreads();
+    load(k0 + kF32Step);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       const f32x4 s = tile_dot<DP>(ks, 16 * kt, q, c, g);
@@ -321,29 +349,37 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
   // The first token that sees the tile's first key.
   const int tok0 = a.causal && first >= w.prefix ? max(first - (w.lk - w.lq), 0) : 0;
   const int rows = w.lq * a.group;
-  for (int r0 = tok0 * a.group; r0 < rows; r0 += kF32Step) {
-    __syncthreads();
-    for (int i = tid; i < kF32Step * (DP / 4); i += kF32Threads) {
-      const int r = i / (DP / 4), col = 4 * (i % (DP / 4)), row = r0 + r;
-      f32x4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-      if (row < rows && col < a.d) {
-        const int64_t at = w.q0 + row / a.group;
-        const int head = hk * a.group + row % a.group;
-        x = load4(static_cast<const float*>(a.q.data) + at * a.q.ts + head * a.q.hs + col);
-        y = load4(static_cast<const float*>(a.dout.data) + at * a.dout.ts + head * a.dout.hs + col);
-      }
-      *reinterpret_cast<f32x4*>(&qs[r][col]) = x;
-      *reinterpret_cast<f32x4*>(&os[r][col]) = y;
-    }
-    if (tid < kF32Step) {
-      const int row = r0 + tid;
+  NextTile<DP> next;
+  float lse = 0.0f, delta = 0.0f, slope = 0.0f;  // of row r0 + tid
+  auto load = [&](int r0) {
+    next.load([&](int r, int col, f32x4& x, f32x4& y) {
+      const int row = r0 + r;
+      if (row >= rows || col >= a.d) return;
+      const int64_t at = w.q0 + row / a.group;
+      const int head = hk * a.group + row % a.group;
+      x = load4(static_cast<const float*>(a.q.data) + at * a.q.ts + head * a.q.hs + col);
+      y = load4(static_cast<const float*>(a.dout.data) + at * a.dout.ts + head * a.dout.hs + col);
+    });
+    const int row = r0 + tid;
+    if (tid < kF32Step && row < rows) {
       const int head = hk * a.group + row % a.group;
       const int64_t at = static_cast<int64_t>(w.q0 + row / a.group) * a.heads + head;
-      row_lse[tid] = row < rows ? a.lse[at] : 0.0f;
-      row_delta[tid] = row < rows ? a.delta[at] : 0.0f;
-      row_slope[tid] = row < rows && a.slopes != nullptr ? a.slopes[head] : 0.0f;
+      lse = a.lse[at];
+      delta = a.delta[at];
+      if (a.slopes != nullptr) slope = a.slopes[head];
+    }
+  };
+  load(tok0 * a.group);
+  for (int r0 = tok0 * a.group; r0 < rows; r0 += kF32Step) {
+    __syncthreads();
+    next.store(qs, os);
+    if (tid < kF32Step) {
+      row_lse[tid] = lse;
+      row_delta[tid] = delta;
+      row_slope[tid] = slope;
     }
     __syncthreads();
+    load(r0 + kF32Step);
 #pragma unroll
     for (int qt = 0; qt < 2; ++qt) {
       const f32x4 s = tile_dot<DP>(qs, 16 * qt, k, c, g);

@@ -84,6 +84,27 @@ struct Range {
   int64_t bytes;
 };
 
+// The device allocation that a call's last checked range lies in: the small
+// tensors of a call often share one, and a look-up costs 0.2 us.
+struct Allocation {
+  uintptr_t lo, hi;
+};
+
+inline int check_device_range(const Range& r, int dev, Allocation* last) {
+  if (r.bytes <= 0) return SOFTMAX_OK;
+  const uintptr_t p = reinterpret_cast<uintptr_t>(r.p);
+  if (p >= last->lo && p < last->hi && static_cast<uintptr_t>(r.bytes) <= last->hi - p)
+    return SOFTMAX_OK;
+  if (const int rc = check_device_range(r.p, r.bytes, dev)) return rc;
+  hipDeviceptr_t base = nullptr;
+  size_t size = 0;
+  if (hipMemGetAddressRange(&base, &size, const_cast<void*>(r.p)) == hipSuccess)
+    *last = {reinterpret_cast<uintptr_t>(base), reinterpret_cast<uintptr_t>(base) + size};
+  else
+    (void)hipGetLastError();  // host memory: each range by itself
+  return SOFTMAX_OK;
+}
+
 // Every range is memory that the current device can use, and no output
 // overlaps an input or another output (`interleaved`: outputs may overlap
 // each other).  Empty ranges may be null.
@@ -102,12 +123,11 @@ int check_ranges(const Range (&in)[NI], const Range (&out)[NO], bool interleaved
   int dev = 0;
   const hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return fail_hip(e);
+  Allocation last = {};
   for (const Range& r : in)
-    if (r.bytes > 0)
-      if (const int rc = check_device_range(r.p, r.bytes, dev)) return rc;
+    if (const int rc = check_device_range(r, dev, &last)) return rc;
   for (const Range& r : out)
-    if (r.bytes > 0)
-      if (const int rc = check_device_range(r.p, r.bytes, dev)) return rc;
+    if (const int rc = check_device_range(r, dev, &last)) return rc;
   return SOFTMAX_OK;
 }
 
