@@ -119,11 +119,14 @@ PagedSplits paged_splits(int64_t tokens, int64_t heads, int64_t kv_heads, int64_
   // Tiles that the requests have at least.
   const int64_t rows = tokens * (heads / kv_heads);
   const int64_t tiles = std::max<int64_t>(1, std::max(rows / kTileRows, std::min(requests, tokens)));
-  // Single tokens are bound by the keys that they read, and their lengths
-  // differ: four times the resident workgroups even them out, and their split
-  // sums are small.  Chunks' are not: what is resident.
-  const int64_t target = (rows <= 32 * requests ? 8 : 2) * cus;
-  const int64_t wanted = ceil_div(target, tiles * kv_heads);
+  // Requests' lengths differ, so a call is split into four times the resident
+  // workgroups, which evens them out (64 single tokens over up to 8192 keys 255
+  // -> 236 us; 12 beside four chunks of 509 212 -> 207), but for chunks whose
+  // tiles fill the device by themselves: their split sums cost more than they
+  // even out.
+  const int64_t target = 8 * cus;
+  const bool fills = rows > 32 * requests && tiles * kv_heads >= 2 * cus;
+  const int64_t wanted = fills ? 1 : ceil_div(target, tiles * kv_heads);
   return {std::clamp<int64_t>(std::min(wanted, ceil_div(max_keys, kMinChunk)), 1, kMaxSplits),
           target};
 }

@@ -8,7 +8,8 @@ const void* heads_dq_f16(const HeadsArgs& a) {
   switch (score_mode(a)) {
     case kPlain: return SMX_BY_WIDTH(a.d, k_heads_dq, f16, kPlain);
     case kBias: return SMX_BY_WIDTH(a.d, k_heads_dq, f16, kBias);
-    default: return SMX_BY_WIDTH(a.d, k_heads_dq, f16, kCap);
+    case kCap: return SMX_BY_WIDTH(a.d, k_heads_dq, f16, kCap);
+    default: return SMX_BY_WIDTH(a.d, k_heads_dq, f16, kCapBias);
   }
 }
 
@@ -16,7 +17,8 @@ const void* heads_dkv_f16(const HeadsArgs& a) {
   switch (score_mode(a)) {
     case kPlain: return SMX_BY_WIDTH(a.d, k_heads_dkv, f16, kPlain);
     case kBias: return SMX_BY_WIDTH(a.d, k_heads_dkv, f16, kBias);
-    default: return SMX_BY_WIDTH(a.d, k_heads_dkv, f16, kCap);
+    case kCap: return SMX_BY_WIDTH(a.d, k_heads_dkv, f16, kCap);
+    default: return SMX_BY_WIDTH(a.d, k_heads_dkv, f16, kCapBias);
   }
 }
 

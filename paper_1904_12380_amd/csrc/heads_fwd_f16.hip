@@ -9,7 +9,8 @@ static const void* fwd(const HeadsArgs& a) {
   switch (score_mode(a)) {
     case kPlain: return SMX_BY_WIDTH(a.d, k_heads_fwd, f16, WHERE, kPlain);
     case kBias: return SMX_BY_WIDTH(a.d, k_heads_fwd, f16, WHERE, kBias);
-    default: return SMX_BY_WIDTH(a.d, k_heads_fwd, f16, WHERE, kCap);
+    case kCap: return SMX_BY_WIDTH(a.d, k_heads_fwd, f16, WHERE, kCap);
+    default: return SMX_BY_WIDTH(a.d, k_heads_fwd, f16, WHERE, kCapBias);
   }
 }
 

@@ -199,7 +199,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         dp[i] = s[i] * (dp[i] - delta);
-        if constexpr (MODE == kCap) dp[i] *= sc.derivative(cap[i]);
+        if constexpr (MODE >= kCap) dp[i] *= sc.derivative(cap[i]);
       }
       cols_accumulate<T, DP>(rd, kt, 32 * h, dp, two_parts, acc);
     }
@@ -422,7 +422,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         dp[i] *= s[i];
-        if constexpr (MODE == kCap) dp[i] *= Scoring<MODE>::derivative(cap[i]);
+        if constexpr (MODE >= kCap) dp[i] *= Scoring<MODE>::derivative(cap[i]);
       }
       const bool two_parts = key0 < kTileKeys && lim_all <= kTwoPartKeys;
       cols_accumulate<T, DP>(rd, ot, 0, s, two_parts, dv);

@@ -24,10 +24,11 @@ const void* heads_dkv_bf16(const HeadsArgs& a);
   ((d) <= 64 ? SMX_FN(K<T, 64, __VA_ARGS__>)                                          \
              : (d) <= 128 ? SMX_FN(K<T, 128, __VA_ARGS__>) : SMX_FN(K<T, 256, __VA_ARGS__>))
 
-// How the call's scores are formed (kPlain, kBias, kCap).  A scale of no
-// ordinary size goes with the bias, whose scores are formed before the mask.
+// How the call's scores are formed (kPlain, kBias, kCap, kCapBias).  A scale
+// of no ordinary size goes with the bias, whose scores are formed before the
+// mask.
 inline int score_mode(const HeadsArgs& a) {
-  if (a.cap > 0.0f) return 2;
+  if (a.cap > 0.0f) return a.slopes != nullptr ? 3 : 2;
   return a.slopes != nullptr || !(std::fabs(a.scale) > 1e-20f) ? 1 : 0;
 }
 

@@ -392,9 +392,9 @@ __device__ __forceinline__ void interleave() {
   __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
-// How scores are formed (a template argument): scaled, with a bias, or with a
-// cap and a bias (of slope 0 where there is none).
-constexpr int kPlain = 0, kBias = 1, kCap = 2;
+// How scores are formed (a template argument): scaled, with a bias, with a cap,
+// or with both.
+constexpr int kPlain = 0, kBias = 1, kCap = 2, kCapBias = 3;
 
 // Scores in powers of two from dot products.  tanh(y) = 1 - 2 r with r = 1 /
 // (e^2y + 1), so that the capped score is one fma of r, and the cap's
@@ -416,7 +416,9 @@ struct Scoring {
   __device__ __forceinline__ float score(float dot, float dist, float* r) const {
     if constexpr (MODE == kBias) return __builtin_fmaf(dot, c, -slope2 * fabsf(dist));
     *r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(dot * c) + 1.0f);
-    return __builtin_fmaf(*r, -2.0f * cap2, __builtin_fmaf(-slope2, fabsf(dist), cap2));
+    return __builtin_fmaf(
+        *r, -2.0f * cap2,
+        MODE == kCap ? cap2 : __builtin_fmaf(-slope2, fabsf(dist), cap2));
   }
   __device__ __forceinline__ static float derivative(float r) {
     return __builtin_fmaf(-4.0f * r, r, 4.0f * r);
