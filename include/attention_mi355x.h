@@ -27,9 +27,10 @@
  * Types: SOFTMAX_F32, SOFTMAX_F16 or SOFTMAX_BF16 for all tensors of a call;
  * lse and slopes are fp32.  Sums, statistics and gradients accumulate in
  * fp32; with 16-bit types the weights are rounded to the type for the
- * products on the matrix cores (in two parts, which keep 16 bits or more, for
- * the first 64 keys of a document, where one weight's rounding is not
- * averaged over many).  Results are bitwise deterministic.
+ * products on the matrix cores (in two parts, which keep 16 bits or more, where
+ * one weight's rounding is not averaged over many: the first 64 keys of rows
+ * that see at most 128, and in the gradients any block with a weight above
+ * 1/8).  Results are bitwise deterministic.
  *
  * Layout: a tensor [tokens, heads, d] has its d entries contiguous; strides
  * between tokens and heads are in elements and not negative.  d is a
@@ -53,7 +54,8 @@ extern "C" {
 #define SOFTMAX_BF16 2
 
 #define SOFTMAX_HEADS_MAX_DIM 256
-#define SOFTMAX_HEADS_MAX_STRIDE 8388608 /* between tokens of softmax_heads_t */
+#define SOFTMAX_HEADS_MAX_STRIDE 8388608 /* elements between tokens */
+#define SOFTMAX_MIN_CAP 1e-30f           /* smallest cap but 0 */
 
 /* A tensor [tokens, heads, d] of a call's type. */
 typedef struct softmax_heads_t {
@@ -82,7 +84,7 @@ typedef struct softmax_cache_t {
 /* How scores are formed from the dot products. */
 typedef struct softmax_score_t {
   float scale;           /* finite */
-  float cap;             /* >= 0 and finite; 0: no cap */
+  float cap;             /* 0: no cap, or SOFTMAX_MIN_CAP and up, finite */
   int32_t causal;        /* 0 or 1 */
   const float* slopes;   /* device, [heads]; NULL: no bias.  Constants: they
                             get no gradient */
@@ -102,7 +104,11 @@ typedef struct softmax_score_t {
  *
  * Tokens past the last document get o = 0 and lse = -infinity.  o and lse
  * may not overlap the inputs.  tokens_q * heads and tokens_k * heads are below
- * 2^31.
+ * 2^31, tokens_k at most 2^30.
+ *
+ * NaN and infinity stay in their document: in q they reach their own row, in
+ * k and v any row of the document (also of one that does not see the key, when
+ * both lie in one tile).
  */
 SOFTMAX_API int softmax_packed_attention_fwd(const softmax_heads_t* q, const softmax_heads_t* k,
                                              const softmax_heads_t* v, void* o, float* lse,
@@ -163,7 +169,8 @@ SOFTMAX_API int64_t softmax_paged_attention_workspace(int64_t tokens, int64_t he
  *   block_table  device, [requests, table_width] int32: the block that holds
  *                the keys c * block_size .. of a request at column c
  *   cu_q         device, [requests + 1] int32, ascending from 0
- *   key_lens     device, [requests] int32; clamped to table_width * block_size
+ *   key_lens     device, [requests] int32; clamped to table_width * block_size,
+ *                which is at most 2^30
  *   o            [tokens, heads, d], contiguous; written
  *   lse          [tokens, heads] fp32, or NULL
  *   workspace    as for softmax_packed_attention_bwd

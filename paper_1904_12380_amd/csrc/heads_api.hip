@@ -325,7 +325,7 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
   int64_t qb = 0, kb = 0, vb = 0;
   if (size == 0 || !score_ok(score) || !heads_ok(q, size, &qb) || !cache_ok(k, size, &kb) ||
       !cache_ok(v, size, &vb) || !same_cache(k, v) || q->d != k->d || table_width < 0 ||
-      table_width > INT32_MAX / k->block_size ||
+      table_width > kMaxTokens / k->block_size ||
       !sizes_ok(q->tokens, q->heads, k->heads, requests) || !aligned16(o) ||
       !aligned16(workspace))
     return SOFTMAX_ERR_INVALID_ARG;

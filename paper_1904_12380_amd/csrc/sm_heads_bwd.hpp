@@ -19,6 +19,20 @@
 
 namespace smx {
 
+// Weights and score gradients of a block of 32 rows and 32 keys are taken in
+// two 16-bit parts where a weight of the block is larger than this: its
+// rounding is then a part of the sums that no others average, and with D's
+// would put gradients of rows with few keys (or a steep bias) off by 1.7 times
+// their own rounding to 16 bits.
+constexpr float kLargeWeight = 0.125f;
+
+__device__ __forceinline__ bool any_large(const f32x16& p) {
+  float top = p[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
+  return __any(top > kLargeWeight);
+}
+
 template <typename T, int DP>
 __device__ __forceinline__ f32x16 rows_dot(const TileReader<DP>& rd, const char SMX_LDS* tile,
                                            int row0,
@@ -135,6 +149,9 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
     for (int i = 0; i < DP / 16; ++i) q[i] = -q[i];
   }
   f32x16 acc[DP / 32] = {};
+  // The sum of P (dP - D), which D's error alone keeps from 0 (the weights sum
+  // to 1): what the gradients of the keys correct it by.
+  float rest[2] = {0.0f, 0.0f};
 
   const TileReader<DP> rd;
   constexpr int kTile = kTileKeys * DP * 2;
@@ -146,16 +163,10 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
     keys.stage(a, keys.v, kt + kTile, k0 + r0);
   };
 
-  // Weights of 32 keys from dot products; cap: what its derivative takes.
+  // Weights of 32 keys from dot products; cap: what the cap's derivative takes.
   auto weights = [&](f32x16& s, f32x16& cap, int k0) {
     if constexpr (MODE != kPlain) {
-      const float dist = static_cast<float>(pos - k0 - 4 * half);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float r = 0.0f;
-        s[i] = sc.score(s[i], dist - (8 * (i / 4) + i % 4), &r);
-        cap[i] = r;
-      }
+      sc.scores(s, cap, static_cast<float>(pos - k0 - 4 * half), -1.0f);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -lse2));
@@ -175,7 +186,6 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
     if (k0 >= lim_any) continue;
     const char SMX_LDS* kt = lds + buf * 2 * kTile;
     const char SMX_LDS* vt = kt + kTile;
-    const bool two_parts = k0 == 0 && lim_all <= kTwoPartKeys;
     if (k0 == 0 && lim_all <= kTileKeys) {
       // Rows that see no key past this tile: D from the weights themselves,
       // which o's rounding would put off where few keys share them.
@@ -196,14 +206,17 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
       f32x16 s = rows_dot<T, DP>(rd, kt, 32 * h, q), cap;
       f32x16 dp = rows_dot<T, DP>(rd, vt, 32 * h, dout);
       weights(s, cap, k0 + 32 * h);
+      const bool two_parts = any_large(s);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         dp[i] = s[i] * (dp[i] - delta);
+        rest[i % 2] += dp[i];
         if constexpr (MODE >= kCap) dp[i] *= sc.derivative(cap[i]);
       }
       cols_accumulate<T, DP>(rd, kt, 32 * h, dp, two_parts, acc);
     }
   }
+  delta += (rest[0] + rest[1]) + half32_partner(rest[0] + rest[1]);
   if (valid && half == 0)
     reinterpret_cast<float2*>(a.delta)[static_cast<int64_t>(head) * a.tokens_q + token] =
         make_float2(-lse2 / c, -delta);
@@ -392,15 +405,9 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
       f32x16 s, cap;
       if constexpr (MODE != kPlain) {
         const Scoring<MODE> sc(a, a.slopes != nullptr ? a.slopes[head] : 0.0f);
-        const float dist = static_cast<float>(t0 + 4 * half + w.lk - w.lq - key);
         s = rows_dot<T, DP>(rd, qt, 0, k);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int r = 8 * (i / 4) + i % 4;
-          float x = 0.0f;
-          s[i] = sc.score(s[i], dist + r, &x) + stats[buf][0][r + 4 * half];
-          cap[i] = x;
-        }
+        sc.scores(s, cap, static_cast<float>(t0 + 4 * half + w.lk - w.lq - key), 1.0f);
+        s += rows_stat(stats[buf][0]);
       } else {
         __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
         s = rows_dot<T, DP>(rd, qt, 0, k, rows_stat(stats[buf][0]));
@@ -419,12 +426,12 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
           if (key >= keys_seen(a, w, tok)) s[i] = 0.0f;
         }
       }
+      const bool two_parts = any_large(s);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         dp[i] *= s[i];
         if constexpr (MODE >= kCap) dp[i] *= Scoring<MODE>::derivative(cap[i]);
       }
-      const bool two_parts = key0 < kTileKeys && lim_all <= kTwoPartKeys;
       cols_accumulate<T, DP>(rd, ot, 0, s, two_parts, dv);
       cols_accumulate<T, DP>(rd, qt, 0, dp, two_parts, dk);
     }

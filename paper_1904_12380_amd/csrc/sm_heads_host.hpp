@@ -26,11 +26,14 @@ inline bool add_extent(int64_t count, int64_t stride, int64_t* extent) {
          !__builtin_add_overflow(*extent, x, extent);
 }
 
+// Positions and their sums with a tile's stay within 31 bits.
+constexpr int64_t kMaxTokens = int64_t(1) << 30;
+
 // The layout rules of a tensor [tokens, heads, d]; its extent in bytes (0
 // when empty).
 inline bool heads_ok(const softmax_heads_t* t, int size, int64_t* bytes) {
   *bytes = 0;
-  if (t == nullptr || t->tokens < 0 || t->heads < 0 || t->tokens > INT32_MAX ||
+  if (t == nullptr || t->tokens < 0 || t->heads < 0 || t->tokens > kMaxTokens ||
       t->heads > INT32_MAX || t->d < 8 || t->d > SOFTMAX_HEADS_MAX_DIM || t->d % 8 != 0)
     return false;
   // A tile's offsets between its rows fit 31 bits.
@@ -54,7 +57,9 @@ inline bool cache_ok(const softmax_cache_t* t, int size, int64_t* bytes) {
       t->heads < 0 || t->heads > INT32_MAX || t->d < 8 || t->d > SOFTMAX_HEADS_MAX_DIM ||
       t->d % 8 != 0)
     return false;
-  if (t->block_stride < 0 || t->token_stride < 0 || t->head_stride < 0) return false;
+  if (t->block_stride < 0 || t->token_stride < 0 || t->token_stride > SOFTMAX_HEADS_MAX_STRIDE ||
+      t->head_stride < 0)
+    return false;
   if (t->blocks == 0 || t->heads == 0) return true;
   const int64_t strip = 16 / size;
   if (!aligned16(t->data) || t->block_stride % strip != 0 || t->token_stride % strip != 0 ||
@@ -75,7 +80,8 @@ inline bool same_cache(const softmax_cache_t* a, const softmax_cache_t* b) {
 }
 
 inline bool score_ok(const softmax_score_t* s) {
-  return s != nullptr && std::isfinite(s->scale) && std::isfinite(s->cap) && s->cap >= 0.0f &&
+  return s != nullptr && std::isfinite(s->scale) && std::isfinite(s->cap) &&
+         (s->cap == 0.0f || s->cap >= SOFTMAX_MIN_CAP) &&
          (s->causal == 0 || s->causal == 1) && (s->causal == 1 || s->prefix == nullptr);
 }
 

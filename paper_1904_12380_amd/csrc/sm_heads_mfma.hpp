@@ -398,32 +398,67 @@ constexpr int kPlain = 0, kBias = 1, kCap = 2, kCapBias = 3;
 
 // Scores in powers of two from dot products.  tanh(y) = 1 - 2 r with r = 1 /
 // (e^2y + 1), so that the capped score is one fma of r, and the cap's
-// derivative 1 - tanh^2 is 4 r (1 - r).  Within 2e-7 of the cap, which the
-// weights' rounding to 16 bits covers (up to caps of 1000).
+// derivative 1 - tanh^2 is 4 r (1 - r).  The difference is within 2e-7 of the
+// cap, which the weights' rounding to 16 bits covers up to kWideCap; past it
+// tanh is formed to 3e-7 of itself, from its series where it is small.
+constexpr float kWideCap = 256.0f;
+
 template <int MODE>
 struct Scoring {
-  float c;       // scale in powers of two (kCap: of e^2y)
-  float cap2;    // the cap in powers of two
-  float slope2;  // the slope in powers of two
+  float c;        // scale in powers of two (with a cap: of e^2y)
+  float cap2;     // the cap in powers of two
+  float slope2;   // the slope in powers of two
+  bool wide;
 
   __device__ __forceinline__ Scoring(const HeadsArgs& a, float slope) {
     c = MODE == kPlain ? fabsf(a.scale) * kLog2eF
         : MODE == kBias ? a.scale * kLog2eF : a.scale * a.exp_cap;
     cap2 = a.cap * kLog2eF;
     slope2 = slope * kLog2eF;
+    wide = a.cap > kWideCap;
   }
-  // The score of a dot product at a distance; *r: for the derivative.
-  __device__ __forceinline__ float score(float dot, float dist, float* r) const {
-    if constexpr (MODE == kBias) return __builtin_fmaf(dot, c, -slope2 * fabsf(dist));
-    *r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(dot * c) + 1.0f);
-    return __builtin_fmaf(
-        *r, -2.0f * cap2,
-        MODE == kCap ? cap2 : __builtin_fmaf(-slope2, fabsf(dist), cap2));
+
+  // tanh(y) for e^2y = 2^z, as 1 - 2 r.  The series' next term is 62 / 2835 y^8,
+  // 3e-7 at 1/4.
+  __device__ __forceinline__ static float wide_r(float z) {
+    const float y = z * (0.5f * kLn2F), s = y * y;
+    const float series =
+        y * __builtin_fmaf(
+                s,
+                __builtin_fmaf(s, __builtin_fmaf(s, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f),
+                1.0f);
+    return fabsf(y) < 0.25f ? series
+                            : 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z) + 1.0f);
+  }
+
+  // 16 dot products of a lane to scores, register i at the distance dist + step *
+  // (8 (i / 4) + i % 4); with a cap r[i] = 1 / (e^2y + 1).
+  __device__ __forceinline__ void scores(f32x16& s, f32x16& r, float dist, float step) const {
+    auto bias = [&](int i) {
+      return -slope2 * fabsf(__builtin_fmaf(step, static_cast<float>(8 * (i / 4) + i % 4), dist));
+    };
+    if constexpr (MODE == kBias) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_fmaf(s[i], c, bias(i));
+    } else if (!wide) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        r[i] = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[i] * c) + 1.0f);
+        s[i] = __builtin_fmaf(r[i], -2.0f * cap2, MODE == kCap ? cap2 : cap2 + bias(i));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float t = wide_r(s[i] * c);
+        r[i] = 0.5f - 0.5f * t;
+        s[i] = MODE == kCap ? t * cap2 : __builtin_fmaf(t, cap2, bias(i));
+      }
+    }
   }
   __device__ __forceinline__ static float derivative(float r) {
     return __builtin_fmaf(-4.0f * r, r, 4.0f * r);
   }
-  // Powers of two per unit of what score() (kPlain: the dot product) gives.
+  // Powers of two per unit of what scores() (kPlain: the dot product) gives.
   __device__ __forceinline__ float unit() const { return MODE == kPlain ? c : 1.0f; }
 };
 
@@ -431,8 +466,8 @@ struct Scoring {
 // that products with the scale stay ordered.
 constexpr float kUnseen = -3.0e38f;
 
-// Weights and score gradients are taken in two 16-bit parts for the first 64
-// keys of a document where rows see at most this many keys.
+// Weights are taken in two 16-bit parts for the first 64 keys of a document
+// where rows see at most this many keys.
 constexpr int kTwoPartKeys = 128;
 
 // A running maximum is moved (and the sums rescaled) when a score passes it by
@@ -473,12 +508,10 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
   if constexpr (MODE != kPlain) {
     const float dist = static_cast<float>(w.pos - k0 - 4 * half);
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float r;
-        s[kt][i] = sc.score(s[kt][i], dist - (32 * kt + 8 * (i / 4) + i % 4), &r);
-      }
+    for (int kt = 0; kt < KT; ++kt) {
+      f32x16 r;
+      sc.scores(s[kt], r, dist - 32 * kt, -1.0f);
+    }
   }
   if (k0 + 32 * KT > w.lim_all || absent != 0) {
 #pragma unroll
