@@ -66,7 +66,8 @@ struct HeadsArgs {
   SplitStat* part_stat;  // [splits, tokens, heads]
   float* part_o;         // [splits, tokens, heads, d]
   int splits;
-  int target;          // workgroups that fill the device
+  int target;          // workgroups that a call aims at
+  int min_chunk;       // fewest keys of a split
   int n, tokens_q, tokens_k, heads, kv_heads, group, d;
   int causal;
   float scale, cap;
@@ -208,11 +209,9 @@ __device__ __forceinline__ int keys_seen(const HeadsArgs& a, const DocTile& w, i
 
 // Splits of the keys (paged).  All chunks of a call have the same length: the
 // keys of all of its tiles of ROWS rows over the workgroups that fill the
-// device, in whole tiles of 64 keys, at least kMinChunk, and such that the
+// device, in whole tiles of 64 keys, at least min_chunk, and such that the
 // longest request fits the launched splits.  0: not split.  Every wavefront of
 // a call computes the same from the lengths; the first notes it for the join.
-constexpr int kMinChunk = 256;
-
 template <int ROWS>
 __device__ __forceinline__ int split_chunk(const HeadsArgs& a, const DocLanes& mine) {
   if (a.splits <= 1) return 0;
@@ -227,7 +226,7 @@ __device__ __forceinline__ int split_chunk(const HeadsArgs& a, const DocLanes& m
   const int64_t all = static_cast<int64_t>(sum) * a.kv_heads;
   const int64_t most = static_cast<int64_t>(longest);
   int64_t chunk = max((all + a.target - 1) / a.target, (most + a.splits - 1) / a.splits);
-  chunk = max((chunk + 63) / 64 * 64, static_cast<int64_t>(kMinChunk));
+  chunk = max((chunk + 63) / 64 * 64, static_cast<int64_t>(a.min_chunk));
   const int n = __builtin_amdgcn_readfirstlane(chunk >= most ? 0 : static_cast<int>(chunk));
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.part_head[0] = n;
   return n;

@@ -318,3 +318,129 @@ def test_paged_agrees_with_packed(sm):
             torch.tensor([b], dtype=torch.int32, device="cuda")))
     # two orders of fp32 sums: 200 terms of weight times value
     assert (torch.cat(parts) - want).abs().max() <= 2e-5
+
+
+# ---------------------------------------------------------------------------
+# Longer ones: several tiles, split keys and split rows, many documents.
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("docs,heads,kv_heads,how", [
+    ([(1500, 1500)], 1, 1, dict()),
+    ([(1100, 1100), (70, 70)], 4, 1, dict(cap=15.0)),
+    ([(1030, 1030)], 3, 1, dict(causal=False)),
+    ([(700, 1300), (40, 900)], 5, 1, dict(bias=True)),
+    ([(1200, 500)], 6, 2, dict(prefix=[333])),
+    ([(640, 640), (641, 641)], 8, 2, dict(bias=True, cap=9.0, prefix=[500, 0]))])
+def test_packed_long_documents(sm, dtype, docs, heads, kv_heads, how):
+    case = Packed(torch, 40, dtype, docs, heads, kv_heads, 64, **how)
+    assert_within(case.run(sm), case.oracle(), TRAIN)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("count", [62, 63, 64, 65, 200])
+def test_packed_many_documents(sm, dtype, count):
+    """Around the 64 documents that a wavefront's lanes hold, and more."""
+    lens = np.random.default_rng(count).integers(0, 30, count)
+    lens[count // 2] = 300
+    case = Packed(torch, 41, dtype, self_docs(*(int(n) for n in lens)), 4, 2, 64, spare=(1, 1))
+    assert_within(case.run(sm), case.oracle(), TRAIN)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cap", [256.0, 257.0, 3000.0, 1e6, 1e-3])
+def test_packed_caps_of_all_sizes(sm, dtype, cap):
+    case = Packed(torch, 42, dtype, self_docs(90, 40), 2, 1, 64, cap=cap, spread=4.0)
+    want = case.oracle()
+    # the bound's term for the cap is for caps of the scores' size
+    if cap > 256.0:
+        want = {**case_with_cap(case, 0.0), **{n: want[n] for n in ("o", "lse", "dq", "dk", "dv")}}
+    assert_within(case.run(sm), want, TRAIN)
+
+
+def case_with_cap(case, cap):
+    kept = case.ref["cap"]
+    case.ref["cap"] = cap
+    bounds = {n: x for n, x in case.oracle().items() if n.startswith("e_")}
+    case.ref["cap"] = kept
+    return bounds
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_packed_nothing_on_one_side(sm, dtype):
+    """No documents, no queries, no keys: zeros, and no read of what is not
+    there."""
+    t = torch.randn(7, 2, 64, device="cuda").to({"f32": torch.float32, "f16": torch.float16,
+                                                 "bf16": torch.bfloat16}[dtype])
+    none, lse0 = t[:0], torch.empty(0, 2, device="cuda")
+    zero = torch.tensor([0, 0], dtype=torch.int32, device="cuda")
+    seven = torch.tensor([0, 7], dtype=torch.int32, device="cuda")
+    o, lse = sm.softmax_packed_attention_fwd(t, t, t, zero[:1])
+    assert not o.any() and torch.isneginf(lse).all()
+    grads = sm.softmax_packed_attention_bwd(t, t, t, t, o, lse, zero[:1])
+    assert not any(g.any() for g in grads)
+    o, lse = sm.softmax_packed_attention_fwd(t, none, none, seven, zero)
+    assert not o.any() and torch.isneginf(lse).all()
+    dq, dk, dv = sm.softmax_packed_attention_bwd(t, t, none, none, o, lse, seven, zero)
+    assert not dq.any() and dk.numel() == dv.numel() == 0
+    o, lse = sm.softmax_packed_attention_fwd(none, t, t, zero, seven)
+    assert o.numel() == lse.numel() == 0
+    dq, dk, dv = sm.softmax_packed_attention_bwd(none, none, t, t, none, lse0, zero, seven)
+    assert dq.numel() == 0 and not dk.any() and not dv.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_packed_infinities_reach_their_own_rows(sm, dtype):
+    case = Packed(torch, 43, dtype, self_docs(150), 2, 1, 64)
+    want = case.run(sm, train=False)["o"]
+    q = case.t["q"].clone()
+    q[70, 1, 3] = float("inf")
+    got = case.run(sm, train=False, q=q)["o"]
+    assert torch.isnan(got[70, 1]).all()
+    keep = torch.ones(150, 2, dtype=torch.bool, device="cuda")
+    keep[70, 1] = False
+    assert torch.equal(got[keep], want[keep])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("requests,heads,kv_heads,size", [
+    ([(1, 9000)], 8, 1, 16),                       # many splits
+    ([(1, 5000), (1, 3), (200, 4100)], 8, 2, 64),  # splits beside chunks
+    ([(1, 100)] * 130, 4, 1, 32),                  # more requests than lanes
+    ([(5, 2000), (0, 700), (1, 1999)], 16, 2, 128)])
+def test_paged_long(sm, dtype, requests, heads, kv_heads, size):
+    case = Paged(torch, 44, dtype, requests, heads, kv_heads, 64, size)
+    assert_within(case.run(sm), case.oracle(), ("o", "lse"))
+
+
+def test_refusals(sm):
+    q = torch.randn(10, 4, 64, device="cuda").bfloat16()
+    k = torch.randn(10, 2, 64, device="cuda").bfloat16()
+    cu = torch.tensor([0, 10], dtype=torch.int32, device="cuda")
+    fwd = sm.softmax_packed_attention_fwd
+    fwd(q, k, k, cu)
+    for bad in (dict(k=k.float()), dict(k=k.cpu()), dict(cu_q=cu.long()), dict(q=q.double()),
+                dict(slopes=torch.ones(4, device="cuda").half()),
+                dict(out=torch.empty_like(q).float())):
+        with pytest.raises((TypeError, ValueError)):
+            fwd(**{**dict(q=q, k=k, v=k, cu_q=cu), **bad})
+    for bad in (dict(q=q[0]), dict(q=q.transpose(1, 2)), dict(cu_q=cu[:0]), dict(k=k[:9], v=k[:9]),
+                dict(slopes=torch.ones(3, device="cuda")), dict(prefix=cu),
+                dict(out=torch.empty(10, 4, 63, device="cuda").bfloat16()),
+                dict(lse=torch.empty(4, 10, device="cuda").t())):
+        with pytest.raises(ValueError):
+            fwd(**{**dict(q=q, k=k, v=k, cu_q=cu), **bad})
+    for bad in (dict(scale=float("nan")), dict(cap=-2.0), dict(out=q),
+                dict(q=q[..., :60], k=k[..., :60], v=k[..., :60]),
+                dict(q=q.flatten()[4:4 + 9 * 256].view(9, 4, 64), k=k[:9], v=k[:9]),
+                dict(causal=False, prefix=cu[:1])):
+        with pytest.raises(sm.SoftmaxError) as e:
+            fwd(**{**dict(q=q, k=k, v=k, cu_q=cu), **bad})
+        assert e.value.code == sm.ERR_INVALID_ARG
+    pinned = torch.empty(4, dtype=torch.int32)       # pageable host memory behind a pointer
+    assert sm.load_library().softmax_cache_slots(
+        cu.data_ptr(), cu.data_ptr(), 2, q.data_ptr(), 1, pinned.data_ptr(), 4, cu.data_ptr(), 16,
+        k.data_ptr(), k.data_ptr() + 64, k.data_ptr() + 128, 1, k.data_ptr() + 256,
+        k.data_ptr() + 320, None) == sm.ERR_NOT_DEVICE
+    with pytest.raises(ValueError):
+        sm.softmax_packed_attention(q, k, k, cu, slopes=torch.ones(4, device="cuda",
+                                                                   requires_grad=True))
