@@ -19,6 +19,7 @@ import ctypes
 import paper_1904_12380_amd as _sm
 
 HEADS_MAX_DIM = 256
+HEADS_MAX_STRIDE = 8388608
 
 _i64, _i32, _f32, _vp = ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_void_p
 
@@ -133,7 +134,7 @@ def _vector(t, name: str, dtype, count, device) -> int:
 def _score(q, docs, causal, scale, cap, slopes, prefix) -> _Score:
     torch = _sm._torch_mod
     if scale is None:
-        scale = q.shape[2] ** -0.5
+        scale = max(q.shape[2], 1) ** -0.5
     return _Score(
         scale, cap, 1 if causal else 0,
         None if slopes is None else _vector(slopes, "slopes", torch.float32, q.shape[1], q.device),
@@ -233,6 +234,14 @@ def _on_stream(work, stream) -> None:
         work.record_stream(stream)
 
 
+def _fits(t) -> bool:
+    """Whether a tensor [tokens, heads, d] has the layout that the kernels take
+    (a gradient's layout is what the operation behind it left)."""
+    strip, (ts, hs, ds) = 16 // t.element_size(), t.stride()
+    return ds == 1 and ts <= HEADS_MAX_STRIDE and ts % strip == hs % strip == 0 and \
+        t.data_ptr() % 16 == 0
+
+
 _function = None
 
 
@@ -253,10 +262,11 @@ def softmax_packed_attention(q, k, v, cu_q, cu_k=None, *, causal=True, scale=Non
                 return o
 
             @staticmethod
+            @torch.autograd.function.once_differentiable
             def backward(ctx, dout):
                 q, k, v, o, lse, cu_q, cu_k, slopes, prefix = ctx.saved_tensors
-                if dout.stride(-1) != 1:
-                    dout = dout.contiguous()
+                if not _fits(dout):
+                    dout = dout.clone(memory_format=torch.contiguous_format)
                 grads = softmax_packed_attention_bwd(dout, q, k, v, o, lse, cu_q, cu_k,
                                                      slopes=slopes, prefix=prefix, **ctx.how)
                 return (*grads, None, None, None, None, None)

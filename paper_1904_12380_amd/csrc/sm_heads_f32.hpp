@@ -417,7 +417,9 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_dkv_f32(HeadsArgs a) {
 template <typename T>
 __device__ __forceinline__ void join_row(const HeadsArgs& a, int64_t rows, int64_t row, int lane,
                                          SplitStat mine) {
-  const int count = __builtin_amdgcn_readfirstlane(mine.count);
+  // Sums that do not ascend leave rows that no workgroup wrote: what their
+  // places hold is no number of splits.
+  const int count = clamp_i(__builtin_amdgcn_readfirstlane(mine.count), 0, a.splits);
   if (lane >= count) mine = {-INFINITY, 0.0f, 0, 0};
   const float m = seg_max<64>(mine.m);
   const float weight = __builtin_amdgcn_exp2f((mine.m - (m == -INFINITY ? 0.0f : m)) * kLog2eF);

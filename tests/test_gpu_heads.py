@@ -444,3 +444,45 @@ def test_refusals(sm):
     with pytest.raises(ValueError):
         sm.softmax_packed_attention(q, k, k, cu, slopes=torch.ones(4, device="cuda",
                                                                    requires_grad=True))
+
+
+def test_gradients_of_any_layout(sm):
+    """autograd hands the gradient on as the operation behind left it: slices
+    whose rows are not whole 16-byte strips, and expanded ones."""
+    case = Packed(torch, 21, "bf16", self_docs(33, 7), 4, 2, 64)
+    leaves = [case.t[n].clone().requires_grad_() for n in ("q", "k", "v")]
+    wide = torch.randn(40, 4 * 64 + 3, device="cuda").bfloat16()
+    for dout in (wide[:, 1:257].unflatten(1, (4, 64)), wide[:, 3:].unflatten(1, (4, 64)),
+                 wide[:1, :1, None].expand(40, 4, 64)):
+        o = sm.softmax_packed_attention(*leaves, *case.cu, **case.own)
+        got = torch.autograd.grad(o, leaves, dout)
+        o, lse = sm.softmax_packed_attention_fwd(*[case.t[n] for n in ("q", "k", "v")], *case.cu,
+                                                 **case.own)
+        want = sm.softmax_packed_attention_bwd(
+            dout.contiguous(), *[case.t[n] for n in ("q", "k", "v")], o, lse, *case.cu,
+            **case.own)
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def test_gradients_have_no_gradient_of_their_own(sm):
+    case = Packed(torch, 22, "f32", self_docs(9,), 2, 2, 16)
+    leaves = [case.t[n].clone().requires_grad_() for n in ("q", "k", "v")]
+    o = sm.softmax_packed_attention(*leaves, *case.cu, **case.own)
+    dq, = torch.autograd.grad(o.sum(), leaves[:1], create_graph=True)
+    with pytest.raises(RuntimeError):
+        dq.sum().backward()
+
+
+def test_paged_sums_out_of_order_stay_in_bounds(sm):
+    """Sums that do not ascend, in a call that is split: what comes out is not
+    specified, but nothing outside of the tensors is touched."""
+    case = Paged(torch, 23, "bf16", [(300, 3000), (1, 900), (2, 2000)], 2, 1, 64, 16)
+    table = torch.from_numpy(case.table).to(torch.int32).cuda()
+    keys = torch.tensor(case.keys, dtype=torch.int32, device="cuda")
+    for bad in ([0, 300, 1, 303], [0, 303, 2, 1], [5, 0, 1 << 30, 7]):
+        cu = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        guard = torch.full((3, 303, 2, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        sm.softmax_paged_attention_fwd(case.q.cuda(), *case.t, table, cu, keys, out=guard[1],
+                                       **case.own)
+        torch.cuda.synchronize()
+        assert (guard[::2] == 7).all()
