@@ -51,6 +51,8 @@ __device__ __forceinline__ SlotRequest slot_request(const SlotArgs& a, int b) {
 // requests.  The token at a block's first row writes the block's table entry:
 // every new block starts with a new token, so each entry has one writer, and
 // entries that are read (blocks held before) are never written.
+// Bound by latency: 8 requests of one token 3.6 us, 2048 of up to 320 (65536
+// tokens) 8.9 us, of a call of 11.4 and 12.2.
 __global__ __launch_bounds__(kSlotThreads) void k_cache_slots(SlotArgs a) {
   __shared__ int64_t tokens_before[kSlotThreads + 1], blocks_before[kSlotThreads];
   __shared__ int64_t wave_sums[3][kSlotThreads / 64];
@@ -158,7 +160,10 @@ struct AppendArgs {
   int per_head, heads, log_block;
 };
 
-// One strip of a key and of its value per thread and turn.
+// One strip of a key and of its value per thread and turn: neighbouring lanes
+// take neighbouring strips of a row, so that both sides move whole lines.  Bound
+// by memory: 16384 tokens of 8 heads of 128 (134 MB in all) 21.9 us, 6.1 TB/s;
+// 64 tokens 3-5 us, the launch.
 __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
   const unsigned per_head = a.per_head, heads = a.heads;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < a.strips;
