@@ -154,6 +154,10 @@ int64_t key_splits(int64_t tokens_q, int64_t tokens_k, int64_t heads, int64_t kv
   return std::clamp<int64_t>(std::min(ceil_div(kKeyTarget, tiles), turns / kMinTurns), 1, 16);
 }
 
+// Workgroups that share a key tile's sum: the sum of one is a few loads behind
+// one another, and most tiles of short documents have nothing to sum.
+constexpr int kSumParts = 4;
+
 // The backward pass' statistics of every row, in whole 16-byte strips, and
 // its split sums.
 int64_t stat_bytes(int64_t tokens_q, int64_t heads) { return (tokens_q * heads * 8 + 15) / 16 * 16; }
@@ -301,7 +305,7 @@ SOFTMAX_API int softmax_packed_attention_bwd(const softmax_heads_t* dout,
         launch2(dkv_fn(dtype, a), slots * a.kv_heads, splits, kTileThreads, &a, stream);
     if (e != hipSuccess) return fail_hip(e);
     if (splits > 1) {
-      const hipError_t f = launch2(sum_fn(dtype), slots * a.kv_heads, 1, 256, &a, stream);
+      const hipError_t f = launch2(sum_fn(dtype), slots * a.kv_heads, kSumParts, 256, &a, stream);
       if (f != hipSuccess) return fail_hip(f);
     }
   }

@@ -465,8 +465,10 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
 }
 
 // Sums the splits of a key tile's gradients, in their order: the same bits each
-// time.  Bound by memory: 8192 tokens of 8 key/value heads of 128 in up to four
-// splits 41 us, 16384 tokens of two heads in eight 76 us.
+// time.  A tile's rows are shared out over the launch's second axis: by one
+// workgroup each, 8192 tokens of 8 key/value heads of 128 in up to four splits
+// took 41 us, 16384 tokens of two heads in eight 76; by four 29 and 41, by memory's
+// rate.
 template <typename T>
 __global__ __launch_bounds__(256) void k_heads_sum(HeadsArgs a) {
   const int hk = blockIdx.x % a.kv_heads;
@@ -479,10 +481,11 @@ __global__ __launch_bounds__(256) void k_heads_sum(HeadsArgs a) {
   if (count == 1) return;
   const int64_t rows = static_cast<int64_t>(a.tokens_k) * a.kv_heads;
   const int quads = a.d / 4, keys = min(w.lk - first, kTileRows);
-  for (int i = threadIdx.x; i < keys * quads; i += 256) {
+  for (int i = threadIdx.x + 256 * blockIdx.y; i < keys * quads; i += 256 * gridDim.y) {
     const int64_t row = static_cast<int64_t>(w.k0 + first + i / quads) * a.kv_heads + hk;
     const int64_t at = row * a.d + i % quads * 4;
     f32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+#pragma unroll 4
     for (int s = 0; s < count; ++s) {
       const float* p = a.part_o + 2 * static_cast<int64_t>(s) * rows * a.d + at;
       k += *reinterpret_cast<const f32x4*>(p);
