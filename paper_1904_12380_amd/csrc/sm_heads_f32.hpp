@@ -431,7 +431,6 @@ __device__ __forceinline__ void join_row(const HeadsArgs& a, int64_t rows, int64
   const int pair = a.d <= 128 ? lane / 32 : 0, step = a.d <= 128 ? 2 : 1;
   const int col = 4 * (a.d <= 128 ? lane % 32 : lane);
   f32x4 acc = {0, 0, 0, 0};
-#pragma unroll 4
   for (int s = 0; s < count; s += step) {
     const int at = s + pair;
     const float f = __shfl(weight, at);
