@@ -486,3 +486,45 @@ def test_paged_sums_out_of_order_stay_in_bounds(sm):
                                        **case.own)
         torch.cuda.synchronize()
         assert (guard[::2] == 7).all()
+
+
+def test_training_and_serving_steps_in_graphs(sm):
+    """Each replay against the eager calls, with other inputs and eager work in
+    between."""
+    case = Packed(torch, 24, "bf16", self_docs(300, 41, 700), 8, 2, 128, cap=20.0)
+    size, n = 16, 3
+    caches = torch.zeros(2, 64, size, 2, 128, dtype=torch.bfloat16, device="cuda")
+    table = torch.full((n, 16), -1, dtype=torch.int32, device="cuda")
+    free = torch.randperm(64, device="cuda").int()
+    left = torch.tensor([64], dtype=torch.int32, device="cuda")
+    held = torch.tensor([0, 0, 0], dtype=torch.int32, device="cuda")
+    new = torch.tensor([5, 1, 2], dtype=torch.int32, device="cuda")
+    q, k, v = (torch.zeros(8, h, 128, dtype=torch.bfloat16, device="cuda") for h in (8, 2, 2))
+
+    def serve(caches, table, left, held):
+        s = sm.softmax_cache_slots(held, new, table, free, left, 8, size)
+        sm.softmax_cache_append(k, v, caches[0], caches[1], s["slots"])
+        o = sm.softmax_paged_attention_fwd(q, caches[0], caches[1], table, s["cu_q"],
+                                           s["key_lens"])
+        held.copy_(s["key_lens"])
+        left.copy_(s["free_count"])
+        return o
+
+    own = (caches.clone(), table.clone(), left.clone(), held.clone())
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = case.run(sm)
+        o = serve(*own)
+    for seed in range(4):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for t in (q, k, v, *(case.t[name] for name in ("q", "k", "v", "dout"))):
+            t.copy_(torch.randn(t.shape, device="cuda", generator=g))
+        want, served = case.run(sm), serve(caches, table, left, held)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[name], want[name]) for name in want)
+        assert torch.equal(o, served) and torch.equal(own[1], table)
+        assert torch.equal(own[0], caches) and torch.equal(own[3], held)
+    assert held.tolist() == [20, 4, 8]
