@@ -74,11 +74,14 @@ constexpr unsigned kFar = 0x80000000u;  // past every buffer
 // 16 bytes per lane from memory into LDS at `lds` (uniform) + 16 * lane.  In
 // asm, since the compiler holds every later read of LDS back until such a load
 // has landed; the kernels wait for a stage's loads themselves (staged()) and
-// put a barrier between a stage's last read and its next load.
+// put a barrier between a stage's last read and its next load.  Nor does it see
+// what the asm reads: the hardware needs five wait states between a vector
+// instruction's write of a scalar register and a load whose resource holds it, and
+// one after m0's, and checks neither, so they are a part of the asm.
 typedef int s32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void load_lds(s32x4 rsrc, unsigned off, unsigned lds) {
   lds = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
                :
                : "v"(off), "s"(rsrc), "s"(lds)
                : "memory");
