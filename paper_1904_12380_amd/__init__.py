@@ -232,6 +232,23 @@ def _run(fn, device, stream, args):
         return fn(*args, _raw_stream(index) if stream is None else int(stream.cuda_stream))
 
 
+def _empty(shape, dtype, device, stream, returned=True):
+    """Memory for a call on ``stream``: allocated for that stream, so that the
+    allocator does not hand out what earlier work on the current stream still
+    uses.  What the call returns (``returned``) is used on the current stream
+    afterwards: once freed, it is kept until that stream has passed it."""
+    torch = _torch_mod
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream.cuda_stream), device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _check_f32_cuda(t, name: str):
     torch = _torch_mod or _torch()
     if not isinstance(t, torch.Tensor):
@@ -251,12 +268,12 @@ def softmax_fwd_clip_ptr(x_ptr: int, y_ptr: int, rows: int, cols: int, clip_lo: 
                                                stream_handle))
 
 
-def _out_for(x, out):
+def _out_for(x, out, stream):
     _check_f32_cuda(x, "x")
     if x.dim() != 2:
         raise ValueError("x must be 2-D [rows, cols]")
     if out is None:
-        return _torch_mod.empty_like(x)
+        return _empty(x.shape, x.dtype, x.device, stream)
     _check_f32_cuda(out, "out")
     if out.shape != x.shape or out.device != x.device:
         raise ValueError("out must match x in shape and device")
@@ -269,7 +286,7 @@ def softmax_fwd(x, out=None, stream=None):
 
     ``out`` may be ``x`` itself (in place).  Runs on ``stream`` (default: the
     current torch stream) and returns without synchronising."""
-    out = _out_for(x, out)
+    out = _out_for(x, out, stream)
     rows, cols = x.shape
     rc = _run(load_library().softmax_fwd, x.device, stream,
               (x.data_ptr(), out.data_ptr(), rows, cols))
@@ -280,7 +297,7 @@ def softmax_fwd(x, out=None, stream=None):
 
 def softmax_fwd_planned(x, plan: dict, out=None, stream=None):
     """softmax_fwd with a caller-chosen kernel (see softmax_fwd_planned_ptr)."""
-    out = _out_for(x, out)
+    out = _out_for(x, out, stream)
     rows, cols = x.shape
     rc = _run(lambda *a: softmax_fwd_planned_ptr(*a[:4], plan, a[4]), x.device, stream,
               (x.data_ptr(), out.data_ptr(), rows, cols))
@@ -292,7 +309,7 @@ def softmax_fwd_planned(x, plan: dict, out=None, stream=None):
 def softmax_fwd_clip(x, clip_lo: float, out=None, stream=None):
     """softmax_fwd with the clip bound as an argument: any value <= CLIP_MAX,
     or -inf for no clip."""
-    out = _out_for(x, out)
+    out = _out_for(x, out, stream)
     rows, cols = x.shape
     rc = _run(load_library().softmax_fwd_clip, x.device, stream,
               (x.data_ptr(), out.data_ptr(), rows, cols, float(clip_lo)))
@@ -311,7 +328,7 @@ def softmax_fwd_approx_ptr(x_ptr: int, y_ptr: int, rows: int, cols: int, clip_lo
 def softmax_fwd_approx(x, clip_lo: float = CLIP_LO, out=None, stream=None):
     """softmax_fwd_clip with the fast fp32 exponential (looser, stated
     bound: 2e-6 + 1.5e-7 |x - max| relative)."""
-    out = _out_for(x, out)
+    out = _out_for(x, out, stream)
     rows, cols = x.shape
     rc = _run(load_library().softmax_fwd_approx, x.device, stream,
               (x.data_ptr(), out.data_ptr(), rows, cols, float(clip_lo)))
@@ -329,7 +346,7 @@ def softmax_log_fwd_ptr(x_ptr: int, y_ptr: int, rows: int, cols: int, clip_lo: f
 
 def softmax_log_fwd(x, clip_lo: float = CLIP_LO, out=None, stream=None):
     """Row-wise log of the clipped softmax, y = max(x - M, clip_lo) - ln S."""
-    out = _out_for(x, out)
+    out = _out_for(x, out, stream)
     rows, cols = x.shape
     rc = _run(load_library().softmax_log_fwd, x.device, stream,
               (x.data_ptr(), out.data_ptr(), rows, cols, float(clip_lo)))
@@ -360,7 +377,7 @@ def softmax_nll_fwd(x, labels, clip_lo: float = CLIP_LO, out=None, stream=None):
     if labels.shape != (rows,) or labels.device != x.device or not labels.is_contiguous():
         raise ValueError("labels must be contiguous [rows] on x's device")
     if out is None:
-        out = torch.empty(rows, dtype=torch.float32, device=x.device)
+        out = _empty(rows, torch.float32, x.device, stream)
     else:
         _check_f32_cuda(out, "out")
         if out.shape != (rows,) or out.device != x.device:
@@ -398,7 +415,7 @@ def softmax_attention_fwd(q, k, v, scale=None, clip_lo: float = CLIP_LO, out=Non
     if scale is None:
         scale = ctypes.c_float(1.0 / max(d, 1) ** 0.5).value
     if out is None:
-        out = torch.empty((b, lq, dv), dtype=torch.float32, device=q.device)
+        out = _empty((b, lq, dv), torch.float32, q.device, stream)
     else:
         _check_f32_cuda(out, "out")
         if tuple(out.shape) != (b, lq, dv):
@@ -427,7 +444,7 @@ def softmax_exp_probe(x, m, out=None, stream=None, clip_lo: float = CLIP_LO,
         if m.shape != x.shape:
             raise ValueError("m must match x")
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty(x.shape, x.dtype, x.device, stream)
     _check_f32_cuda(out, "out")
     rc = _run(load_library().softmax_exp_probe, x.device, stream,
               (x.data_ptr(), None if m is None else m.data_ptr(), out.data_ptr(), x.numel(),
@@ -442,7 +459,7 @@ def softmax_copy_probe(x, out=None, stream=None):
     torch = _torch()
     _check_f32_cuda(x, "x")
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty(x.shape, x.dtype, x.device, stream)
     _check_f32_cuda(out, "out")
     if out.numel() != x.numel():
         raise ValueError("out must have as many elements as x")

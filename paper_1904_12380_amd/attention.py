@@ -141,10 +141,9 @@ def _score(q, docs, causal, scale, cap, slopes, prefix) -> _Score:
         None if prefix is None else _vector(prefix, "prefix", torch.int32, docs, q.device))
 
 
-def _output(out, shape, dtype, device, name):
-    torch = _sm._torch_mod
+def _output(out, shape, dtype, device, name, stream):
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _sm._empty(shape, dtype, device, stream)
     _tensor(out, name, len(shape))
     if out.dtype != dtype or tuple(out.shape) != tuple(shape) or out.device != device or \
             not out.is_contiguous():
@@ -187,8 +186,8 @@ def softmax_packed_attention_fwd(q, k, v, cu_q, cu_k=None, *, causal=True, scale
     if cu_k is None and k.shape[0] != q.shape[0]:
         raise ValueError("k must have q's tokens unless cu_k is given")
     score = _score(q, docs, causal, scale, cap, slopes, prefix)
-    out = _output(out, q.shape, q.dtype, q.device, "out")
-    lse = _output(lse, q.shape[:2], _sm._torch_mod.float32, q.device, "lse")
+    out = _output(out, q.shape, q.dtype, q.device, "out", stream)
+    lse = _output(lse, q.shape[:2], _sm._torch_mod.float32, q.device, "lse", stream)
     _checked(_sm._run(fn, q.device, stream, (aq, ak, av, out.data_ptr(), lse.data_ptr(), pq, pk,
                                              docs, score, _dtypes[q.dtype])),
              "softmax_packed_attention_fwd")
@@ -212,26 +211,18 @@ def softmax_packed_attention_bwd(dout, q, k, v, o, lse, cu_q, cu_k=None, *, caus
     if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or \
             lse.device != q.device:
         raise ValueError("lse must be contiguous float32 [tokens, heads]")
-    dq = _output(dq, q.shape, q.dtype, q.device, "dq")
-    dk = _output(dk, k.shape, q.dtype, q.device, "dk")
-    dv = _output(dv, v.shape, q.dtype, q.device, "dv")
+    dq = _output(dq, q.shape, q.dtype, q.device, "dq", stream)
+    dk = _output(dk, k.shape, q.dtype, q.device, "dk", stream)
+    dv = _output(dv, v.shape, q.dtype, q.device, "dv", stream)
     room = _fns.softmax_packed_attention_bwd_workspace(aq.tokens, ak.tokens, aq.heads, ak.heads,
                                                        aq.d, _dtypes[q.dtype])
-    work = torch.empty(max(room, 0), dtype=torch.uint8, device=q.device)
-    _on_stream(work, stream)
+    work = _sm._empty(max(room, 0), torch.uint8, q.device, stream, returned=False)
     _checked(_sm._run(fn, q.device, stream,
                       (ad, aq, ak, av, ao, lse.data_ptr(), dq.data_ptr(), dk.data_ptr(),
                        dv.data_ptr(), pq, pk, docs, score, _dtypes[q.dtype], work.data_ptr(),
                        room)),
              "softmax_packed_attention_bwd")
     return dq, dk, dv
-
-
-def _on_stream(work, stream) -> None:
-    """A workspace of this call's own, used on another stream than the one
-    that it was allocated for, is kept until that stream has passed it."""
-    if stream is not None:
-        work.record_stream(stream)
 
 
 def _fits(t) -> bool:
@@ -300,14 +291,12 @@ def softmax_paged_attention_fwd(q, k_cache, v_cache, block_table, cu_q, key_lens
     pq = _vector(cu_q, "cu_q", torch.int32, requests + 1, device)
     pk = _vector(key_lens, "key_lens", torch.int32, requests, device)
     score = _score(q, requests, causal, scale, cap, slopes, prefix)
-    out = _output(out, q.shape, q.dtype, device, "out")
+    out = _output(out, q.shape, q.dtype, device, "out", stream)
     if lse is not None:
-        lse = _output(lse, q.shape[:2], torch.float32, device, "lse")
+        lse = _output(lse, q.shape[:2], torch.float32, device, "lse", stream)
     room = _fns.softmax_paged_attention_workspace(aq.tokens, aq.heads, ak.heads, aq.d, requests,
                                                   width * ak.block_size)
-    work = torch.empty(room, dtype=torch.uint8, device=device) if room > 0 else None
-    if work is not None:
-        _on_stream(work, stream)
+    work = _sm._empty(room, torch.uint8, device, stream, returned=False) if room > 0 else None
     _checked(_sm._run(fn, device, stream,
                       (aq, ak, av, block_table.data_ptr(), width, pq, pk, requests, score,
                        _dtypes[q.dtype], out.data_ptr(), None if lse is None else lse.data_ptr(),
@@ -342,8 +331,8 @@ def softmax_cache_slots(context_lens, new_lens, block_table, free_blocks, free_c
     new = _vector(new_lens, "new_lens", i32, n, device)
     free = _vector(free_blocks, "free_blocks", i32, None, device)
     count = _vector(free_count, "free_count", i32, 1, device)
-    slots = torch.empty(total, dtype=torch.int64, device=device)
-    sums = torch.empty(2 * n + 3, dtype=i32, device=device)
+    slots = _sm._empty(total, torch.int64, device, stream)
+    sums = _sm._empty(2 * n + 3, i32, device, stream)
     at = sums.data_ptr()
     _checked(_sm._run(fn, device, stream,
                       (context, new, n, block_table.data_ptr(), width, free, len(free_blocks),
