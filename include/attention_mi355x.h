@@ -30,7 +30,9 @@
  * products on the matrix cores (in two parts, which keep 16 bits or more, where
  * one weight's rounding is not averaged over many: the first 64 keys of rows
  * that see at most 128, and in the gradients any block with a weight above
- * 1/8).  Results are bitwise deterministic.
+ * 1/8).  In the gradients of fp16 weights and score gradients are scaled into the
+ * type's range before they are rounded, and back in the sums.  Results are
+ * bitwise deterministic.
  *
  * Layout: a tensor [tokens, heads, d] has its d entries contiguous; strides
  * between tokens and heads are in elements and not negative.  d is a

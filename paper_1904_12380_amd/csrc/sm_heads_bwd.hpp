@@ -9,7 +9,7 @@
 // would take, but every sum has one owner: no atomics, the same bits each time.
 //
 // The first kernel writes what the second needs of every row as a pair (-lse
-// / c, -D), head by head, so that the second reads it by tokens: the values
+// / c, -D) (fp16: with its lift of the weights, below), head by head, so that the second reads it by tokens: the values
 // that its scores and dP start from, so that the shift and the difference cost
 // no instruction.
 #pragma once
@@ -26,12 +26,62 @@ namespace smx {
 // their own rounding to 16 bits.
 constexpr float kLargeWeight = 0.125f;
 
-__device__ __forceinline__ bool any_large(const f32x16& p) {
+__device__ __forceinline__ bool any_large(const f32x16& p, float large) {
   float top = p[0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) top = fmaxf(top, p[i]);
-  return __any(top > kLargeWeight);
+  return __any(top > large);
 }
+
+// What is rounded to fp16 for a product is put into its range first, and its sums
+// are taken back when they are stored; bf16 has the range of fp32 and needs
+// neither.
+//
+// Weights for dV are at most 1 but for their scores' rounding, and a key that
+// many rows see little of sums up many small ones: they are formed 2^kWeightLift
+// times as large, in the exponent's argument, with 11 bits down to 2^-26.
+template <typename T>
+constexpr int kWeightLift = __is_same(T, f16) ? 12 : 0;
+
+// Score gradients are of any size, with that of dO.  A lane pair's own (one row
+// of dQ, one key of dK) are taken times a power of two, lowered when a value
+// would pass 2^15, to leave it below 2^9, so that few blocks lower it; the sums so
+// far go with it.  A value then loses bits to fp16's denormal numbers only where it
+// is 2^22 times smaller than one that the sum already has.
+template <typename T>
+struct FitRange {
+  template <int N>
+  __device__ __forceinline__ void fit(f32x16&, f32x16 (&)[N]) {}
+  __device__ __forceinline__ float back() const { return 1.0f; }
+};
+template <>
+struct FitRange<f16> {
+  float f = 0x1p100f;  // fp16's smallest dO, V and weights leave more than 2^-80
+
+  // x is multiplied by f; acc holds sums of earlier such x.
+  template <int N>
+  __device__ __forceinline__ void fit(f32x16& x, f32x16 (&acc)[N]) {
+    float top = fabsf(x[0]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+    top = fmaxf(top, half32_partner(top));
+    if (__any(top * f > 0x1p15f)) {
+      // 2^8 <= top * next < 2^9, from top's exponent.
+      const int now = __builtin_bit_cast(int, f);
+      const int next = top * f > 0x1p15f
+                           ? (127 + 127 + 8 - (__builtin_bit_cast(int, top) >> 23)) << 23 : now;
+      const float ratio = __builtin_bit_cast(float, max(next - now + (127 << 23), 0));
+#pragma unroll
+      for (int t = 0; t < N; ++t) acc[t] *= ratio;
+      f = __builtin_bit_cast(float, next);
+    }
+    x *= f;
+  }
+  // 1 / f.
+  __device__ __forceinline__ float back() const {
+    return __builtin_bit_cast(float, (254 << 23) - __builtin_bit_cast(int, f));
+  }
+};
 
 template <typename T, int DP>
 __device__ __forceinline__ f32x16 rows_dot(const TileReader<DP>& rd, const char SMX_LDS* tile,
@@ -72,10 +122,10 @@ __device__ __forceinline__ void cols_accumulate(const TileReader<DP>& rd,
   }
 }
 
-// The lane's row, of fp32 sums.
+// The lane's row, of fp32 sums, times f.
 template <int DP>
 __device__ __forceinline__ void store_sums(float* p, int d, int half,
-                                           const f32x16 (&acc)[DP / 32]) {
+                                           const f32x16 (&acc)[DP / 32], float f) {
 #pragma unroll
   for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
@@ -83,7 +133,7 @@ __device__ __forceinline__ void store_sums(float* p, int d, int half,
       const int col = 32 * t + 8 * i + 4 * half;
       f32x4 x;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = acc[t][4 * i + j];
+      for (int j = 0; j < 4; ++j) x[j] = acc[t][4 * i + j] * f;
       if (col < d) *reinterpret_cast<f32x4*>(p + col) = x;
     }
 }
@@ -155,6 +205,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
     for (int i = 0; i < DP / 16; ++i) q[i] = -q[i];
   }
   f32x16 acc[DP / 32] = {};
+  FitRange<T> range;
   // The sum of P (dP - D), which D's error alone keeps from 0 (the weights sum
   // to 1): what the gradients of the keys correct it by.
   float rest[2] = {0.0f, 0.0f};
@@ -212,23 +263,24 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
       f32x16 s = rows_dot<T, DP>(rd, kt, 32 * h, q), cap;
       f32x16 dp = rows_dot<T, DP>(rd, vt, 32 * h, dout);
       weights(s, cap, k0 + 32 * h);
-      const bool two_parts = any_large(s);
+      const bool two_parts = any_large(s, kLargeWeight);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         dp[i] = s[i] * (dp[i] - delta);
         rest[i % 2] += dp[i];
         if constexpr (MODE >= kCap) dp[i] *= sc.derivative(cap[i]);
       }
+      range.fit(dp, acc);
       cols_accumulate<T, DP>(rd, kt, 32 * h, dp, two_parts, acc);
     }
   }
   delta += (rest[0] + rest[1]) + half32_partner(rest[0] + rest[1]);
   if (valid && half == 0)
     reinterpret_cast<float2*>(a.delta)[static_cast<int64_t>(head) * a.tokens_q + token] =
-        make_float2(-lse2 / c, -delta);
+        make_float2((kWeightLift<T> - lse2) / c, -delta);
   __syncthreads();
-  store_rows<T, DP>(lds + wave * 32 * DP * 2, acc, a.scale, static_cast<T*>(a.out),
-                    valid ? static_cast<int>(out) : -1, a.d);
+  store_rows<T, DP>(lds + wave * 32 * DP * 2, acc, a.scale * range.back(),
+                    static_cast<T*>(a.out), valid ? static_cast<int>(out) : -1, a.d);
 }
 
 // The turns of a key tile: 32 tokens of one head each, head by head, each from
@@ -343,6 +395,8 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
     for (int i = 0; i < DP / 16; ++i) k[i] = -k[i];
   }
   f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
+  FitRange<T> range;
+  constexpr float kLift = 1 << kWeightLift<T>, kLower = 1.0f / kLift;
 
   const TileReader<DP> reader;
   constexpr int kTile = kTurnRows * DP * 2;
@@ -436,13 +490,14 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
           if (key >= keys_seen(a, w, tok)) s[i] = 0.0f;
         }
       }
-      const bool two_parts = any_large(s);
+      const bool two_parts = any_large(s, kLargeWeight * kLift);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         dp[i] *= s[i];
         if constexpr (MODE >= kCap) dp[i] *= Scoring<MODE>::derivative(cap[i]);
       }
       cols_accumulate<T, DP>(rd, ot, 0, s, two_parts, dv);
+      range.fit(dp, dk);
       cols_accumulate<T, DP>(rd, qt, 0, dp, two_parts, dk);
     }
     write_stats(buf ^ 1);
@@ -452,16 +507,18 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
     if (!valid) return;
     const int64_t rows = static_cast<int64_t>(a.tokens_k) * a.kv_heads;
     float* p = a.part_o + ((2 * static_cast<int64_t>(blockIdx.y)) * rows + row) * a.d;
-    store_sums<DP>(p, a.d, half, dk);
-    store_sums<DP>(p + rows * a.d, a.d, half, dv);
+    store_sums<DP>(p, a.d, half, dk, range.back() * kLower);
+    store_sums<DP>(p + rows * a.d, a.d, half, dv, kLower);
     return;
   }
   // The wavefront's own V has landed (also without a turn) and been read: its
   // place turns the rows.
   staged();
   const int index = valid ? static_cast<int>(row) : -1;
-  store_rows<T, DP>(lds + 32 * wave * DP * 2, dk, a.scale, static_cast<T*>(a.dk), index, a.d);
-  store_rows<T, DP>(lds + 32 * wave * DP * 2, dv, 1.0f, static_cast<T*>(a.dv), index, a.d);
+  store_rows<T, DP>(lds + 32 * wave * DP * 2, dk, a.scale * range.back() * kLower,
+                    static_cast<T*>(a.dk), index, a.d);
+  store_rows<T, DP>(lds + 32 * wave * DP * 2, dv, kLower, static_cast<T*>(a.dv), index,
+                    a.d);
 }
 
 // Sums the splits of a key tile's gradients, in their order: the same bits each
