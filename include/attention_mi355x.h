@@ -28,10 +28,10 @@
  * lse and slopes are fp32.  Sums, statistics and gradients accumulate in
  * fp32; with 16-bit types the weights are rounded to the type for the
  * products on the matrix cores (in two parts, which keep 16 bits or more, where
- * one weight's rounding is not averaged over many: the first 64 keys of rows
- * that see at most 128, and in the gradients any block with a weight above
- * 1/8).  In the gradients of fp16 weights and score gradients are scaled into the
- * type's range before they are rounded, and back in the sums.  Results are
+ * one weight's rounding is not averaged over many: in the forward pass the first
+ * 64 keys of rows that see at most 128, in the gradients any block with a weight
+ * above 1/8).  In the gradients of fp16 weights and score gradients are scaled
+ * into the type's range before they are rounded, and back in the sums.  Results are
  * bitwise deterministic.
  *
  * Layout: a tensor [tokens, heads, d] has its d entries contiguous; strides

@@ -469,8 +469,10 @@ struct Scoring {
 // that products with the scale stay ordered.
 constexpr float kUnseen = -3.0e38f;
 
-// Weights are taken in two 16-bit parts for the first 64 keys of a document
-// where rows see at most this many keys.
+// Weights are taken in two 16-bit parts for the first kTileKeys keys of a
+// document (in tiles of up to 32 rows these are two wavefronts' first) where rows
+// see at most this many keys.  The rule goes by place, not by weight: past it a
+// weight is rounded to the type once, whatever its share of the row.
 constexpr int kTwoPartKeys = 128;
 
 // A running maximum is moved (and the sums rescaled) when a score passes it by
@@ -562,7 +564,7 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
   interleave<2 * KT * DP / 32, 2>();
   // A document's first keys: what the weights' rounding left, where rows see
   // few keys to average it.
-  if (k0 == 0 && w.lim_all <= kTwoPartKeys) {
+  if (k0 < kTileKeys && w.lim_all <= kTwoPartKeys) {
 #pragma unroll
     for (int u = 0; u < 2 * KT; ++u) p[u] = pack8_rest<T>(s[u / 2], 8 * (u % 2), p[u]);
 #pragma unroll
