@@ -396,7 +396,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
   }
   f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
   FitRange<T> range;
-  constexpr float kLift = 1 << kWeightLift<T>, kLower = 1.0f / kLift;
+  constexpr float kRaise = 1 << kWeightLift<T>, kLower = 1.0f / kRaise;
 
   const TileReader<DP> reader;
   constexpr int kTile = kTurnRows * DP * 2;
@@ -490,7 +490,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(H
           if (key >= keys_seen(a, w, tok)) s[i] = 0.0f;
         }
       }
-      const bool two_parts = any_large(s, kLargeWeight * kLift);
+      const bool two_parts = any_large(s, kLargeWeight * kRaise);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         dp[i] *= s[i];

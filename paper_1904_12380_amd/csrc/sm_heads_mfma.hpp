@@ -476,9 +476,15 @@ constexpr float kUnseen = -3.0e38f;
 constexpr int kTwoPartKeys = 128;
 
 // A running maximum is moved (and the sums rescaled) when a score passes it by
-// this many powers of two: weights then stay below 2^8, and most tiles
-// rescale nothing.
-constexpr float kSlack = 8.0f;
+// kSlack powers of two: weights then stay below 2^kSlack, and most tiles rescale
+// nothing.  For fp16 all weights and their sum are 2^kLift times as large, which
+// puts its range around them: below 2^15.5, with 11 bits down to 2^-26 of the
+// maximum's weight.  Thousands of keys of 2^-24 and less beside a large one would
+// otherwise be rounded to denormal numbers or to 0.
+template <typename T>
+constexpr float kSlack = __is_same(T, f16) ? 3.5f : 8.0f;
+template <typename T>
+constexpr float kLift = __is_same(T, f16) ? 12.0f : 0.0f;
 
 // One wavefront's state for 32 rows, a lane's row at l % 32.
 template <typename T, int DP>
@@ -533,7 +539,7 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kt][i]);
   top = fmaxf(top, half32_partner(top));
-  if (__any((top - w.m) * w.c > kSlack)) {
+  if (__any((top - w.m) * w.c > kSlack<T>)) {
     const float next = fmaxf(top, w.m);
     const float alpha = __builtin_amdgcn_exp2f((w.m - next) * w.c);
     w.m = next;
@@ -541,7 +547,7 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) w.acc[t] *= alpha;
   }
-  const float shift = w.m > kUnseen ? -w.m * w.c : 0.0f;
+  const float shift = w.m > kUnseen ? kLift<T> - w.m * w.c : 0.0f;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     float part[2] = {0.0f, 0.0f};
@@ -824,7 +830,8 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
     if (!valid) return;
     const int64_t at = split * static_cast<int64_t>(a.tokens_q) * a.heads + out;
     if (writes_stats)
-      a.part_stat[at] = {some ? m * st.c * kLn2F : -INFINITY, l, split_count(seen, chunk), 0};
+      a.part_stat[at] = {some ? (m * st.c - kLift<T>) * kLn2F : -INFINITY, l,
+                         split_count(seen, chunk), 0};
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
@@ -841,7 +848,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
   }
   const float inv = some ? 1.0f / l : 0.0f;
   if (writes_stats && a.lse != nullptr)
-    a.lse[out] = some ? (m * st.c + __builtin_amdgcn_logf(l)) * kLn2F : -INFINITY;
+    a.lse[out] = some ? (m * st.c + (__builtin_amdgcn_logf(l) - kLift<T>)) * kLn2F : -INFINITY;
   if (!few) {
     __syncthreads();  // the last tile has been read: its place turns the rows
     store_rows<T, DP>(lds + wave * 32 * kRowBytes, st.acc, inv, static_cast<T*>(a.out),

@@ -87,3 +87,28 @@ def test_values_of_keys_that_all_rows_see_little_of(sm):
     got, want = case.run(sm)["dv"][-1].double().cpu().numpy(), case.oracle()["dv"][-1]
     # 2^-11 of the sum, its own denormal step, and the fp32 sum of 32768 terms
     assert np.abs(got - want).max() <= 2.0 ** -10 * np.abs(want).max() + 2.0 ** -25
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows", [1, 40, 130])
+@pytest.mark.parametrize("gap", [9.0, 14.0, 17.5])
+def test_many_keys_of_small_weight_beside_a_large_one(sm, dtype, rows, gap):
+    """One key holds most of each row's weight, thousands of others e^-gap of it
+    each: together they move the result by many times its rounding."""
+    keys, d = 60000, 64
+    case = Packed(torch, 54, dtype, [(rows, keys)], 1, 1, d, causal=False, scale=1.0)
+    case.t["q"][:] = 0.0
+    case.t["k"][:] = 0.0
+    case.t["q"][..., 0] = 1.0
+    case.t["k"][..., 0] = -gap
+    case.t["k"][7, :, 0] = 0.0
+    case.t["v"] += 1.0
+    case.t["v"][7] = 0.0
+    for name in ("q", "k", "v"):
+        case.f[name] = case.t[name].double().cpu().numpy()
+    got = case.run(sm, train=False)["o"].double().cpu().numpy()
+    want = case.oracle(train=False)["o"]
+    # the weight's and the output's rounding, and the fp32 sum of the keys: 938
+    # steps of 64, each off by at most 2^-24 of the sum
+    u = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
+    assert np.abs(got - want).max() <= (2.0 * u + 2.0 ** -14) * np.abs(want).max()
