@@ -108,9 +108,9 @@ typedef struct softmax_score_t {
  * may not overlap the inputs.  tokens_q * heads and tokens_k * heads are below
  * 2^31, tokens_k at most 2^30.
  *
- * NaN and infinity stay in their document: in q they reach their own row, in
- * k and v any row of the document (also of one that does not see the key, when
- * both lie in one tile).
+ * NaN and infinity stay in their document: in q they reach their own row's o and
+ * lse, in k and v any row of the document (also of one that does not see the key,
+ * when both lie in one tile).
  */
 SOFTMAX_API int softmax_packed_attention_fwd(const softmax_heads_t* q, const softmax_heads_t* k,
                                              const softmax_heads_t* v, void* o, float* lse,

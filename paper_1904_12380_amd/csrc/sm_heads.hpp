@@ -257,6 +257,10 @@ __device__ __forceinline__ int64_t paged_row(const HeadsArgs& a, int b, int j, i
   return id * bs + (j & ((1 << a.log_block) - 1)) * ts;
 }
 
+// lse of a row without a maximum, from its sum: it sees no key (0), or all of its
+// scores are NaN and the sum with them.
+__device__ __forceinline__ float lse_of_none(float l) { return l == 0.0f ? -INFINITY : l; }
+
 __device__ __forceinline__ float group4_max(float v) {  // over lanes l % 16
   v = fmaxf(v, row16_partner(v));
   return fmaxf(v, half32_partner(v));

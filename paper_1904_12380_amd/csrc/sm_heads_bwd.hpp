@@ -9,9 +9,9 @@
 // would take, but every sum has one owner: no atomics, the same bits each time.
 //
 // The first kernel writes what the second needs of every row as a pair (-lse
-// / c, -D) (fp16: with its lift of the weights, below), head by head, so that the second reads it by tokens: the values
-// that its scores and dP start from, so that the shift and the difference cost
-// no instruction.
+// / c, -D) (fp16: with the lift of the weights, below), head by head, so that the
+// second reads it by tokens: the values that its scores and dP start from, so that
+// the shift and the difference cost no instruction.
 #pragma once
 
 #include "sm_heads_f32.hpp"

@@ -233,7 +233,7 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
   }
   const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
   if (g == 0 && a.lse != nullptr)
-    a.lse[out] = m == -INFINITY ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2F;
+    a.lse[out] = m == -INFINITY ? lse_of_none(l) : m + __builtin_amdgcn_logf(l) * kLn2F;
 #pragma unroll
   for (int t = 0; t < DP / 16; ++t)
     if (16 * t + 4 * g < a.d)
@@ -442,7 +442,7 @@ __device__ __forceinline__ void join_row(const HeadsArgs& a, int64_t rows, int64
     for (int j = 0; j < 4; ++j) acc[j] += half32_partner(acc[j]);
   const float inv = m == -INFINITY ? 0.0f : 1.0f / l;
   if (lane == 0 && a.lse != nullptr)
-    a.lse[row] = m == -INFINITY ? -INFINITY : m + __builtin_amdgcn_logf(l) * kLn2F;
+    a.lse[row] = m == -INFINITY ? lse_of_none(l) : m + __builtin_amdgcn_logf(l) * kLn2F;
   if (pair == 0 && col < a.d) store4(static_cast<T*>(a.out) + row * a.d + col, acc * inv);
 }
 

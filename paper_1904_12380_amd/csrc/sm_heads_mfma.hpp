@@ -848,7 +848,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(H
   }
   const float inv = some ? 1.0f / l : 0.0f;
   if (writes_stats && a.lse != nullptr)
-    a.lse[out] = some ? (m * st.c + (__builtin_amdgcn_logf(l) - kLift<T>)) * kLn2F : -INFINITY;
+    a.lse[out] = some ? (m * st.c + (__builtin_amdgcn_logf(l) - kLift<T>)) * kLn2F : lse_of_none(l);
   if (!few) {
     __syncthreads();  // the last tile has been read: its place turns the rows
     store_rows<T, DP>(lds + wave * 32 * kRowBytes, st.acc, inv, static_cast<T*>(a.out),
