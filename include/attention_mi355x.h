@@ -39,6 +39,10 @@
  * multiple of 8 up to SOFTMAX_HEADS_MAX_DIM; the data and all strides are
  * multiples of 16 bytes.
  *
+ * Sizes: tokens * heads is below 2^31, and a launch has fewer than 2^24
+ * workgroups: with T = 128 (fp32: 64), (tokens * heads / kv_heads / T + documents
+ * + 1) * kv_heads < 2^24.
+ *
  * Device data is not trusted for addressing: sums outside [0, tokens] are
  * clamped to it, and block ids outside the cache hold no keys.
  */
@@ -105,8 +109,8 @@ typedef struct softmax_score_t {
  *   cu_q, cu_k device, [docs + 1] int32, ascending from 0
  *
  * Tokens past the last document get o = 0 and lse = -infinity.  o and lse
- * may not overlap the inputs.  tokens_q * heads and tokens_k * heads are below
- * 2^31, tokens_k at most 2^30.
+ * may not overlap the inputs.  tokens_k is at most 2^30, and its product with heads
+ * is bounded like that of tokens_q.
  *
  * NaN and infinity stay in their document: in q they reach their own row's o and
  * lse, in k and v any row of the document (also of one that does not see the key,

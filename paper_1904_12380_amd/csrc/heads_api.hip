@@ -39,11 +39,21 @@ void set_shape(HeadsArgs* a, int64_t tokens_q, int64_t tokens_k, int64_t heads, 
   a->exp_cap = s->cap > 0.0f ? 2.0f * kLog2eF / s->cap : 0.0f;
 }
 
-// Sizes that a call's index arithmetic holds.
-bool sizes_ok(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t docs) {
-  return kv_heads > 0 && heads % kv_heads == 0 && docs >= 0 && docs < INT32_MAX / 4 &&
+// Rows (keys) of a workgroup's tile: the kernels' kF32Rows and kTileRows, with
+// kF32Threads = kTileThreads threads.
+int tile_rows(int dtype) { return dtype == SOFTMAX_F32 ? kF32Rows : kTileRows; }
+static_assert(kF32Threads == kTileThreads, "one launch shape");
+
+// Workgroups of kTileThreads threads along a launch's first axis, whose threads
+// have to stay below 2^32.
+constexpr int64_t kMaxTiles = (int64_t(1) << 32) / kTileThreads - 1;
+
+// Sizes that a call's index arithmetic and its launches, for tiles of `tile` rows,
+// hold.
+bool sizes_ok(int64_t tokens, int64_t heads, int64_t kv_heads, int64_t docs, int tile) {
+  return kv_heads > 0 && heads % kv_heads == 0 && docs >= 0 && docs <= kMaxTiles &&
          tokens <= INT32_MAX / std::max<int64_t>(heads, 1) &&
-         tile_slots(tokens * heads / kv_heads, docs, 16) <= INT32_MAX / kv_heads;
+         tile_slots(tokens * heads / kv_heads, docs, tile) <= kMaxTiles / kv_heads;
 }
 
 hipError_t launch2(const void* fn, int64_t x, int64_t y, int block, HeadsArgs* a, hipStream_t s) {
@@ -99,11 +109,6 @@ const void* join_fn(int dtype) {
 const void* sum_fn(int dtype) {
   return dtype == SOFTMAX_F16 ? SMX_FN(k_heads_sum<f16>) : SMX_FN(k_heads_sum<bf16>);
 }
-
-// Rows (keys) of a workgroup's tile: the kernels' kF32Rows and kTileRows, with
-// kF32Threads = kTileThreads threads.
-int tile_rows(int dtype) { return dtype == SOFTMAX_F32 ? kF32Rows : kTileRows; }
-static_assert(kF32Threads == kTileThreads, "one launch shape");
 
 // Splits of the keys to launch: enough that the call's tiles fill `target`
 // workgroups, no more than the longest request has chunks of, at most 64.
@@ -193,8 +198,8 @@ SOFTMAX_API int softmax_packed_attention_fwd(const softmax_heads_t* q, const sof
       !heads_ok(v, size, &vb))
     return SOFTMAX_ERR_INVALID_ARG;
   if (k->tokens != v->tokens || k->heads != v->heads || k->d != v->d || q->d != k->d ||
-      !sizes_ok(q->tokens, q->heads, k->heads, docs) ||
-      !sizes_ok(k->tokens, q->heads, k->heads, docs) || !aligned16(o))
+      !sizes_ok(q->tokens, q->heads, k->heads, docs, tile_rows(dtype)) ||
+      !sizes_ok(k->tokens, q->heads, k->heads, docs, tile_rows(dtype)) || !aligned16(o))
     return SOFTMAX_ERR_INVALID_ARG;
   if (qb == 0) return SOFTMAX_OK;
   const int64_t rows = q->tokens * q->heads;
@@ -227,8 +232,8 @@ SOFTMAX_API int64_t softmax_packed_attention_bwd_workspace(int64_t tokens_q, int
                                                            int64_t heads, int64_t kv_heads,
                                                            int64_t d, int dtype) {
   if (tokens_q < 0 || tokens_k < 0 || heads < 0 || d < 8 || d > SOFTMAX_HEADS_MAX_DIM ||
-      dtype_size(dtype) == 0 || !sizes_ok(tokens_q, heads, kv_heads, 0) ||
-      !sizes_ok(tokens_k, heads, kv_heads, 0))
+      dtype_size(dtype) == 0 || !sizes_ok(tokens_q, heads, kv_heads, 0, tile_rows(dtype)) ||
+      !sizes_ok(tokens_k, heads, kv_heads, 0, tile_rows(dtype)))
     return -1;
   return stat_bytes(tokens_q, heads) +
          part_bytes(key_splits(tokens_q, tokens_k, heads, kv_heads, dtype), tokens_k, kv_heads, d);
@@ -250,9 +255,9 @@ SOFTMAX_API int softmax_packed_attention_bwd(const softmax_heads_t* dout,
   if (k->tokens != v->tokens || k->heads != v->heads || k->d != v->d || q->d != k->d ||
       o->tokens != q->tokens || o->heads != q->heads || o->d != q->d ||
       dout->tokens != q->tokens || dout->heads != q->heads || dout->d != q->d ||
-      !sizes_ok(q->tokens, q->heads, k->heads, docs) ||
-      !sizes_ok(k->tokens, q->heads, k->heads, docs) || !aligned16(dq) || !aligned16(dk) ||
-      !aligned16(dv) || !aligned16(workspace))
+      !sizes_ok(q->tokens, q->heads, k->heads, docs, tile_rows(dtype)) ||
+      !sizes_ok(k->tokens, q->heads, k->heads, docs, tile_rows(dtype)) || !aligned16(dq) ||
+      !aligned16(dk) || !aligned16(dv) || !aligned16(workspace))
     return SOFTMAX_ERR_INVALID_ARG;
   const int64_t rows = q->tokens * q->heads, krows = k->tokens * k->heads;
   const int64_t splits = key_splits(q->tokens, k->tokens, q->heads, k->heads, dtype);
@@ -316,7 +321,7 @@ SOFTMAX_API int64_t softmax_paged_attention_workspace(int64_t tokens, int64_t he
                                                       int64_t kv_heads, int64_t d,
                                                       int64_t requests, int64_t max_keys) {
   if (tokens < 0 || heads < 0 || d < 8 || d > SOFTMAX_HEADS_MAX_DIM || max_keys < 0 ||
-      !sizes_ok(tokens, heads, kv_heads, requests))
+      !sizes_ok(tokens, heads, kv_heads, requests, kTileRows))
     return -1;
   int64_t cus = 0;
   if (current_cus(&cus) != SOFTMAX_OK) return -1;
@@ -336,7 +341,7 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
   if (size == 0 || !score_ok(score) || !heads_ok(q, size, &qb) || !cache_ok(k, size, &kb) ||
       !cache_ok(v, size, &vb) || !same_cache(k, v) || q->d != k->d || table_width < 0 ||
       table_width > kMaxTokens / k->block_size ||
-      !sizes_ok(q->tokens, q->heads, k->heads, requests) || !aligned16(o) ||
+      !sizes_ok(q->tokens, q->heads, k->heads, requests, tile_rows(dtype)) || !aligned16(o) ||
       !aligned16(workspace))
     return SOFTMAX_ERR_INVALID_ARG;
   if (qb == 0) return SOFTMAX_OK;
