@@ -212,8 +212,9 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
  *   missing      [1] int32; written: blocks that were needed but not had.
  *                Their entries are -1 where the table has them
  *
- * Negative lengths count as 0; sums are meant to stay below 2^31.  Written
- * arrays may not overlap each other or the inputs, except that the table is
+ * Negative lengths count as 0; sums are meant to stay below 2^31 (past it cu_q,
+ * key_lens and missing are not specified).  The work of a call goes by the sizes
+ * of its arrays, whatever the lengths.  Written arrays may not overlap each other or the inputs, except that the table is
  * both.  At most SOFTMAX_CACHE_MAX_REQUESTS requests.
  */
 #define SOFTMAX_CACHE_MAX_REQUESTS 65536

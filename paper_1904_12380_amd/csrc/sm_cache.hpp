@@ -50,7 +50,10 @@ __device__ __forceinline__ SlotRequest slot_request(const SlotArgs& a, int b) {
 // search over the threads' sums in LDS and a walk over that thread's
 // requests.  The token at a block's first row writes the block's table entry:
 // every new block starts with a new token, so each entry has one writer, and
-// entries that are read (blocks held before) are never written.
+// entries that are read (blocks held before) are never written.  Where there are
+// more tokens than slots to write, the entries are shared out by themselves: the
+// turns are then bounded by the outputs' sizes, not by lengths that the device's
+// data holds.
 // Bound by latency: 8 requests of one token 3.6 us, 2048 of up to 320 (65536
 // tokens) 8.9 us, of a call of 11.4 and 12.2.
 __global__ __launch_bounds__(kSlotThreads) void k_cache_slots(SlotArgs a) {
@@ -107,21 +110,26 @@ __global__ __launch_bounds__(kSlotThreads) void k_cache_slots(SlotArgs a) {
     }
   }
   __syncthreads();
-  const int64_t stop = max(all[0], a.total);
-  for (int64_t t = static_cast<int64_t>(blockIdx.x) * kSlotThreads + tid; t < stop;
-       t += static_cast<int64_t>(gridDim.x) * kSlotThreads) {
+  // The last thread whose sum is at most x.  Threads without tokens (or blocks)
+  // share their sum with the next that has some: the last of them holds x.
+  auto holder = [](const int64_t* before, int64_t x) {
+    int lo = 0, hi = kSlotThreads - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (before[mid] <= x)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    return lo;
+  };
+  const int64_t turn0 = static_cast<int64_t>(blockIdx.x) * kSlotThreads + tid;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kSlotThreads;
+  const bool by_blocks = all[0] > a.total;
+  for (int64_t t = turn0; t < a.total; t += step) {
     int64_t slot = -1;
     if (t < all[0]) {
-      int lo = 0, hi = kSlotThreads - 1;  // the last thread whose sum is at most t
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (tokens_before[mid] <= t)
-          lo = mid;
-        else
-          hi = mid - 1;
-      }
-      // Threads without tokens share their sum with the next that has some:
-      // the last of them is the one that holds t.
+      const int lo = holder(tokens_before, t);
       int64_t token = tokens_before[lo], block = blocks_before[lo];
       int b = lo * per;
       SlotRequest r = slot_request(a, b);
@@ -138,14 +146,27 @@ __global__ __launch_bounds__(kSlotThreads) void k_cache_slots(SlotArgs a) {
         if (col >= r.first) {
           const int64_t k = block + col - r.first;
           id = k < count ? a.free_blocks[count - 1 - k] : -1;
-          if (row == 0) *entry = id;
+          if (row == 0 && !by_blocks) *entry = id;
         } else {
           id = *entry;
         }
         if (id >= 0) slot = (static_cast<int64_t>(id) << a.log_block) + row;
       }
     }
-    if (t < a.total) a.slots[t] = slot;
+    a.slots[t] = slot;
+  }
+  if (!by_blocks) return;
+  for (int64_t k = turn0; k < all[1]; k += step) {
+    const int lo = holder(blocks_before, k);
+    int64_t block = blocks_before[lo];
+    int b = lo * per;
+    SlotRequest r = slot_request(a, b);
+    while (block + r.last - r.first <= k) {
+      block += r.last - r.first;
+      r = slot_request(a, ++b);
+    }
+    a.table[b * static_cast<int64_t>(a.width) + r.first + k - block] =
+        k < count ? a.free_blocks[count - 1 - k] : -1;
   }
 }
 
