@@ -214,8 +214,9 @@ SOFTMAX_API int softmax_paged_attention_fwd(const softmax_heads_t* q, const soft
  *
  * Negative lengths count as 0; sums are meant to stay below 2^31 (past it cu_q,
  * key_lens and missing are not specified).  The work of a call goes by the sizes
- * of its arrays, whatever the lengths.  Written arrays may not overlap each other or the inputs, except that the table is
- * both.  At most SOFTMAX_CACHE_MAX_REQUESTS requests.
+ * of its arrays, whatever the lengths.  Written arrays may not overlap each
+ * other or the inputs, except that the table is both.  At most
+ * SOFTMAX_CACHE_MAX_REQUESTS requests.
  */
 #define SOFTMAX_CACHE_MAX_REQUESTS 65536
 SOFTMAX_API int softmax_cache_slots(const int32_t* context_lens, const int32_t* new_lens,
