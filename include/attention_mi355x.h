@@ -229,7 +229,8 @@ SOFTMAX_API int softmax_cache_slots(const int32_t* context_lens, const int32_t* 
 /*
  * softmax_cache_append -- k[t] and v[t] into slot slots[t] of the caches, for
  * every token t; slots outside the cache (-1) are skipped.  Slots of a call
- * are meant to be distinct.
+ * are meant to be distinct.  The caches may lie between each other's rows (a
+ * tensor of both), but have no element in common.
  *
  *   k, v   [tokens, heads, d];  k_cache, v_cache of the same heads and d
  *   slots  device, [tokens] int64

@@ -77,6 +77,7 @@ SOFTMAX_API int softmax_cache_append(const softmax_heads_t* k, const softmax_hea
   const Range inputs[] = {{k->data, kb}, {v->data, vb}, {slots, k->tokens * 8}};
   const Range outputs[] = {{k_cache->data, kcb}, {v_cache->data, vcb}};
   // Keys and values of one allocation may interleave: a cache of both.
+  if (caches_meet(k_cache, kcb, v_cache, vcb, size)) return SOFTMAX_ERR_INVALID_ARG;
   const int rc = check_ranges(inputs, outputs, true);
   if (rc != SOFTMAX_OK) return rc;
   const int per = 16 / size;

@@ -1,7 +1,9 @@
 // Host-side checks shared by the entry points of attention_mi355x.h.
 #pragma once
 
+#include <algorithm>
 #include <cmath>
+#include <cstdlib>
 
 #include "../../include/attention_mi355x.h"
 #include "sm_host.hpp"
@@ -77,6 +79,40 @@ inline bool cache_ok(const softmax_cache_t* t, int size, int64_t* bytes) {
 inline bool same_cache(const softmax_cache_t* a, const softmax_cache_t* b) {
   return a->blocks == b->blocks && a->block_size == b->block_size && a->heads == b->heads &&
          a->d == b->d;
+}
+
+// Whether two caches of one shape have an element in common.  Their extents may
+// overlap: a cache of both, with one's rows between the other's.  With the same
+// strides two elements meet where the distance of the caches is a sum of index
+// differences times strides; strides that do not overlap themselves leave two
+// choices per axis, from the largest stride down, and a remainder within a row.
+// Caches of different strides have no element in common if their extents have
+// none, or else are taken to interleave unless they start at one place.
+inline bool caches_meet(const softmax_cache_t* a, int64_t a_bytes, const softmax_cache_t* b,
+                        int64_t b_bytes, int size) {
+  const auto pa = reinterpret_cast<uintptr_t>(a->data), pb = reinterpret_cast<uintptr_t>(b->data);
+  if (pa >= pb + b_bytes || pb >= pa + a_bytes) return false;
+  if (pa == pb) return true;
+  if (a->block_stride != b->block_stride || a->token_stride != b->token_stride ||
+      a->head_stride != b->head_stride)
+    return false;
+  struct Axis {
+    int64_t stride, count;
+  } axes[3] = {{a->block_stride, a->blocks}, {a->token_stride, a->block_size},
+               {a->head_stride, a->heads}};
+  std::sort(axes, axes + 3, [](const Axis& x, const Axis& y) { return x.stride > y.stride; });
+  int64_t left[8] = {static_cast<int64_t>(pa > pb ? pa - pb : pb - pa) / size};
+  int n = 1;
+  for (const Axis& x : axes) {
+    if (x.stride == 0 || x.count <= 1) continue;
+    for (int i = n; i-- > 0;) {  // the distance left over, or what the next step is too far
+      const int64_t from = left[i], q = std::min(from / x.stride, x.count - 1);
+      left[i] = from - q * x.stride;
+      left[n + i] = q + 1 < x.count ? std::abs(from - (q + 1) * x.stride) : left[i];
+    }
+    n *= 2;
+  }
+  return std::any_of(left, left + n, [&](int64_t x) { return x < a->d; });
 }
 
 inline bool score_ok(const softmax_score_t* s) {
