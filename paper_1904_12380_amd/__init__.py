@@ -232,6 +232,14 @@ def _run(fn, device, stream, args):
         return fn(*args, _raw_stream(index) if stream is None else int(stream.cuda_stream))
 
 
+def _on_device(device, fn, *args):
+    """``fn(*args)`` with ``device`` current: what it asks of the device."""
+    if device.index is None or _get_device() == device.index:
+        return fn(*args)
+    with _torch_mod.cuda.device(device.index):
+        return fn(*args)
+
+
 def _empty(shape, dtype, device, stream, returned=True):
     """Memory for a call on ``stream``: allocated for that stream, so that the
     allocator does not hand out what earlier work on the current stream still

@@ -294,8 +294,8 @@ def softmax_paged_attention_fwd(q, k_cache, v_cache, block_table, cu_q, key_lens
     out = _output(out, q.shape, q.dtype, device, "out", stream)
     if lse is not None:
         lse = _output(lse, q.shape[:2], torch.float32, device, "lse", stream)
-    room = _fns.softmax_paged_attention_workspace(aq.tokens, aq.heads, ak.heads, aq.d, requests,
-                                                  width * ak.block_size)
+    room = _sm._on_device(device, _fns.softmax_paged_attention_workspace, aq.tokens, aq.heads,
+                          ak.heads, aq.d, requests, width * ak.block_size)
     work = _sm._empty(room, torch.uint8, device, stream, returned=False) if room > 0 else None
     _checked(_sm._run(fn, device, stream,
                       (aq, ak, av, block_table.data_ptr(), width, pq, pk, requests, score,
