@@ -11,6 +11,9 @@ and the current stream, and there is no fallback.
     softmax_cache_slots(context_lens, new_lens, block_table, free_blocks, free_count, total,
                         block_size) -> dict
     softmax_cache_append(k, v, k_cache, v_cache, slots)
+
+Only softmax_packed_attention records a graph: the results of the other
+functions are constants for torch.autograd, also where inputs require gradients.
 """
 from __future__ import annotations
 
@@ -149,7 +152,14 @@ def _output(out, shape, dtype, device, name, stream):
             not out.is_contiguous():
         raise ValueError(f"{name} must be contiguous {list(shape)} of {dtype} on the device of "
                          "the other tensors")
+    _written(out)
     return out
+
+
+def _written(*tensors) -> None:
+    """Counts a write of the caller's tensors, as torch's own in-place
+    operations do: a backward pass that saved their former values is refused."""
+    _sm._torch_mod.autograd.graph.increment_version(tensors)
 
 
 def _checked(rc: int, what: str) -> None:
@@ -331,6 +341,7 @@ def softmax_cache_slots(context_lens, new_lens, block_table, free_blocks, free_c
     new = _vector(new_lens, "new_lens", i32, n, device)
     free = _vector(free_blocks, "free_blocks", i32, None, device)
     count = _vector(free_count, "free_count", i32, 1, device)
+    _written(block_table)
     slots = _sm._empty(total, torch.int64, device, stream)
     sums = _sm._empty(2 * n + 3, i32, device, stream)
     at = sums.data_ptr()
@@ -351,5 +362,6 @@ def softmax_cache_append(k, v, k_cache, v_cache, slots, *, stream=None) -> None:
     ak, av = _heads(k, "k"), _heads(v, "v", k)
     ck, cv = _cache(k_cache, "k_cache", k), _cache(v_cache, "v_cache", k)
     at = _vector(slots, "slots", _sm._torch_mod.int64, ak.tokens, k.device)
+    _written(k_cache, v_cache)
     _checked(_sm._run(fn, k.device, stream, (ak, av, ck, cv, at, _dtypes[k.dtype])),
              "softmax_cache_append")
