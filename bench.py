@@ -60,6 +60,7 @@ import json
 import math
 import os
 import platform
+import re
 import subprocess
 import sys
 import time
@@ -97,14 +98,31 @@ def cpu_model() -> str:
     return platform.processor() or "unknown"
 
 
+# The sources of the kernels that this file runs; the rest of csrc/ holds others.
+MEASURED_SOURCES = ("softmax_api.hip", "attention_api.hip")
+
+
+def measured_source_files() -> list[str]:
+    """Names of the measured sources and of what they include from csrc/."""
+    found, todo = set(), list(MEASURED_SOURCES)
+    while todo:
+        name = todo.pop()
+        if name in found or not os.path.exists(os.path.join(CSRC, name)):
+            continue
+        found.add(name)
+        with open(os.path.join(CSRC, name)) as f:
+            todo += re.findall(r'^\s*#\s*include\s+"([^"/]+)"', f.read(), re.M)
+    return sorted(found)
+
+
 def kernel_source_sha256() -> str:
-    """Hash of the HIP sources: counter and trace summaries are tied to it."""
+    """Hash of the measured kernels' HIP sources: counter and trace summaries
+    are tied to it."""
     h = hashlib.sha256()
-    for path in sorted(glob.glob(os.path.join(CSRC, "*"))):
-        if path.endswith((".hip", ".hpp", ".h")):
-            h.update(os.path.basename(path).encode())
-            with open(path, "rb") as f:
-                h.update(f.read())
+    for name in measured_source_files():
+        h.update(name.encode())
+        with open(os.path.join(CSRC, name), "rb") as f:
+            h.update(f.read())
     return h.hexdigest()
 
 
