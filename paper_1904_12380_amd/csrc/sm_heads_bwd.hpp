@@ -138,6 +138,12 @@ __device__ __forceinline__ void store_sums(float* p, int d, int half,
     }
 }
 
+// D's error that is left alone, as a part of the sum of the sizes of a row's score
+// gradients: half of the type's unit roundoff.  Where one key's term opposes all
+// others' it is half of that sum, and dQ's error then stays within the roundoff.
+template <typename T>
+constexpr float kMostOff = __is_same(T, f16) ? 0x1p-12f : 0x1p-9f;
+
 // dQ and D, by rows: three products for each pair, in one pass over the keys.
 // 16384 tokens of one document (16 heads of 128 on 2, bf16): 1.56 ms, 1060
 // TFLOP/s; 8192 tokens of documents of up to 2048 (32 heads on 8): 148 us, 540
@@ -147,6 +153,7 @@ __device__ __forceinline__ void store_sums(float* p, int d, int half,
 template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) char lds_bytes[tile_lds_bytes<DP>()];
+  __shared__ int redo[4];
   char SMX_LDS* lds = (char SMX_LDS*)lds_bytes;
   const int hk = blockIdx.x % a.kv_heads;
   const int slot = static_cast<int>(gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads);
@@ -182,7 +189,7 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
   load_operand<T, DP>(dout,
                       static_cast<const T*>(a.dout.data) + token * a.dout.ts + head * a.dout.hs,
                       valid, half, a.d);
-  float delta = 0.0f;
+  float delta = 0.0f, around = 0.0f;  // D, and the sum of |do o|
   {
     V o[DP / 16];
     load_operand<T, DP>(o, static_cast<const T*>(a.o.data) + token * a.o.ts + head * a.o.hs,
@@ -190,9 +197,13 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s)
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        delta = __builtin_fmaf(static_cast<float>(o[s][j]), static_cast<float>(dout[s][j]), delta);
+      for (int j = 0; j < 8; ++j) {
+        const float x = static_cast<float>(o[s][j]) * static_cast<float>(dout[s][j]);
+        delta += x;
+        around += fabsf(x);
+      }
     delta += half32_partner(delta);
+    around += half32_partner(around);
   }
   // Rows that see no key: weights of zero from the finite scores.
   float lse2 = INFINITY;
@@ -207,8 +218,8 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
   f32x16 acc[DP / 32] = {};
   FitRange<T> range;
   // The sum of P (dP - D), which D's error alone keeps from 0 (the weights sum
-  // to 1): what the gradients of the keys correct it by.
-  float rest[2] = {0.0f, 0.0f};
+  // to 1): what D is corrected by; and the sum of its terms' sizes.
+  float rest[2] = {0.0f, 0.0f}, size = 0.0f;
 
   const TileReader<DP> rd;
   constexpr int kTile = kTileKeys * DP * 2;
@@ -268,17 +279,57 @@ __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(He
       for (int i = 0; i < 16; ++i) {
         dp[i] = s[i] * (dp[i] - delta);
         rest[i % 2] += dp[i];
+        size += fabsf(dp[i]);
         if constexpr (MODE >= kCap) dp[i] *= sc.derivative(cap[i]);
       }
       range.fit(dp, acc);
       cols_accumulate<T, DP>(rd, kt, 32 * h, dp, two_parts, acc);
     }
   }
-  delta += (rest[0] + rest[1]) + half32_partner(rest[0] + rest[1]);
+  // D comes from o as it was rounded.  Where that error counts beside the row's
+  // score gradients (weights of nearly one key, whose terms all but cancel; values
+  // with a large common part), a second pass takes it out of dQ: it subtracts its
+  // product with P K.  With scores of a deviation of 30, dQ was off by 4.4 times its
+  // own rounding.  2^-19 of the sum of |do o| is what fp32 sums of D leave.
+  const float off = (rest[0] + rest[1]) + half32_partner(rest[0] + rest[1]);
+  size += half32_partner(size);
+  const bool wrong = fabsf(off) > fmaxf(kMostOff<T> * size, 0x1p-19f * around);
+  if (lane == 0) redo[wave] = __any(wrong);
+  __syncthreads();  // the last tile has been read
+  if (redo[0] || redo[1] || redo[2] || redo[3]) {
+    // Blocks of weights this small count for nothing, all of them together.
+    const float small = kMostOff<T> / 256.0f * size / (fabsf(off) * ((to + 31) / 32));
+    auto stage_keys = [&](int k0, int buf) {
+      keys.stage(a, keys.k, lds + buf * kTile + r0 * DP * 2, k0 + r0);
+    };
+    stage_keys(0, 0);
+    buf = 0;
+    for (int k0 = 0; k0 < to; k0 += kTileKeys, buf ^= 1) {
+      staged();
+      __syncthreads();
+      if (k0 + kTileKeys < to) stage_keys(k0 + kTileKeys, buf ^ 1);
+      if (k0 >= lim_any) continue;
+      const char SMX_LDS* kt = lds + buf * kTile;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f32x16 s = rows_dot<T, DP>(rd, kt, 32 * h, q), cap;
+        weights(s, cap, k0 + 32 * h);
+        if (!any_large(s, small)) continue;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[i] *= -off;
+          if constexpr (MODE >= kCap) s[i] *= sc.derivative(cap[i]);
+        }
+        range.fit(s, acc);
+        cols_accumulate<T, DP>(rd, kt, 32 * h, s, false, acc);
+      }
+    }
+    __syncthreads();
+  }
+  delta += off;
   if (valid && half == 0)
     reinterpret_cast<float2*>(a.delta)[static_cast<int64_t>(head) * a.tokens_q + token] =
         make_float2((kWeightLift<T> - lse2) / c, -delta);
-  __syncthreads();
   store_rows<T, DP>(lds + wave * 32 * DP * 2, acc, a.scale * range.back(),
                     static_cast<T*>(a.out), valid ? static_cast<int>(out) : -1, a.d);
 }
