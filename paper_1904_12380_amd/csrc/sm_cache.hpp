@@ -54,8 +54,8 @@ __device__ __forceinline__ SlotRequest slot_request(const SlotArgs& a, int b) {
 // more tokens than slots to write, the entries are shared out by themselves: the
 // turns are then bounded by the outputs' sizes, not by lengths that the device's
 // data holds.
-// Bound by latency: 8 requests of one token 3.6 us, 2048 of up to 320 (65536
-// tokens) 8.9 us, of a call of 11.4 and 12.2.
+// Bound by latency: 8 requests of one token 3.9 us, 2048 of up to 320 (65536
+// tokens) 9.0 us, of a call of 11.7 and 12.5.
 __global__ __launch_bounds__(kSlotThreads) void k_cache_slots(SlotArgs a) {
   __shared__ int64_t tokens_before[kSlotThreads + 1], blocks_before[kSlotThreads];
   __shared__ int64_t wave_sums[3][kSlotThreads / 64];

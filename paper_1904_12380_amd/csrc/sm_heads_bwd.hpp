@@ -144,12 +144,14 @@ __device__ __forceinline__ void store_sums(float* p, int d, int half,
 template <typename T>
 constexpr float kMostOff = __is_same(T, f16) ? 0x1p-12f : 0x1p-9f;
 
-// dQ and D, by rows: three products for each pair, in one pass over the keys.
-// 16384 tokens of one document (16 heads of 128 on 2, bf16): 1.56 ms, 1060
-// TFLOP/s; 8192 tokens of documents of up to 2048 (32 heads on 8): 148 us, 540
-// TFLOP/s, since most of these are a few tiles long.  Bound by matrix ops and LDS
-// reads: one operand of each product comes from LDS, 32 rows of it for 32 columns
-// held in registers.
+// dQ and D, by rows: three products for each pair, in one pass over the keys, and
+// where D's error counts (below) two more in a second.  16384 tokens of one document
+// (16 heads of 128 on 2, bf16): 1.65 ms, 1000 TFLOP/s; 8192 tokens of documents of up
+// to 2048 (32 heads on 8): 156 us, 510 TFLOP/s, since most of these are a few tiles
+// long.  Bound by matrix ops and LDS reads: one operand of each product comes from
+// LDS, 32 rows of it for 32 columns held in registers.  At a width of 128 the plain
+// scores' instance holds all of its registers; a bias spills 22 of them, a cap 8 and
+// both 88.
 template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dq(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) char lds_bytes[tile_lds_bytes<DP>()];
@@ -399,11 +401,16 @@ constexpr int kKeyLds = (kTileRows + 2 * 2 * kTurnRows) * DP * 2;
 
 // dK and dV, by keys: four products for each pair.  16384 tokens of one
 // document: 2.4 ms, 920 TFLOP/s; packed documents of 8192 tokens 190 us (sizes as
-// above).  Bound by matrix ops and LDS reads, of which V's are a fifth.
+// above).  Bound by matrix ops and LDS reads, of which V's are a fifth.  Where a call
+// has 64 documents or more every workgroup reads all of their lengths for its
+// splits: 8192 tokens in 2048 documents of 4 take 3.8 ms forward and backward.
 //
 // A wavefront's K operand stays in registers, its V operand in LDS: with both in
 // registers (64 at a width of 128, beside 128 of sums and 32 of scores) some
-// were spilled, and a reload from scratch waits for the next stage's loads.
+// were spilled, and a reload from scratch waits for the next stage's loads.  The
+// instances with a bias, a cap or both still spill 29, 78 and 83 registers there, and
+// all of width 256 do: packed documents of 8192 tokens take 717, 750 and 905 us
+// forward and backward with them, and 515 without.
 template <typename T, int DP, int MODE>
 __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_dkv(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) char lds_bytes[kKeyLds<DP>];

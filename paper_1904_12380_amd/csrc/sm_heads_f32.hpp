@@ -13,9 +13,13 @@
 // A workgroup of four wavefronts takes 64 rows (16 each, operands in
 // registers) against tiles of 32 keys (or 64 keys against tiles of 32 rows),
 // staged as fp32 in LDS, whose rows are 4 floats longer than a row so that 16
-// rows read at one column spread over the banks.  Bound by the fp32 matrix rate
-// (150 TFLOP/s) on long calls; 101 tokens of four heads of 80 in short
-// documents take 9 us forward and 26 us back, a few tiles' latency each.
+// rows read at one column spread over the banks.  Bound by latency: a tile's product
+// is one chain of dependent matrix ops.  4096 tokens of one document (16 heads of
+// 128 on 4) take 0.81 ms forward, 85 of the 154 TFLOP/s that a large product
+// reaches, and 4.7 ms back, 51; 64 single tokens over up to 8192 keys (32 heads on
+// 8) 1.4 ms, 1.6 TB/s, since three of four wavefronts have no row; 101 tokens of
+// four heads of 80 in short documents 9 us forward and 26 us back, a few tiles'
+// latency each.
 #pragma once
 
 #include "sm_heads.hpp"
@@ -209,6 +213,7 @@ __global__ __launch_bounds__(kF32Threads) void k_heads_fwd_f32(HeadsArgs a) {
     for (int kt = 0; kt < 2; ++kt) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        // The argument's rounding is 2^-24 of it: 1e-6 of a weight of e^-16.
         s[kt][i] = __builtin_amdgcn_exp2f((s[kt][i] - base) * kLog2eF);
         part += s[kt][i];
       }

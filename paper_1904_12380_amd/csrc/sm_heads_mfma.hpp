@@ -614,13 +614,17 @@ __device__ __forceinline__ void store_rows(char SMX_LDS* lds, const f32x16 (&acc
 }
 
 // One pass over the keys with a running maximum and sum.  A chunk of 2048 tokens
-// over 65536 keys (32 heads of 128 on 8, bf16, a bias): 2.5 ms, 860 TFLOP/s,
+// over 65536 keys (32 heads of 128 on 8, bf16, a bias): 2.5 ms, 855 TFLOP/s,
 // where a product of 8192 x 8192 matrices reaches 1230 on this card: bound by
 // the matrix ops and the exponentials between them, which take turns on a
 // SIMD; two workgroups per CU let one's products run during the other's
 // softmax.  64 single tokens over up to 8192 keys: 235 us, 4.9 TB/s, bound by
-// memory.  16384 tokens of one document (16 heads of 128 on 2): 1.04 ms, 1060
+// memory.  16384 tokens of one document (16 heads of 128 on 2): 1.07 ms, 1030
 // TFLOP/s.
+//
+// Weights are rounded to the type for the value product, which the matrix ops of
+// 16-bit types ask for; their sum is taken before.  Against one rounding of the
+// result in all, errors are 1.1 to 1.3 times as large by norm.
 template <typename T, int DP, int WHERE, int MODE>
 __global__ __launch_bounds__(kTileThreads, DP <= 128 ? 2 : 1) void k_heads_fwd(HeadsArgs a) {
   __shared__ __attribute__((aligned(16))) char lds_bytes[tile_lds_bytes<DP>()];
