@@ -141,7 +141,9 @@ SOFTMAX_API int64_t softmax_packed_attention_bwd_workspace(int64_t tokens_q, int
  * the sums for dk and dv over all query heads of a key/value head too.
  *
  *   dout       gradient of o, [tokens_q, heads, d]
- *   o, lse     of the forward call
+ *   o, lse     of the forward call.  Weights come from lse, whose fp32 leaves
+ *              them off by 2^-23 of the largest score's size: gradients are
+ *              meant for scores of up to 10^5, and need not be finite past 10^7
  *   dq, dk, dv contiguous, of the shapes of q, k and v; written in full
  *              (zeros for tokens that no document holds)
  *   workspace  at least softmax_packed_attention_bwd_workspace() bytes of

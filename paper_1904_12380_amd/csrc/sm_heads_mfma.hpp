@@ -486,6 +486,8 @@ constexpr float kSlack = __is_same(T, f16) ? 3.5f : 8.0f;
 template <typename T>
 constexpr float kLift = __is_same(T, f16) ? 12.0f : 0.0f;
 
+constexpr float kFarShift = 0x1p14f;
+
 // One wavefront's state for 32 rows, a lane's row at l % 32.
 template <typename T, int DP>
 struct RowState {
@@ -547,7 +549,19 @@ __device__ __forceinline__ void attend(const Scoring<MODE>& sc, RowState<T, DP>&
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t) w.acc[t] *= alpha;
   }
-  const float shift = w.m > kUnseen ? kLift<T> - w.m * w.c : 0.0f;
+  // Past kFarShift the shift's own rounding would scale a row's weights by a part of
+  // a power of two, and further on by several (past fp16's range from scores of
+  // 10^7): differences are formed first there, which makes them exact.
+  float shift = w.m > kUnseen ? kLift<T> - w.m * w.c : 0.0f;
+  const bool far = fabsf(shift) > kFarShift;
+  if (__any(far)) {  // other rows of the wavefront keep their bits
+    const float base = far ? w.m : 0.0f;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kt][i] -= base;
+    if (far) shift = kLift<T>;
+  }
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     float part[2] = {0.0f, 0.0f};
