@@ -13,6 +13,8 @@ Contents
                           parity references).
 ``attention_f64``        float64 softmax attention, softmax(scale Q K^T) V
                           per batch element, built on ``softmax_f64``.
+``decoder_f64``           the loss over a vocabulary, embedding rows and norms of
+                          rows, with their gradients.
 ``cpu_fp32_baseline.c``  a straightforward single-thread fp32 C softmax in the
                           loop shape of the paper's MKL-era functor; it is a
                           timed CPU baseline, never a parity reference.

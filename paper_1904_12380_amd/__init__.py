@@ -36,6 +36,18 @@ and those of attention.py, the attention of language models:
     softmax_cache_slots(context_lens, new_lens, block_table, free_blocks, free_count,
                         total, block_size) -> dict
     softmax_cache_append(k, v, k_cache, v_cache, slots)
+
+and those of decoder.py, what a decoder has around its attention:
+
+    softmax_linear_nll(x, weight, labels, ignore=-100) -> loss, differentiable
+    softmax_linear_nll_fwd(x, weight, labels, ...) -> (loss, lse)
+    softmax_linear_nll_bwd(dloss, x, weight, labels, loss, lse, ...) -> (dx, dweight)
+    softmax_embedding(ids, table, scale=1.0) -> torch.Tensor, differentiable
+    softmax_embedding_fwd(ids, table, ...) -> torch.Tensor
+    softmax_embedding_bwd(dout, ids, rows, ...) -> dtable
+    softmax_layer_norm(x, weight=None, bias=None, eps=1e-5, center=True), differentiable
+    softmax_layer_norm_fwd(x, weight=None, bias=None, ...) -> (y, mean, rstd)
+    softmax_layer_norm_bwd(dy, x, weight, mean, rstd, ...) -> (dx, dweight, dbias)
 """
 from __future__ import annotations
 
@@ -53,6 +65,9 @@ __all__ = [
     "softmax_packed_attention", "softmax_packed_attention_fwd", "softmax_packed_attention_bwd",
     "softmax_paged_attention_fwd", "softmax_cache_slots", "softmax_cache_append",
     "HEADS_MAX_DIM",
+    "softmax_linear_nll", "softmax_linear_nll_fwd", "softmax_linear_nll_bwd",
+    "softmax_embedding", "softmax_embedding_fwd", "softmax_embedding_bwd",
+    "softmax_layer_norm", "softmax_layer_norm_fwd", "softmax_layer_norm_bwd", "MAX_WIDTH",
     "CLIP_LO", "CLIP_MAX", "KERNEL_NAMES",
 ]
 
@@ -137,6 +152,7 @@ def load_library() -> ctypes.CDLL:
     lib.softmax_exchange_status.argtypes = [u64p, u64p, ctypes.POINTER(ctypes.c_int32)]
     lib.softmax_exchange_status.restype = ctypes.c_int
     attention.declare(lib)
+    decoder.declare(lib)
     _lib = lib
     return lib
 
@@ -478,7 +494,11 @@ def softmax_copy_probe(x, out=None, stream=None):
     return out
 
 
-from . import attention  # noqa: E402  (it uses the helpers above)
+from . import attention, decoder  # noqa: E402  (they use the helpers above)
 from .attention import (  # noqa: E402,F401
     HEADS_MAX_DIM, softmax_cache_append, softmax_cache_slots, softmax_packed_attention,
     softmax_packed_attention_bwd, softmax_packed_attention_fwd, softmax_paged_attention_fwd)
+from .decoder import (  # noqa: E402,F401
+    MAX_WIDTH, softmax_embedding, softmax_embedding_bwd, softmax_embedding_fwd,
+    softmax_layer_norm, softmax_layer_norm_bwd, softmax_layer_norm_fwd, softmax_linear_nll,
+    softmax_linear_nll_bwd, softmax_linear_nll_fwd)

@@ -1,0 +1,273 @@
+// C ABI of the loss over a vocabulary: argument checks, workspace and launches.
+// Declarations and contract: include/decoder_mi355x.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "sm_decoder_host.hpp"
+#include "sm_linear_nll.hpp"
+#include "sm_linear_nll_launch.hpp"
+
+namespace {
+
+using namespace smx;
+using namespace smx_host;
+
+constexpr int64_t kTile = 256;  // all tiles' sizes divide it
+
+NllProduct product(int kind, int64_t tokens, int dtype) {
+  return dtype == SOFTMAX_F32   ? nll_product_f32(kind, tokens)
+         : dtype == SOFTMAX_F16 ? nll_product_f16(kind, tokens)
+                                : nll_product_bf16(kind, tokens);
+}
+
+// The kernels' NllHead, places and tokens, and the packed rows.
+struct Room {
+  int64_t place, token, packed, more, end;
+};
+
+Room room(int64_t rows, int64_t d, int size) {
+  const int64_t padded = up_to(rows, kTile);
+  Room r;
+  r.place = sizeof(NllHead);
+  r.token = r.place + up_to(rows * 4, 16);
+  r.packed = r.token + padded * static_cast<int64_t>(sizeof(NllToken));
+  r.more = r.packed + padded * up_to(d * size, kLineBytes);
+  r.end = r.more;
+  return r;
+}
+
+int64_t forward_bytes(int64_t rows, int64_t vocab, int64_t d, int dtype) {
+  const int64_t padded = up_to(rows, kTile);
+  const int64_t tiles = ceil_div(vocab, product(kLogits, rows, dtype).bm);
+  return room(rows, d, dtype_size(dtype)).more + padded * 4 + tiles * padded * 8;
+}
+
+// The piece of the vocabulary whose g is kept at a time: what fits kPieceBytes, in
+// equal pieces.
+constexpr int64_t kPieceBytes = int64_t(512) << 20;
+
+int64_t piece_of(int64_t rows, int64_t vocab, int size) {
+  const int64_t most = std::clamp<int64_t>(kPieceBytes / size / up_to(rows, kTile) / kTile, 1, 4096);
+  const int64_t tiles = ceil_div(vocab, kTile);
+  return ceil_div(tiles, ceil_div(tiles, most)) * kTile;
+}
+
+// Splits of a piece's rows for dx: as few as leave at most a tenth of the device
+// idle, or else those that leave the least; a split has eight stages or more.  The
+// number of CUs is MI355X's: the order of the sums, and the workspace, go by sizes
+// alone.
+constexpr int64_t kCus = 256;
+
+int64_t splits_of(int64_t rows, int64_t piece, int64_t d, int dtype) {
+  const NllProduct p = product(kInput, rows, dtype);
+  const int64_t tiles = ceil_div(rows, p.bn) * ceil_div(d, p.bm);
+  const int64_t stages = piece * dtype_size(dtype) / kLineBytes;
+  const int64_t most = std::clamp<int64_t>(stages / 8, 1, 64);
+  int64_t best = 1;
+  double full = 0.0;
+  for (int64_t s = 1; s <= most && full < 0.9; ++s) {
+    const double f = static_cast<double>(tiles * s) / (ceil_div(tiles * s, kCus) * kCus);
+    if (f > full) {
+      full = f;
+      best = s;
+    }
+  }
+  return best;
+}
+
+struct Backward {
+  int64_t g, sums, end, piece, splits;
+};
+
+Backward backward_room(int64_t rows, int64_t vocab, int64_t d, int dtype) {
+  const int size = dtype_size(dtype);
+  const int64_t padded = up_to(rows, kTile);
+  Backward b;
+  b.piece = piece_of(rows, vocab, size);
+  b.splits = splits_of(rows, b.piece, d, dtype);
+  b.g = room(rows, d, size).more;
+  b.sums = b.g + padded * b.piece * size;
+  b.end = b.sums + b.splits * padded * up_to(d * size, kLineBytes) / size * 4;
+  return b;
+}
+
+// Workgroups of tiles of bm x bn, within what a launch takes.
+bool sizes_ok(int64_t rows, int64_t vocab, int64_t d, int dtype) {
+  if (dtype_size(dtype) == 0 || !count_ok(rows) || !count_ok(vocab) || !width_ok(d)) return false;
+  const int64_t tile = dtype == SOFTMAX_F32 ? 128 : 256;
+  const int64_t most = (int64_t(1) << 32) / (dtype == SOFTMAX_F32 ? 256 : 512);
+  const int64_t t = ceil_div(rows, tile), v = ceil_div(vocab, tile), c = ceil_div(d, tile);
+  return std::max({t * v, t * c, v * c}) < most - 64;
+}
+
+bool strides_ok(int64_t x_stride, int64_t w_stride) {
+  return x_stride >= 0 && w_stride >= 0 && w_stride <= SOFTMAX_MAX_ROW_STRIDE;
+}
+
+void set_call(NllArgs* a, const void* x, int64_t x_stride, const void* weight, int64_t w_stride,
+              const int64_t* labels, int64_t rows, int64_t vocab, int64_t d, int64_t ignore,
+              int size, void* workspace) {
+  const Room r = room(rows, d, size);
+  char* const at = static_cast<char*>(workspace);
+  a->x = x;
+  a->x_pitch = x_stride * size;
+  a->weight = weight;
+  a->w_pitch = w_stride * size;
+  a->labels = labels;
+  a->ignore = ignore;
+  a->rows = static_cast<int>(rows);
+  a->vocab = static_cast<int>(vocab);
+  a->d = static_cast<int>(d);
+  a->padded_rows = static_cast<int>(up_to(rows, kTile));
+  a->padded_d = static_cast<int>(up_to(d * size, kLineBytes) / size);
+  a->head = reinterpret_cast<NllHead*>(at);
+  a->place = reinterpret_cast<int*>(at + r.place);
+  a->token = reinterpret_cast<NllToken*>(at + r.token);
+  a->packed = at + r.packed;
+}
+
+hipError_t start(const void* fn, int64_t x, int64_t y, int threads, void** args, hipStream_t s) {
+  return hipLaunchKernel(fn, dim3(static_cast<uint32_t>(x), static_cast<uint32_t>(y)),
+                         dim3(threads), args, 0, s);
+}
+
+template <bool BACK>
+hipError_t pack(NllArgs* a, int dtype, hipStream_t stream) {
+  // At most 1024 workgroups, since each counts the labels before its own.
+  int each = static_cast<int>(up_to(std::max<int64_t>(ceil_div(a->rows, 1024), 1), kPackTokens));
+  const void* fn = dtype == SOFTMAX_F32   ? reinterpret_cast<const void*>(&k_nll_pack<float, BACK>)
+                   : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_nll_pack<f16, BACK>)
+                                          : reinterpret_cast<const void*>(&k_nll_pack<bf16, BACK>);
+  void* args[] = {a, &each};
+  return start(fn, ceil_div(a->rows, each), 1, 256, args, stream);
+}
+
+hipError_t multiply_tiles(const NllProduct& p, int64_t m, int64_t n, int64_t splits, NllArgs* a,
+                          hipStream_t stream) {
+  void* args[] = {a};
+  return start(p.fn, up_to(ceil_div(m, p.bm) * ceil_div(n, p.bn), kXcds), splits, p.threads, args,
+               stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+SOFTMAX_API int64_t softmax_linear_nll_fwd_workspace(int64_t rows, int64_t vocab, int64_t d,
+                                                     int dtype) {
+  if (!sizes_ok(rows, vocab, d, dtype)) return -1;
+  return rows == 0 || vocab == 0 ? 0 : forward_bytes(rows, vocab, d, dtype);
+}
+
+SOFTMAX_API int softmax_linear_nll_fwd(const void* x, int64_t x_stride, const void* weight,
+                                       int64_t w_stride, const int64_t* labels, int64_t rows,
+                                       int64_t vocab, int64_t d, int64_t ignore, int dtype,
+                                       float* loss, float* lse, void* workspace,
+                                       int64_t workspace_bytes, hipStream_t stream) {
+  const int size = dtype_size(dtype);
+  int64_t xb = 0, wb = 0;
+  if (!sizes_ok(rows, vocab, d, dtype) || !strides_ok(x_stride, w_stride) ||
+      !rows_ok(x, rows, x_stride, d, size, &xb) ||
+      !rows_ok(weight, vocab, w_stride, d, size, &wb) || !aligned16(workspace))
+    return SOFTMAX_ERR_INVALID_ARG;
+  if (rows == 0) return SOFTMAX_OK;
+  const int64_t need = forward_bytes(rows, vocab, d, dtype);
+  if (vocab == 0 || workspace_bytes < need) return SOFTMAX_ERR_INVALID_ARG;
+  const Range inputs[] = {{x, xb}, {weight, wb}, {labels, rows * 8}};
+  const Range outputs[] = {{loss, rows * 4}, {lse, rows * 4}, {workspace, need}};
+  const int rc = check_ranges(inputs, outputs);
+  if (rc != SOFTMAX_OK) return rc;
+  NllArgs a = {};
+  set_call(&a, x, x_stride, weight, w_stride, labels, rows, vocab, d, ignore, size, workspace);
+  a.loss = loss;
+  a.lse = lse;
+  const NllProduct p = product(kLogits, rows, dtype);
+  a.tiles = static_cast<int>(ceil_div(vocab, p.bm));
+  a.at = reinterpret_cast<float*>(static_cast<char*>(workspace) + room(rows, d, size).more);
+  a.part = reinterpret_cast<f32x2*>(a.at + a.padded_rows);
+  a.piece = static_cast<int>(up_to(vocab, kTile));
+  hipError_t e = pack<false>(&a, dtype, stream);
+  if (e == hipSuccess) e = multiply_tiles(p, vocab, rows, 1, &a, stream);
+  if (e == hipSuccess) {
+    void* args[] = {&a};
+    e = start(reinterpret_cast<const void*>(&k_nll_join<4>), ceil_div(rows, 64), 1, 256, args,
+              stream);
+  }
+  return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
+}
+
+SOFTMAX_API int64_t softmax_linear_nll_bwd_workspace(int64_t rows, int64_t vocab, int64_t d,
+                                                     int dtype) {
+  if (!sizes_ok(rows, vocab, d, dtype)) return -1;
+  return rows == 0 || vocab == 0 ? 0 : backward_room(rows, vocab, d, dtype).end;
+}
+
+SOFTMAX_API int softmax_linear_nll_bwd(const float* dloss, const void* x, int64_t x_stride,
+                                       const void* weight, int64_t w_stride,
+                                       const int64_t* labels, int64_t rows, int64_t vocab,
+                                       int64_t d, int64_t ignore, int dtype, const float* loss,
+                                       const float* lse, void* dx, void* dweight,
+                                       void* workspace, int64_t workspace_bytes,
+                                       hipStream_t stream) {
+  const int size = dtype_size(dtype);
+  int64_t xb = 0, wb = 0;
+  if (!sizes_ok(rows, vocab, d, dtype) || !strides_ok(x_stride, w_stride) ||
+      !rows_ok(x, rows, x_stride, d, size, &xb) ||
+      !rows_ok(weight, vocab, w_stride, d, size, &wb) || !aligned16(workspace) ||
+      !aligned16(dx) || !aligned16(dweight))
+    return SOFTMAX_ERR_INVALID_ARG;
+  const bool some = rows > 0 && vocab > 0;
+  if (rows > 0 && vocab == 0) return SOFTMAX_ERR_INVALID_ARG;
+  if (rows == 0 && (vocab == 0 || dweight == nullptr)) return SOFTMAX_OK;
+  const Backward b = some ? backward_room(rows, vocab, d, dtype) : Backward{};
+  if (workspace_bytes < b.end) return SOFTMAX_ERR_INVALID_ARG;
+  const Range inputs[] = {{dloss, rows * 4}, {x, xb},       {weight, wb}, {labels, rows * 8},
+                          {loss, rows * 4},  {lse, rows * 4}};
+  const Range outputs[] = {{dx, dx ? rows * d * size : 0},
+                           {dweight, dweight ? vocab * d * size : 0},
+                           {workspace, b.end}};
+  const int rc = check_ranges(inputs, outputs);
+  if (rc != SOFTMAX_OK) return rc;
+  if (!some) {
+    // No rows: the sums over them are zeros.
+    uint4* out = static_cast<uint4*>(dweight);
+    int64_t strips = vocab * d * size / 16;
+    void* args[] = {&out, &strips};
+    const hipError_t e = start(reinterpret_cast<const void*>(&k_nll_clear<0>),
+                               std::min<int64_t>(ceil_div(strips, 256), 2048), 1, 256, args, stream);
+    return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
+  }
+  NllArgs a = {};
+  set_call(&a, x, x_stride, weight, w_stride, labels, rows, vocab, d, ignore, size, workspace);
+  a.dloss = dloss;
+  a.loss = const_cast<float*>(loss);
+  a.lse = const_cast<float*>(lse);
+  a.dx = dx;
+  a.dweight = dweight;
+  a.g = static_cast<char*>(workspace) + b.g;
+  a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + b.sums);
+  a.piece = static_cast<int>(b.piece);
+  a.splits = static_cast<int>(b.splits);
+  if (dx == nullptr && dweight == nullptr) return SOFTMAX_OK;
+  hipError_t e = pack<true>(&a, dtype, stream);
+  for (int64_t from = 0; from < vocab && e == hipSuccess; from += b.piece) {
+    a.from = static_cast<int>(from);
+    const int64_t left = std::min(vocab - from, b.piece);
+    e = multiply_tiles(product(kProbs, rows, dtype), b.piece, rows, 1, &a, stream);
+    if (e == hipSuccess && dx != nullptr)
+      e = multiply_tiles(product(kInput, rows, dtype), d, rows, b.splits, &a, stream);
+    if (e == hipSuccess && dweight != nullptr)
+      e = multiply_tiles(product(kWeight, rows, dtype), d, left, 1, &a, stream);
+  }
+  if (e == hipSuccess && dx != nullptr) {
+    void* args[] = {&a};
+    const void* fn = dtype == SOFTMAX_F32   ? reinterpret_cast<const void*>(&k_nll_input<float>)
+                     : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_nll_input<f16>)
+                                            : reinterpret_cast<const void*>(&k_nll_input<bf16>);
+    e = start(fn, std::min<int64_t>(ceil_div(rows * (d / 8), 256), 16 * kCus), 1, 256, args, stream);
+  }
+  return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
+}
+
+}  // extern "C"

@@ -1,0 +1,8 @@
+// Instances of the tile products of the loss over a vocabulary for bf16.
+#include "sm_linear_nll_shapes.hpp"
+
+namespace smx {
+
+NllProduct nll_product_bf16(int kind, int64_t tokens) { return nll_product_16<bf16>(kind, tokens); }
+
+}  // namespace smx

@@ -1,0 +1,451 @@
+// The loss of hidden states against the rows of a vocabulary, and its gradients
+// (include/decoder_mi355x.h has the operation), without keeping the logits.
+//
+//   k_nll_pack      tokens that have a loss are taken together: x of token t
+//                   goes to row place[t] of a matrix with rows of whole stages,
+//                   so that tokens without a loss cost nothing in the products,
+//                   whatever their x holds, and strides and row tails end here.
+//   k_nll_product   four products of tiles (sm_product.hpp):
+//     kLogits   logits of a tile of the vocabulary by tokens; what stays of them
+//               is each token's maximum and sum of exponentials over the tile
+//     kProbs    the same logits again, turned into g = dl/dlogit, kept for a
+//               piece of the vocabulary
+//     kInput    sums over the piece's rows for dx, in splits, fp32
+//     kWeight   sums over the tokens for the piece's rows of dweight, whole
+//   k_nll_join      the tiles' statistics to lse and loss
+//   k_nll_input     the splits' sums to dx
+//
+// The logits are formed in both passes by the same operations in the same order.
+// Of g the label's entry is taken from the loss, e^-loss - 1, which keeps it exact
+// where the likelihood is near 1 and lse and the label's logit cancel.
+//
+// g is rounded to the type for the products on the matrix cores.  It is formed
+// relative to the largest |dloss| of the call, in fp32, which enters the sums' last
+// rounding: a loss that is a mean over tokens then leaves the label's entry e^-loss
+// - 1 itself, not the product with 1 / tokens, whose rounding would be the same for
+// all tokens and not average out.  For fp16 it is 2^14 times as large on top: fp16
+// then holds 11 bits of it down to 2^-28 of the largest.
+#pragma once
+
+#include "sm_product.hpp"
+
+namespace smx {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kNoLogit = -__builtin_inff();
+constexpr int kLogits = 0, kProbs = 1, kInput = 2, kWeight = 3;
+
+// What the products know of a token: g = e^(logit - lse) * weight, and `label_g`
+// at the label (-1: the label is no row of the vocabulary).
+struct NllToken {
+  float lse, weight, label_g;
+  int label;
+};
+
+// What a call knows of its tokens, at the start of its workspace.
+struct NllHead {
+  int live;      // tokens that have a loss
+  float unit;    // what the sums of g are multiplied with
+  int pad[2];
+};
+
+struct NllArgs {
+  const void* x;
+  int64_t x_pitch;        // bytes
+  const void* weight;
+  int64_t w_pitch;        // bytes
+  const int64_t* labels;
+  int64_t ignore;
+  int rows, vocab, d;
+  int padded_rows;        // rows, in whole tiles
+  int padded_d;           // d, in whole stages
+  float* loss;            // written by the forward pass, read by the backward
+  float* lse;
+  const float* dloss;
+  void* dx;               // may be null
+  void* dweight;          // may be null
+  // Workspace.
+  NllHead* head;
+  int* place;             // [rows]: a token's row among those that have a loss, or -1
+  NllToken* token;        // [padded_rows]
+  char* packed;           // [padded_rows, padded_d] of the type
+  f32x2* part;            // forward: (max, sum) [tiles, padded_rows]
+  float* at;              // forward: the label's logit [padded_rows]
+  char* g;                // backward: [padded_rows, piece] of the type
+  float* sums;            // backward: [splits, padded_rows, padded_d]
+  int tiles;              // tiles of the vocabulary that `part` has
+  int from, piece;        // backward: first row of the piece, and its padded length
+  int splits;
+};
+
+// The largest finite |dloss| is a power of two times this much in g.
+template <typename T>
+constexpr float kUnitUp = __is_same(T, f16) ? 0x1p14f : 1.0f;
+
+constexpr int kPackTokens = 16;  // fewest tokens of a workgroup
+
+// Tokens together.  Every workgroup counts the tokens before its own by itself:
+// that reads the labels once per workgroup, from the L2, and saves a launch;
+// `each` tokens per workgroup grow with their number.
+template <typename T, bool BACK>
+__global__ __launch_bounds__(256) void k_nll_pack(NllArgs a, int each) {
+  __shared__ int count_lds[4];
+  __shared__ float most_lds[4];
+  const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
+  const int first = blockIdx.x * each, last = min(first + each, a.rows);
+  int count = 0;
+  for (int t = tid; t < first; t += 256) count += a.labels[t] != a.ignore;
+  float most = 0.0f;
+  if constexpr (BACK) {
+    for (int t = tid; t < a.rows; t += 256) {
+      const float w = fabsf(a.dloss[t]);
+      if (w <= 3.402823466e38f && a.labels[t] != a.ignore) most = fmaxf(most, w);
+    }
+    most = seg_max<64>(most);
+    if (lane == 0) most_lds[wave] = most;
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) count += __shfl_xor(count, s);
+  if (lane == 0) count_lds[wave] = count;
+  __syncthreads();
+  count = count_lds[0] + count_lds[1] + count_lds[2] + count_lds[3];
+  float unit = 1.0f;
+  if constexpr (BACK) {
+    most = fmaxf(fmaxf(most_lds[0], most_lds[1]), fmaxf(most_lds[2], most_lds[3]));
+    // A |dloss| below the normal numbers is taken as it is.
+    unit = most < 0x1p-100f ? 1.0f : most;
+  }
+  // Each wavefront copies a quarter of the tokens, all of them know all places.
+  const int chunks = a.padded_d * static_cast<int>(sizeof(T)) / 16;
+  const int whole = a.d * static_cast<int>(sizeof(T)) / 16;
+  for (int t0 = first; t0 < last; t0 += 64) {
+    const int t = t0 + lane;
+    const int64_t label = t < last ? a.labels[t] : a.ignore;
+    const bool live = t < last && label != a.ignore;
+    const uint64_t mask = __ballot(live);
+    const int row = count + __popcll(mask & ((uint64_t(1) << lane) - 1));
+    if (t < last && wave == 0) {
+      a.place[t] = live ? row : -1;
+      if (live) {
+        NllToken k = {0.0f, 0.0f, 0.0f, -1};
+        if (label >= 0 && label < a.vocab) k.label = static_cast<int>(label);
+        if constexpr (BACK) {
+          const float loss = a.loss[t];
+          k.lse = a.lse[t];
+          k.weight = a.dloss[t] / unit * kUnitUp<T>;
+          k.label_g = expm1f(-loss) * k.weight;
+          if (k.label < 0) k.weight = __builtin_nanf("");
+        }
+        a.token[row] = k;
+      }
+    }
+    for (int i = wave; i < 64 && t0 + i < last; i += 4) {
+      if (!(mask >> i & 1)) continue;
+      const int64_t to = count + __popcll(mask & ((uint64_t(1) << i) - 1));
+      const uint4* from = reinterpret_cast<const uint4*>(static_cast<const char*>(a.x) +
+                                                         (t0 + i) * a.x_pitch);
+      uint4* out = reinterpret_cast<uint4*>(a.packed) + to * chunks;
+      for (int c = lane; c < chunks; c += 64) out[c] = c < whole ? from[c] : uint4{0, 0, 0, 0};
+    }
+    count += __popcll(mask);
+  }
+  if (last != a.rows) return;
+  // The last workgroup knows the number of tokens, and clears the rows up to the
+  // end of their last tile.
+  if (tid == 0) *a.head = {count, unit / kUnitUp<T>, {0, 0}};
+  const int end = min((count + 255) / 256 * 256, a.padded_rows);
+  for (int r = count + wave; r < end; r += 4) {
+    if (lane == 0) a.token[r] = {INFINITY, 0.0f, 0.0f, -1};
+    uint4* out = reinterpret_cast<uint4*>(a.packed) + static_cast<int64_t>(r) * chunks;
+    for (int c = lane; c < chunks; c += 64) out[c] = uint4{0, 0, 0, 0};
+  }
+}
+
+// Eight fp32 values (four of registers i0 .., four of i0 + 4 ..) to the type, as
+// the 16 bytes m = 16 (i0 / 8) + 8 (l / 32) .. of the lane's column: the halves of
+// the wavefront swap what the other one's strip holds.
+template <typename T>
+__device__ __forceinline__ uint4 strip8(const float (&v)[8]) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 p, q;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    p[j] = static_cast<T>(v[j]);
+    q[j] = static_cast<T>(v[4 + j]);
+  }
+  const uint2 pu = __builtin_bit_cast(uint2, p), qu = __builtin_bit_cast(uint2, q);
+  const auto x = __builtin_amdgcn_permlane32_swap(pu.x, qu.x, false, false);
+  const auto y = __builtin_amdgcn_permlane32_swap(pu.y, qu.y, false, false);
+  return {x[0], y[0], x[1], y[1]};
+}
+
+template <int KIND>
+struct NllShape {
+  static constexpr bool kARows = KIND == kLogits || KIND == kProbs;  // m by rows
+  static constexpr bool kBRows = KIND != kWeight;
+};
+
+// One workgroup's tile of one of the products.  In each of them the entries that
+// lie side by side in the result are the rows (m) of the tile:
+//
+//     kLogits, kProbs   m: vocabulary   n: tokens      k: d
+//     kInput            m: d            n: tokens      k: vocabulary (piece, split)
+//     kWeight           m: d            n: vocabulary  k: tokens
+template <typename T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
+  typedef Product<T, NllShape<KIND>::kARows, NllShape<KIND>::kBRows, BM, BN, WM, WN, STAGES> P;
+  constexpr int kSize = sizeof(T);
+  __shared__ __attribute__((aligned(16))) char raw_lds[P::kLds];
+  char SMX_LDS* const lds = (char SMX_LDS*)raw_lds;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / 64);
+  const int lane = static_cast<int>(__lane_id()), half = lane / 32;
+  const int live = a.head->live;
+  const int rows = (live + BN - 1) / BN;  // tiles of tokens
+  const int left = min(a.vocab - a.from, a.piece);  // of the vocabulary
+  int mt, nt;
+  const int mtiles = KIND == kLogits  ? (a.vocab + BM - 1) / BM
+                     : KIND == kProbs ? a.piece / BM : (a.d + BM - 1) / BM;
+  const int ntiles = KIND == kWeight ? (left + BN - 1) / BN : rows;
+  if (!tile_of(blockIdx.x, mtiles, ntiles, &mt, &nt)) return;
+  const int m0 = mt * BM, n0 = nt * BN;
+  const int64_t packed_pitch = static_cast<int64_t>(a.padded_d) * kSize;
+  const int64_t g_pitch = static_cast<int64_t>(a.piece) * kSize;
+  const char* const weight = static_cast<const char*>(a.weight) +
+                             (KIND == kLogits ? 0 : a.from) * a.w_pitch;
+  P p;
+  if constexpr (KIND == kLogits || KIND == kProbs) {
+    typename P::A x(weight, a.w_pitch, m0, KIND == kLogits ? a.vocab : left, 0, wave);
+    typename P::B y(a.packed, packed_pitch, n0, a.padded_rows, 0, wave);
+    p.run(x, y, lds, a.d, wave);
+  } else if constexpr (KIND == kInput) {
+    // A split's share of the piece, in whole stages.
+    const int stages = (left + P::A::kK - 1) / P::A::kK;
+    const int s0 = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / a.splits);
+    const int s1 = static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / a.splits);
+    const int64_t k0 = static_cast<int64_t>(s0) * P::A::kK;
+    const int64_t k1 = min(static_cast<int64_t>(s1) * P::A::kK, static_cast<int64_t>(left));
+    typename P::A x(weight, a.w_pitch, m0, a.d, k0, wave);
+    typename P::B y(a.g, g_pitch, n0, a.padded_rows, k0, wave);
+    p.run(x, y, lds, max(k1 - k0, static_cast<int64_t>(0)), wave);
+  } else {
+    typename P::A x(a.packed, packed_pitch, m0, a.padded_d, 0, wave);
+    typename P::B y(a.g, g_pitch, n0, a.piece, 0, wave);
+    p.run(x, y, lds, live, wave);
+  }
+  const int mw = m0 + wave % WM * (BM / WM);  // the wavefront's first row
+  const int nw = n0 + wave / WM * (BN / WN) + lane % 32;
+  const int m4 = mw + 4 * half;  // of register 0
+  if constexpr (KIND == kLogits) {
+    f32x2 SMX_LDS* const stat = (f32x2 SMX_LDS*)lds;
+    // Rows past the vocabulary are no classes.
+    if (m0 + BM > a.vocab) {
+#pragma unroll
+      for (int i = 0; i < P::kMT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (m4 + 32 * i + 8 * (r / 4) + r % 4 >= a.vocab) {
+#pragma unroll
+            for (int j = 0; j < P::kNT; ++j) p.acc[i][j][r] = kNoLogit;
+          }
+    }
+#pragma unroll
+    for (int j = 0; j < P::kNT; ++j) {
+      const int row = nw + 32 * j;
+      const int label = a.token[row].label;
+      float m = kNoLogit;
+#pragma unroll
+      for (int i = 0; i < P::kMT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m = fmaxf(m, p.acc[i][j][r]);
+      m = fmaxf(m, half32_partner(m));
+      const float ref = m == kNoLogit ? 0.0f : m;
+      float t[8] = {};
+#pragma unroll
+      for (int i = 0; i < P::kMT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          t[r % 8] += __builtin_amdgcn_exp2f((p.acc[i][j][r] - ref) * kLog2eF);
+      float s = tree_sum(t);
+      s += half32_partner(s);
+      if (half == 0) stat[wave % WM * BN + row - n0] = f32x2{m, s};
+      // The label's logit, where it is one of the wavefront's.
+      const int rel = label - m4;
+      if (__ballot(label >= mw && label < mw + BM / WM) != 0) {
+#pragma unroll
+        for (int i = 0; i < P::kMT; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (rel == 32 * i + 8 * (r / 4) + r % 4) a.at[row] = p.acc[i][j][r];
+      }
+    }
+    __syncthreads();
+    for (int n = threadIdx.x; n < BN; n += 64 * WM * WN) {
+      f32x2 v = stat[n];
+#pragma unroll
+      for (int w = 1; w < WM; ++w) {
+        const f32x2 u = stat[w * BN + n];
+        const float m = fmaxf(v.x, u.x), ref = m == kNoLogit ? 0.0f : m;
+        v.y = v.y * __builtin_amdgcn_exp2f((v.x - ref) * kLog2eF) +
+              u.y * __builtin_amdgcn_exp2f((u.x - ref) * kLog2eF);
+        v.x = m;
+      }
+      a.part[static_cast<int64_t>(mt) * a.padded_rows + n0 + n] = v;
+    }
+  } else if constexpr (KIND == kProbs) {
+#pragma unroll
+    for (int j = 0; j < P::kNT; ++j) {
+      const int row = nw + 32 * j;
+      const NllToken k = a.token[row];
+      const int rel = k.label - a.from - m4;
+      const int rest = left - m4;
+      char* const out = a.g + row * g_pitch;
+#pragma unroll
+      for (int i = 0; i < P::kMT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 8) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int at = 32 * i + 8 * ((r + e) / 4) + e % 4;
+            v[e] = __builtin_amdgcn_exp2f((p.acc[i][j][r + e] - k.lse) * kLog2eF) * k.weight;
+            v[e] = rel == at ? k.label_g : v[e];
+            v[e] = at < rest ? v[e] : 0.0f;
+          }
+          if constexpr (kSize == 2) {
+            *reinterpret_cast<uint4*>(out + (mw + 32 * i + 2 * r + 8 * half) * 2) = strip8<T>(v);
+          } else {
+            float* const o = reinterpret_cast<float*>(out) + m4 + 32 * i + 2 * r;
+            *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(o + 8) = f32x4{v[4], v[5], v[6], v[7]};
+          }
+        }
+    }
+  } else if constexpr (KIND == kInput) {
+    float* const sums = a.sums + static_cast<int64_t>(blockIdx.y) * a.padded_rows * a.padded_d;
+#pragma unroll
+    for (int j = 0; j < P::kNT; ++j) {
+      float* const out = sums + static_cast<int64_t>(nw + 32 * j) * a.padded_d;
+#pragma unroll
+      for (int i = 0; i < P::kMT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int m = m4 + 32 * i + 2 * r;
+          if (m >= a.d) continue;
+          f32x4 v = {p.acc[i][j][r], p.acc[i][j][r + 1], p.acc[i][j][r + 2], p.acc[i][j][r + 3]};
+          f32x4* const o = reinterpret_cast<f32x4*>(out + m);
+          if (a.from > 0) v += *o;
+          *o = v;
+        }
+    }
+  } else {
+    const float unit = a.head->unit;
+#pragma unroll
+    for (int j = 0; j < P::kNT; ++j) {
+      const int row = nw + 32 * j;
+      char* const out = static_cast<char*>(a.dweight) +
+                        (static_cast<int64_t>(a.from) + row) * a.d * kSize;
+#pragma unroll
+      for (int i = 0; i < P::kMT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 8) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = p.acc[i][j][r + e] * unit;
+          if constexpr (kSize == 2) {
+            const uint4 strip = strip8<T>(v);
+            const int m = mw + 32 * i + 2 * r + 8 * half;
+            if (row < left && m < a.d) *reinterpret_cast<uint4*>(out + m * 2) = strip;
+          } else {
+            const int m = m4 + 32 * i + 2 * r;
+            float* const o = reinterpret_cast<float*>(out) + m;
+            if (row < left && m < a.d) *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
+            if (row < left && m + 8 < a.d)
+              *reinterpret_cast<f32x4*>(o + 8) = f32x4{v[4], v[5], v[6], v[7]};
+          }
+        }
+    }
+  }
+}
+
+// lse = M + ln S and loss = (M - x_label) + ln S from the tiles' statistics, in
+// binary64: 64 tokens per workgroup, four wavefronts over the tiles.
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_nll_join(NllArgs a) {
+  static_assert(WAVES == 4, "as summed up below");
+  __shared__ float m_lds[4][64];
+  __shared__ double s_lds[4][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int t = blockIdx.x * 64 + lane;
+  const int row = t < a.rows ? a.place[t] : -1;
+  float m = kNoLogit;
+  if (row >= 0)
+    for (int i = wave; i < a.tiles; i += 4)
+      m = fmaxf(m, a.part[static_cast<int64_t>(i) * a.padded_rows + row].x);
+  m_lds[wave][lane] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(m_lds[0][lane], m_lds[1][lane]), fmaxf(m_lds[2][lane], m_lds[3][lane]));
+  const float ref = m == kNoLogit ? 0.0f : m;
+  double s = 0.0;
+  if (row >= 0)
+    for (int i = wave; i < a.tiles; i += 4) {
+      const f32x2 v = a.part[static_cast<int64_t>(i) * a.padded_rows + row];
+      s += static_cast<double>(v.y * __builtin_amdgcn_exp2f((v.x - ref) * kLog2eF));
+    }
+  s_lds[wave][lane] = s;
+  __syncthreads();
+  if (wave != 0 || t >= a.rows) return;
+  s = (s_lds[0][lane] + s_lds[1][lane]) + (s_lds[2][lane] + s_lds[3][lane]);
+  float loss = 0.0f, lse = 0.0f;
+  if (row >= 0) {
+    const double log_s = log(s);
+    const bool bad = a.token[row].label < 0;
+    lse = static_cast<float>(m + log_s);
+    loss = bad ? __builtin_nanf("")
+               : static_cast<float>(static_cast<double>(m) - a.at[row] + log_s);
+  }
+  a.lse[t] = lse;
+  a.loss[t] = loss;
+}
+
+template <int UNUSED>
+__global__ __launch_bounds__(256) void k_nll_clear(uint4* out, int64_t strips) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < strips;
+       i += static_cast<int64_t>(gridDim.x) * 256)
+    out[i] = uint4{0, 0, 0, 0};
+}
+
+// dx of every token from the splits' sums: zeros for those without a loss.
+template <typename T>
+__global__ __launch_bounds__(256) void k_nll_input(NllArgs a) {
+  const int strips = a.d / 8;
+  const int64_t all = static_cast<int64_t>(a.rows) * strips;
+  const float unit = a.head->unit;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all;
+       i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int t = static_cast<int>(i / strips), c = static_cast<int>(i % strips) * 8;
+    const int row = a.place[t];
+    f32x4 lo = {}, hi = {};
+    if (row >= 0) {
+      for (int s = 0; s < a.splits; ++s) {
+        const float* p =
+            a.sums + (static_cast<int64_t>(s) * a.padded_rows + row) * a.padded_d + c;
+        lo += *reinterpret_cast<const f32x4*>(p);
+        hi += *reinterpret_cast<const f32x4*>(p + 4);
+      }
+    }
+    lo *= unit;
+    hi *= unit;
+    T* const out = static_cast<T*>(a.dx) + static_cast<int64_t>(t) * a.d + c;
+    typedef T T8 __attribute__((ext_vector_type(8)));
+    T8 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] = static_cast<T>(lo[j]);
+      v[4 + j] = static_cast<T>(hi[j]);
+    }
+    *reinterpret_cast<T8*>(out) = v;
+  }
+}
+
+}  // namespace smx

@@ -1,0 +1,19 @@
+// The compiled instances of the tile products behind the loss over a vocabulary,
+// each type in a source file of its own.
+#pragma once
+
+#include <stdint.h>
+
+namespace smx {
+
+// One of the products (kLogits .. kWeight of sm_linear_nll.hpp) and its shape.
+struct NllProduct {
+  const void* fn;
+  int bm, bn, threads;
+};
+
+NllProduct nll_product_f32(int kind, int64_t tokens);
+NllProduct nll_product_f16(int kind, int64_t tokens);
+NllProduct nll_product_bf16(int kind, int64_t tokens);
+
+}  // namespace smx
