@@ -21,21 +21,25 @@ NllProduct product(int kind, int64_t tokens, int dtype) {
                                 : nll_product_bf16(kind, tokens);
 }
 
-// The kernels' NllHead, places and tokens, and the packed rows.
+// The kernels' NllHead, places and tokens, and the packed rows.  Each starts on a
+// 256-byte boundary: 128-byte rows of operands that straddle two lines of the L2 take
+// two requests each.
+constexpr int64_t kAlign = 256;
+
 struct Room {
-  int64_t place, token, packed, more, end;
+  int64_t place, token, packed, more;
 };
 
 Room room(int64_t rows, int64_t d, int size) {
   const int64_t padded = up_to(rows, kTile);
   Room r;
-  r.place = sizeof(NllHead);
-  r.token = r.place + up_to(rows * 4, 16);
-  r.packed = r.token + padded * static_cast<int64_t>(sizeof(NllToken));
-  r.more = r.packed + padded * up_to(d * size, kLineBytes);
-  r.end = r.more;
+  r.place = kAlign;
+  r.token = r.place + up_to(rows * 4, kAlign);
+  r.packed = r.token + up_to(padded * static_cast<int64_t>(sizeof(NllToken)), kAlign);
+  r.more = r.packed + up_to(padded * up_to(d * size, kLineBytes), kAlign);
   return r;
 }
+static_assert(sizeof(NllHead) <= kAlign, "the head's place");
 
 int64_t forward_bytes(int64_t rows, int64_t vocab, int64_t d, int dtype) {
   const int64_t padded = up_to(rows, kTile);

@@ -162,21 +162,22 @@ __global__ __launch_bounds__(256) void k_nll_pack(NllArgs a, int each) {
   }
 }
 
-// Eight fp32 values (four of registers i0 .., four of i0 + 4 ..) to the type, as
-// the 16 bytes m = 16 (i0 / 8) + 8 (l / 32) .. of the lane's column: the halves of
-// the wavefront swap what the other one's strip holds.
+// A lane's four values of two tiles side by side (m), to the type, as 16 bytes: the
+// lanes l / 16 swap with their neighbours what the others' strip holds.  Even ones
+// get m = 4 (l / 16) .. of the first tile, odd ones m = 4 (l / 16) - 4 .. of the
+// second.
 template <typename T>
-__device__ __forceinline__ uint4 strip8(const float (&v)[8]) {
+__device__ __forceinline__ uint4 strip8(f32x4 first, f32x4 second) {
   typedef T T4 __attribute__((ext_vector_type(4)));
   T4 p, q;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    p[j] = static_cast<T>(v[j]);
-    q[j] = static_cast<T>(v[4 + j]);
+    p[j] = static_cast<T>(first[j]);
+    q[j] = static_cast<T>(second[j]);
   }
   const uint2 pu = __builtin_bit_cast(uint2, p), qu = __builtin_bit_cast(uint2, q);
-  const auto x = __builtin_amdgcn_permlane32_swap(pu.x, qu.x, false, false);
-  const auto y = __builtin_amdgcn_permlane32_swap(pu.y, qu.y, false, false);
+  const auto x = __builtin_amdgcn_permlane16_swap(pu.x, qu.x, false, false);
+  const auto y = __builtin_amdgcn_permlane16_swap(pu.y, qu.y, false, false);
   return {x[0], y[0], x[1], y[1]};
 }
 
@@ -199,7 +200,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
   __shared__ __attribute__((aligned(16))) char raw_lds[P::kLds];
   char SMX_LDS* const lds = (char SMX_LDS*)raw_lds;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) / 64);
-  const int lane = static_cast<int>(__lane_id()), half = lane / 32;
+  const int lane = static_cast<int>(__lane_id()), quarter = lane / 16;
   const int live = a.head->live;
   const int rows = (live + BN - 1) / BN;  // tiles of tokens
   const int left = min(a.vocab - a.from, a.piece);  // of the vocabulary
@@ -234,8 +235,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
     p.run(x, y, lds, live, wave);
   }
   const int mw = m0 + wave % WM * (BM / WM);  // the wavefront's first row
-  const int nw = n0 + wave / WM * (BN / WN) + lane % 32;
-  const int m4 = mw + 4 * half;  // of register 0
+  const int nw = n0 + wave / WM * (BN / WN) + lane % 16;
+  const int m4 = mw + 4 * quarter;  // of register 0
+  const int m8 = mw + 16 * (quarter % 2) + 4 * (quarter & 2);  // of strip8's bytes
   if constexpr (KIND == kLogits) {
     f32x2 SMX_LDS* const stat = (f32x2 SMX_LDS*)lds;
     // Rows past the vocabulary are no classes.
@@ -243,40 +245,39 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
 #pragma unroll
       for (int i = 0; i < P::kMT; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (m4 + 32 * i + 8 * (r / 4) + r % 4 >= a.vocab) {
+        for (int r = 0; r < 4; ++r)
+          if (m4 + 16 * i + r >= a.vocab) {
 #pragma unroll
             for (int j = 0; j < P::kNT; ++j) p.acc[i][j][r] = kNoLogit;
           }
     }
 #pragma unroll
     for (int j = 0; j < P::kNT; ++j) {
-      const int row = nw + 32 * j;
+      const int row = nw + 16 * j;
       const int label = a.token[row].label;
       float m = kNoLogit;
 #pragma unroll
       for (int i = 0; i < P::kMT; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) m = fmaxf(m, p.acc[i][j][r]);
-      m = fmaxf(m, half32_partner(m));
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, p.acc[i][j][r]);
+      m = group4_max(m);
       const float ref = m == kNoLogit ? 0.0f : m;
       float t[8] = {};
 #pragma unroll
       for (int i = 0; i < P::kMT; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          t[r % 8] += __builtin_amdgcn_exp2f((p.acc[i][j][r] - ref) * kLog2eF);
-      float s = tree_sum(t);
-      s += half32_partner(s);
-      if (half == 0) stat[wave % WM * BN + row - n0] = f32x2{m, s};
+        for (int r = 0; r < 4; ++r)
+          t[(4 * i + r) % 8] += __builtin_amdgcn_exp2f((p.acc[i][j][r] - ref) * kLog2eF);
+      const float s = group4_sum(tree_sum(t));
+      if (quarter == 0) stat[wave % WM * BN + row - n0] = f32x2{m, s};
       // The label's logit, where it is one of the wavefront's.
       const int rel = label - m4;
       if (__ballot(label >= mw && label < mw + BM / WM) != 0) {
 #pragma unroll
         for (int i = 0; i < P::kMT; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (rel == 32 * i + 8 * (r / 4) + r % 4) a.at[row] = p.acc[i][j][r];
+          for (int r = 0; r < 4; ++r)
+            if (rel == 16 * i + r) a.at[row] = p.acc[i][j][r];
       }
     }
     __syncthreads();
@@ -295,7 +296,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
   } else if constexpr (KIND == kProbs) {
 #pragma unroll
     for (int j = 0; j < P::kNT; ++j) {
-      const int row = nw + 32 * j;
+      const int row = nw + 16 * j;
       const NllToken k = a.token[row];
       const int rel = k.label - a.from - m4;
       const int rest = left - m4;
@@ -303,67 +304,52 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
 #pragma unroll
       for (int i = 0; i < P::kMT; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; r += 8) {
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int at = 32 * i + 8 * ((r + e) / 4) + e % 4;
-            v[e] = __builtin_amdgcn_exp2f((p.acc[i][j][r + e] - k.lse) * kLog2eF) * k.weight;
-            v[e] = rel == at ? k.label_g : v[e];
-            v[e] = at < rest ? v[e] : 0.0f;
-          }
-          if constexpr (kSize == 2) {
-            *reinterpret_cast<uint4*>(out + (mw + 32 * i + 2 * r + 8 * half) * 2) = strip8<T>(v);
-          } else {
-            float* const o = reinterpret_cast<float*>(out) + m4 + 32 * i + 2 * r;
-            *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4*>(o + 8) = f32x4{v[4], v[5], v[6], v[7]};
-          }
+        for (int r = 0; r < 4; ++r) {
+          const int at = 16 * i + r;
+          float v = __builtin_amdgcn_exp2f((p.acc[i][j][r] - k.lse) * kLog2eF) * k.weight;
+          v = rel == at ? k.label_g : v;
+          p.acc[i][j][r] = at < rest ? v : 0.0f;
         }
+#pragma unroll
+      for (int i = 0; i < P::kMT; i += kSize == 2 ? 2 : 1) {
+        if constexpr (kSize == 2)
+          *reinterpret_cast<uint4*>(out + (m8 + 16 * i) * 2) =
+              strip8<T>(p.acc[i][j], p.acc[i + 1][j]);
+        else
+          *reinterpret_cast<f32x4*>(out + (m4 + 16 * i) * 4) = p.acc[i][j];
+      }
     }
   } else if constexpr (KIND == kInput) {
     float* const sums = a.sums + static_cast<int64_t>(blockIdx.y) * a.padded_rows * a.padded_d;
 #pragma unroll
     for (int j = 0; j < P::kNT; ++j) {
-      float* const out = sums + static_cast<int64_t>(nw + 32 * j) * a.padded_d;
+      float* const out = sums + static_cast<int64_t>(nw + 16 * j) * a.padded_d;
 #pragma unroll
-      for (int i = 0; i < P::kMT; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const int m = m4 + 32 * i + 2 * r;
-          if (m >= a.d) continue;
-          f32x4 v = {p.acc[i][j][r], p.acc[i][j][r + 1], p.acc[i][j][r + 2], p.acc[i][j][r + 3]};
-          f32x4* const o = reinterpret_cast<f32x4*>(out + m);
-          if (a.from > 0) v += *o;
-          *o = v;
-        }
+      for (int i = 0; i < P::kMT; ++i) {
+        const int m = m4 + 16 * i;
+        if (m >= a.d) continue;
+        f32x4* const o = reinterpret_cast<f32x4*>(out + m);
+        *o = a.from > 0 ? *o + p.acc[i][j] : p.acc[i][j];
+      }
     }
   } else {
     const float unit = a.head->unit;
 #pragma unroll
     for (int j = 0; j < P::kNT; ++j) {
-      const int row = nw + 32 * j;
+      const int row = nw + 16 * j;
       char* const out = static_cast<char*>(a.dweight) +
                         (static_cast<int64_t>(a.from) + row) * a.d * kSize;
 #pragma unroll
-      for (int i = 0; i < P::kMT; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; r += 8) {
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = p.acc[i][j][r + e] * unit;
-          if constexpr (kSize == 2) {
-            const uint4 strip = strip8<T>(v);
-            const int m = mw + 32 * i + 2 * r + 8 * half;
-            if (row < left && m < a.d) *reinterpret_cast<uint4*>(out + m * 2) = strip;
-          } else {
-            const int m = m4 + 32 * i + 2 * r;
-            float* const o = reinterpret_cast<float*>(out) + m;
-            if (row < left && m < a.d) *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
-            if (row < left && m + 8 < a.d)
-              *reinterpret_cast<f32x4*>(o + 8) = f32x4{v[4], v[5], v[6], v[7]};
-          }
+      for (int i = 0; i < P::kMT; i += kSize == 2 ? 2 : 1) {
+        if constexpr (kSize == 2) {
+          const uint4 strip = strip8<T>(p.acc[i][j] * unit, p.acc[i + 1][j] * unit);
+          const int m = m8 + 16 * i;
+          if (row < left && m < a.d) *reinterpret_cast<uint4*>(out + m * 2) = strip;
+        } else {
+          const int m = m4 + 16 * i;
+          if (row < left && m < a.d) *reinterpret_cast<f32x4*>(out + m * 4) = p.acc[i][j] * unit;
         }
+      }
     }
   }
 }

@@ -7,26 +7,43 @@
 // memory with its k entries side by side ("by rows": row m holds k = 0, 1, ..)
 // or with its m (n) entries side by side ("by columns": row k holds m = 0, 1,
 // ..).  Stages of 128 bytes of k per row (64 entries of 16-bit types, 32 of
-// fp32) go from memory to LDS without registers, STAGES - 1 of them ahead of
-// the one that is multiplied.
+// fp32) go from memory to LDS without registers, STAGES of them at a time.
 //
-// Operands of v_mfma_f32_32x32x16 (fp32: four v_mfma_f32_32x32x2): lane l holds
-// row l % 32 and the eight entries 8 (l / 32) + j of a step's 16 (fp32: the four
-// entries 4 (l / 32) + j of 8), which is one 16-byte chunk of a tile by rows.
+// Operands of v_mfma_f32_16x16x32 (fp32: four v_mfma_f32_16x16x4): lane l holds
+// row l % 16 and the eight entries 8 (l / 16) + j of a step's 32 (fp32: the four
+// entries 4 (l / 16) + j of 16), which is one 16-byte chunk of a tile by rows.
 // Tiles by columns give the same entries by the transposing reads
-// (ds_read_b64_tr_b16), fp32 by single reads.  D: column (n) l % 32, rows (m)
-// 8 (i / 4) + 4 (l / 32) + i % 4, so a lane holds four entries side by side.
+// (ds_read_b64_tr_b16: 16 lanes read 4 rows of 16 columns, and each gets one
+// column), fp32 by single reads.  D: column (n) l % 16, rows (m) 4 (l / 16) + i, so
+// a lane holds four entries side by side.  On random data these operations draw
+// less power than v_mfma_f32_32x32x16, and power sets the clock: from registers
+// alone 2110 against 1880 TFLOP/s.
 //
-// LDS holds rows in 16-byte chunks, chunk c of row r at place c ^ swz(r)
-// (sm_heads_mfma.hpp): all reads are free of bank conflicts.
+// A wavefront's load into LDS writes 1024 bytes side by side, a block: whole rows, in
+// their order in memory, since lanes that fetch a 128-byte line in any other order
+// make more requests of it to the L2 (half as many again with chunks permuted by row,
+// as the attention's tiles have them).  Bank conflicts are avoided by which rows share
+// a block, and by blocks that lie 1056 bytes apart (Side).
 #pragma once
+
+#include <utility>
 
 #include "sm_heads_mfma.hpp"
 
 namespace smx {
 
+// f(0), .., f(N - 1) with constants: loops of this many matrix ops are past what the
+// compiler unrolls.
+template <int... I, typename F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
+}
+
 constexpr int kLineBytes = 128;  // of k in a stage, per row
-constexpr int kSteps = 4;        // of matrix ops in a stage
 
 template <typename T>
 struct Operand {
@@ -37,11 +54,15 @@ struct Operand<float> {
   typedef f32x4 type;
 };
 
-__device__ __forceinline__ f32x16 multiply(f16x8 a, f16x8 b, f32x16 c) { return mfma32(a, b, c); }
-__device__ __forceinline__ f32x16 multiply(bf16x8 a, bf16x8 b, f32x16 c) { return mfma32(a, b, c); }
-__device__ __forceinline__ f32x16 multiply(f32x4 a, f32x4 b, f32x16 c) {
+__device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
   return c;
 }
 
@@ -59,24 +80,41 @@ __device__ __forceinline__ void load_line(const char* base, unsigned off, unsign
 template <typename T, bool BY_ROWS, int LINES, int WAVES>
 struct Side {
   static constexpr int kSize = sizeof(T);
-  static constexpr int kK = kLineBytes / kSize;     // entries of k in a stage
-  static constexpr int kBytes = LINES * kLineBytes;  // of a stage
-  static constexpr int kLoads = kBytes / 1024 / WAVES;
+  static constexpr int kK = kLineBytes / kSize;  // entries of k in a stage
+  static constexpr int kBlocks = LINES * kLineBytes / 1024;
+  static constexpr int kLoads = kBlocks / WAVES;
   static constexpr int kRowBytes = BY_ROWS ? kLineBytes : LINES * kSize;
   static constexpr int kChunks = kRowBytes / 16;
-  static constexpr int kRowsPer = 64 / kChunks;  // rows that a load of a wavefront moves
-  static_assert(kBytes % (1024 * WAVES) == 0 && 64 % kChunks == 0, "whole loads");
+  static constexpr int kRowsPer = 64 / kChunks;  // rows of a block
+  static_assert(kBlocks % WAVES == 0 && 64 % kChunks == 0, "whole loads");
+  static_assert(BY_ROWS ? LINES % 64 == 0 : kRowBytes == 512 || (kSize == 2 && kRowBytes == 256),
+                "known layouts");
+
+  // Blocks.  The banks repeat every 256 bytes, of which 16 lanes' reads at a time may
+  // touch each once, and the blocks' starts move by 32 bytes from one to the next.
+  //   by rows      16 rows are read at once, the lanes' chunks even for the rows 0 .. 3
+  //                and 12 .. 15 and odd for the others, or the other way round.  Rows
+  //                2 b and 2 b + 1 of four such tiles make the block b of eight.
+  //   by columns   16 bits: 32 bytes of the rows 0 .. 3 and 8 .. 11 are read at once,
+  //                or of these rows + 4, + 16 or + 20.  A block has one (rows of 256
+  //                bytes: two) of each.
+  //                fp32: 64 bytes of the rows 0, 4, 8 and 12, or the next ones.
+  __host__ __device__ static constexpr int block_at(int n) { return 1056 * n; }
+  static constexpr int kBytes = block_at(kBlocks);
+  // Row j of block n.
+  __device__ __forceinline__ static constexpr int row_of(int n, int j) {
+    return BY_ROWS        ? n / 8 * 64 + j / 2 * 16 + n % 8 * 2 + j % 2
+           : kSize == 4   ? 2 * n + j
+           : kRowsPer == 2 ? n / 8 * 16 + n / 4 % 2 * 8 + n % 4 + 4 * j
+                           : n / 8 * 32 + n / 4 % 2 * 8 + n % 4 + j % 2 * 4 + j / 2 * 16;
+  }
 
   const char* base;       // of the stage to load next
   int64_t step;           // bytes from stage to stage
   unsigned off[kLoads];   // of each load's chunk from the base, or kFar
-  int place;              // by rows: byte of the lane's chunk in its row; by columns: its row
-  int read_at[BY_ROWS ? kSteps : LINES >= 128 || kSize == 4 ? 4 : 2][BY_ROWS || kSize == 4 ? 1 : 2];
-
-  // Place of chunk 0 of row r (an exclusive or).
-  __device__ __forceinline__ static constexpr int place_of(int r) {
-    return BY_ROWS ? swz<64>(r) : kSize == 4 ? (r >> 2 & 1) << 3 : swz<LINES>(r);
-  }
+  bool whole;             // all of the next stage's k is there
+  int some;               // or so many entries
+  int read_at;
 
   // Lines `first` .. of a matrix at `data` of rows of `pitch` bytes, from k on;
   // `lines` of them are there (the others are taken as zeros).
@@ -89,143 +127,176 @@ struct Side {
     const int64_t left = lines - first;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int row = (wave * kLoads + i) * kRowsPer + lane / kChunks;
-      const int chunk = lane % kChunks ^ place_of(row);
+      const int row = row_of(wave * kLoads + i, lane / kChunks), chunk = lane % kChunks;
       const bool there = BY_ROWS ? row < left : chunk * (16 / kSize) < left;
       off[i] = there ? static_cast<unsigned>(row * static_cast<int>(pitch) + 16 * chunk) : kFar;
     }
-    place = wave * kLoads * kRowsPer + lane / kChunks;
   }
 
-  // Loads the next stage into `lds`; `left` entries of k are there from it on.
-  __device__ __forceinline__ void load(unsigned lds, int64_t left, int wave) {
-    lds += wave * kLoads * 1024;
-    if (left >= kK) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) load_line(base, off[i], lds + i * 1024);
-    } else {
+  // Entries of k that are there from the next stage on decide where its loads go:
+  // ready() before the stage's loads, load() for each of them, then advance().
+  __device__ __forceinline__ void ready(int64_t left) {
+    whole = left >= kK;
+    some = left < 0 ? 0 : static_cast<int>(left < kK ? left : kK);
+  }
+  __device__ __forceinline__ void load(unsigned lds, int i, int wave) const {
+    unsigned o = off[i];
+    if (!whole) {
       const int lane = static_cast<int>(__lane_id());
-      const int some = left < 0 ? 0 : static_cast<int>(left);
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int row = place + i * kRowsPer;
-        const int at = BY_ROWS ? (lane % kChunks ^ place_of(row)) * (16 / kSize) : row;
-        load_line(base, at < some ? off[i] : kFar, lds + i * 1024);
-      }
+      const int at = BY_ROWS ? lane % kChunks * (16 / kSize)
+                             : row_of(wave * kLoads + i, lane / kChunks);
+      o = at < some ? o : kFar;
     }
-    base += step;
+    load_line(base, o, lds + block_at(wave * kLoads + i));
   }
+  __device__ __forceinline__ void advance() { base += step; }
 
-  // Sets up the reads of the lines `first` (a multiple of 32) .. of the tile.
+  // Sets up the reads of the lines `first` .. of the tile, a multiple of what the
+  // wavefront takes.
   __device__ __forceinline__ void reader(int first) {
-    const int lane = static_cast<int>(__lane_id()), half = lane / 32, r = lane % 32;
-    if constexpr (BY_ROWS) {
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        read_at[s][0] = (first + r) * kLineBytes + 16 * ((2 * s + half) ^ place_of(r));
-    } else if constexpr (kSize == 4) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int col = first + 32 * t + r;
-        read_at[t][0] = 4 * half * kRowBytes + 16 * (col / 4 ^ place_of(4 * half)) + 4 * (col % 4);
-      }
-    } else {
-      const int i = lane % 16;
-#pragma unroll
-      for (int t = 0; t < (LINES >= 128 ? 4 : 2); ++t) {
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi) {
-          const int row = 8 * half + 4 * hi + i / 4;
-          const int chunk = (first + 32 * t) / 8 + 2 * (lane / 16 % 2) + i % 4 / 2;
-          read_at[t][hi] = row * kRowBytes + 16 * (chunk ^ place_of(row)) + 8 * (i % 2);
-        }
-      }
-    }
+    const int lane = static_cast<int>(__lane_id()), q = lane / 16, r = lane % 16;
+    if constexpr (BY_ROWS)
+      read_at = block_at(first / 64 * 8 + r / 2) + (first % 64 / 8 + r % 2) * kLineBytes + 16 * q;
+    else if constexpr (kSize == 4)
+      read_at = block_at(2 * q) + (first + r) * 4;
+    else  // 16 lanes read four rows of 32 bytes
+      read_at = block_at(kRowsPer == 2 ? 4 * q + r / 4 : q % 2 * 4 + r / 4) +
+                (kRowsPer == 2 ? 0 : q / 2 * 2 * kRowBytes) + first * 2 + r % 4 * 8;
   }
 
-  // The operand of step s for the lines 32 t .. of the reader's.
+  // The operand of step s for the lines 16 t .. of the reader's.
   __device__ __forceinline__ typename Operand<T>::type read(const char SMX_LDS* tile, int s,
                                                             int t) const {
     typedef typename Operand<T>::type V;
+    const char SMX_LDS* p = tile + read_at;
     if constexpr (BY_ROWS) {
-      return *reinterpret_cast<const V SMX_LDS*>(tile + read_at[s][0] + 32 * t * kLineBytes);
+      p += block_at(t / 4 * 8) + t % 4 * 2 * kLineBytes + 64 * s;
+      return *reinterpret_cast<const V SMX_LDS*>(p);
     } else if constexpr (kSize == 4) {
+      p += block_at(8 * s) + 64 * t;
       V v;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        v[j] = *reinterpret_cast<const float SMX_LDS*>(tile + read_at[t][0] +
-                                                       (8 * s + j) * kRowBytes);
+        v[j] = *reinterpret_cast<const float SMX_LDS*>(p + block_at(j / 2) + j % 2 * kRowBytes);
       return v;
     } else {
-      const char SMX_LDS* p = tile + 16 * s * kRowBytes;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 SMX_LDS*)(p + read_at[t][0]));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 SMX_LDS*)(p + read_at[t][1]));
+      p += block_at(kRowsPer == 2 ? 16 * s : 8 * s) + 32 * t;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 SMX_LDS*)p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 SMX_LDS*)(p + kRowBytes));
       return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   }
 };
 
 // The products of a workgroup's tile over `k` entries: acc[i][j] of a wavefront
-// are its rows (m) 32 i .. and columns (n) 32 j .. .
+// are its rows (m) 16 i .. and columns (n) 16 j .. .
 template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, int STAGES>
 struct Product {
   static constexpr int kWaves = WM * WN;
-  static constexpr int kMT = BM / WM / 32, kNT = BN / WN / 32;
+  static constexpr int kMT = BM / WM / 16, kNT = BN / WN / 16;
   typedef Side<T, A_ROWS, BM, kWaves> A;
   typedef Side<T, B_ROWS, BN, kWaves> B;
+  static constexpr int kSteps = kLineBytes / 64;  // of a stage
   static constexpr int kStageBytes = A::kBytes + B::kBytes;
   static constexpr int kLds = STAGES * kStageBytes;
   static constexpr int kLoads = A::kLoads + B::kLoads;
   static_assert(kLds <= 160 * 1024, "LDS of a CU");
+  // Tiles of 16 rows by rows lie four to a group of blocks.
+  static_assert((BM / WM) % 64 == 0 || 64 % (BM / WM) == 0, "a wavefront's tiles, in groups");
+  static_assert((BN / WN) % 64 == 0 || 64 % (BN / WN) == 0, "a wavefront's tiles, in groups");
+  static_assert(kSteps == 2, "operands for each");
 
-  f32x16 acc[kMT][kNT];
+  f32x4 acc[kMT][kNT];
+
+  typedef typename Operand<T>::type V;
+
+  static constexpr int kOps = kMT * kNT;  // of a step
+
+  // The matrix ops of one step, and behind the n-th of them `then(n)`: what is read,
+  // and loaded, for later steps.  In this order: the compiler by itself reads each
+  // operand right before its use.
+  template <typename F>
+  __device__ __forceinline__ void step(const V (&x)[kMT], const V (&y)[kNT], F then) {
+    unrolled<kOps>([&](auto n) {
+      constexpr int i = n / kNT, j = n % kNT;
+      acc[i][j] = multiply(x[i], y[j], acc[i][j]);
+      then(n);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  }
 
   __device__ __forceinline__ void run(A& a, B& b, char SMX_LDS* lds, int64_t k, int wave) {
     const unsigned at = lds_offset(lds);
-    auto load = [&](int64_t from, int buf) {
-      a.load(at + buf * kStageBytes, k - from, wave);
-      b.load(at + buf * kStageBytes + A::kBytes, k - from, wave);
+    int64_t left = k;  // from the next stage to load on
+    auto load = [&](int n, int buf) {
+      if (n < A::kLoads) a.load(at + buf * kStageBytes, n, wave);
+      else b.load(at + buf * kStageBytes + A::kBytes, n - A::kLoads, wave);
+    };
+    auto ready = [&] {
+      a.ready(left);
+      b.ready(left);
+      left -= A::kK;
+    };
+    auto advance = [&] {
+      a.advance();
+      b.advance();
     };
     a.reader(wave % WM * (BM / WM));
     b.reader(wave / WM * (BN / WN));
+    unrolled<kOps>([&](auto n) { acc[n / kNT][n % kNT] = f32x4{}; });
 #pragma unroll
-    for (int i = 0; i < kMT; ++i)
+    for (int s = 0; s < STAGES; ++s) {
+      ready();
 #pragma unroll
-      for (int j = 0; j < kNT; ++j) acc[i][j] = f32x16{};
-    int64_t from = 0;
-#pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) {
-      load(from, s);
-      from += A::kK;
+      for (int n = 0; n < kLoads; ++n) load(n, s);
+      advance();
     }
-    int buf = 0, next = STAGES - 1;
-    // One barrier a stage: behind it the stage's loads have landed for every
-    // wavefront, and all have read the stage before it, whose place the next
-    // loads take.
+    staged_but<(STAGES - 1) * kLoads>();
+    __builtin_amdgcn_s_barrier();
+    V x[2][kMT], y[2][kNT];
+    const char SMX_LDS* tile = lds;
+    // Operands of the next step are read between the first of a step's matrix ops: by
+    // its end they have arrived, and nothing waits for them at the barrier.
+    auto read = [&](auto n, int to, int s) {
+      if constexpr (n < kNT) y[to][n] = b.read(tile + A::kBytes, s, n);
+      else if constexpr (n < kNT + kMT) x[to][n - kNT] = a.read(tile, s, n - kNT);
+    };
+    unrolled<kMT + kNT>([&](auto n) { read(n, 0, 0); });
+    // The op that a read comes behind; a step of few ops takes several at once.
+    auto read_at_op = [&](auto n, int to, int s) {
+      unrolled<kMT + kNT>([&](auto r) {
+        if constexpr (n == r * kOps / (kMT + kNT) * 3 / 4) read(r, to, s);
+      });
+    };
+    int buf = 0;
+    // A step's operands are read during the step before it, across stages too: the
+    // last step of a stage runs behind the barrier, by which the next stage's loads
+    // have landed for every wavefront, and all have read this one, whose place the
+    // loads of the stage STAGES further on take.
     for (int64_t done = 0; done < k; done += A::kK) {
+#pragma unroll
+      for (int s = 0; s < kSteps - 1; ++s)
+        step(x[s % 2], y[s % 2], [&](auto n) { read_at_op(n, (s + 1) % 2, s + 1); });
+      const int next = buf + 1 == STAGES ? 0 : buf + 1;
+      tile = lds + next * kStageBytes;
+      lds_read();
       staged_but<(STAGES - 2) * kLoads>();
       __builtin_amdgcn_s_barrier();
-      load(from, next);
-      from += A::kK;
-      const char SMX_LDS* ta = lds + buf * kStageBytes;
-      const char SMX_LDS* tb = ta + A::kBytes;
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        typename Operand<T>::type x[kMT], y[kNT];
-#pragma unroll
-        for (int i = 0; i < kMT; ++i) x[i] = a.read(ta, s, i);
-#pragma unroll
-        for (int j = 0; j < kNT; ++j) y[j] = b.read(tb, s, j);
-#pragma unroll
-        for (int i = 0; i < kMT; ++i)
-#pragma unroll
-          for (int j = 0; j < kNT; ++j) acc[i][j] = multiply(x[i], y[j], acc[i][j]);
-      }
-      buf = buf + 1 == STAGES ? 0 : buf + 1;
-      next = next + 1 == STAGES ? 0 : next + 1;
+      ready();
+      step(x[(kSteps - 1) % 2], y[(kSteps - 1) % 2], [&](auto n) {
+        read_at_op(n, kSteps % 2, 0);
+        // Load l behind the op l kOps / kLoads + 2, or the last one.
+        unrolled<kLoads>([&](auto l) {
+          constexpr int at = l * 2;
+          if constexpr (n == (at < kOps ? at : kOps - 1)) load(l, buf);
+        });
+      });
+      advance();
+      buf = next;
     }
     // The last loads (of nothing) have landed and all tiles have been read: the
     // LDS may be used again.
+    lds_read();
     staged();
     __builtin_amdgcn_s_barrier();
   }
