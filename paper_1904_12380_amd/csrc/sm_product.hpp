@@ -218,7 +218,8 @@ struct Product {
   template <typename F>
   __device__ __forceinline__ void step(const V (&x)[kMT], const V (&y)[kNT], F then) {
     unrolled<kOps>([&](auto n) {
-      constexpr int i = n / kNT, j = n % kNT;
+      // Rows in turn from either end: one operand stays from op to op.
+      constexpr int i = n / kNT, j = i % 2 == 0 ? n % kNT : kNT - 1 - n % kNT;
       acc[i][j] = multiply(x[i], y[j], acc[i][j]);
       then(n);
       __builtin_amdgcn_sched_barrier(0);
