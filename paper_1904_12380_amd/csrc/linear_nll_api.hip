@@ -15,10 +15,11 @@ using namespace smx_host;
 
 constexpr int64_t kTile = 256;  // all tiles' sizes divide it
 
-NllProduct product(int kind, int64_t tokens, int dtype) {
-  return dtype == SOFTMAX_F32   ? nll_product_f32(kind, tokens)
-         : dtype == SOFTMAX_F16 ? nll_product_f16(kind, tokens)
-                                : nll_product_bf16(kind, tokens);
+// The product of `kind` for m x n entries of the result.
+NllProduct product(int kind, int64_t m, int64_t n, int dtype) {
+  return dtype == SOFTMAX_F32   ? nll_product_f32(kind, m, n)
+         : dtype == SOFTMAX_F16 ? nll_product_f16(kind, m, n)
+                                : nll_product_bf16(kind, m, n);
 }
 
 // The kernels' NllHead, places and tokens, and the packed rows.  Each starts on a
@@ -43,31 +44,32 @@ static_assert(sizeof(NllHead) <= kAlign, "the head's place");
 
 int64_t forward_bytes(int64_t rows, int64_t vocab, int64_t d, int dtype) {
   const int64_t padded = up_to(rows, kTile);
-  const int64_t tiles = ceil_div(vocab, product(kLogits, rows, dtype).bm);
+  const int64_t tiles = ceil_div(vocab, product(kLogits, vocab, rows, dtype).bm);
   return room(rows, d, dtype_size(dtype)).more + padded * 4 + tiles * padded * 8;
 }
 
 // The piece of the vocabulary whose g is kept at a time: what fits kPieceBytes, in
-// equal pieces.
+// whole rounds of dweight's tiles over the CUs (8192 tokens x 50001 x 2048 of bf16: 8
+// rounds in two equal pieces, 7 in pieces of 128 and 68 tiles of the vocabulary).
+// Pieces of 128 MiB, which the last cache holds, were slower: 1215 against 1254
+// TFLOP/s there.
 constexpr int64_t kPieceBytes = int64_t(512) << 20;
+constexpr int64_t kCus = 256;  // of MI355X: workspaces and orders of sums go by sizes alone
 
-int64_t piece_of(int64_t rows, int64_t vocab, int size) {
+int64_t piece_of(int64_t rows, int64_t vocab, int64_t d, int size) {
   const int64_t most = std::clamp<int64_t>(kPieceBytes / size / up_to(rows, kTile) / kTile, 1, 4096);
   const int64_t tiles = ceil_div(vocab, kTile);
-  return ceil_div(tiles, ceil_div(tiles, most)) * kTile;
+  if (tiles <= most) return tiles * kTile;
+  const int64_t round = std::max<int64_t>(kCus / ceil_div(d, kTile), 1);
+  return (most > round ? most - most % round : most) * kTile;
 }
 
-// Splits of a piece's rows for dx: as few as leave at most a tenth of the device
-// idle, or else those that leave the least; a split has eight stages or more.  The
-// number of CUs is MI355X's: the order of the sums, and the workspace, go by sizes
-// alone.
-constexpr int64_t kCus = 256;
-
-int64_t splits_of(int64_t rows, int64_t piece, int64_t d, int dtype) {
-  const NllProduct p = product(kInput, rows, dtype);
-  const int64_t tiles = ceil_div(rows, p.bn) * ceil_div(d, p.bm);
-  const int64_t stages = piece * dtype_size(dtype) / kLineBytes;
-  const int64_t most = std::clamp<int64_t>(stages / 8, 1, 64);
+// Splits of the sums behind a product's tiles: as few as leave at most a tenth of the
+// device idle, or else those that leave the least; a split has four stages or more.
+int64_t splits_of(const NllProduct& p, int64_t m, int64_t n, int64_t k, int dtype) {
+  const int64_t tiles = ceil_div(m, p.bm) * ceil_div(n, p.bn);
+  const int64_t stages = ceil_div(k * dtype_size(dtype), kLineBytes);
+  const int64_t most = std::clamp<int64_t>(stages / 4, 1, 64);
   int64_t best = 1;
   double full = 0.0;
   for (int64_t s = 1; s <= most && full < 0.9; ++s) {
@@ -81,18 +83,24 @@ int64_t splits_of(int64_t rows, int64_t piece, int64_t d, int dtype) {
 }
 
 struct Backward {
-  int64_t g, sums, end, piece, splits;
+  int64_t g, rest, sums, w_sums, end, piece, splits, w_splits;
 };
 
 Backward backward_room(int64_t rows, int64_t vocab, int64_t d, int dtype) {
   const int size = dtype_size(dtype);
   const int64_t padded = up_to(rows, kTile);
   Backward b;
-  b.piece = piece_of(rows, vocab, size);
-  b.splits = splits_of(rows, b.piece, d, dtype);
+  b.piece = piece_of(rows, vocab, d, size);
+  b.splits = splits_of(product(kInput, d, rows, dtype), d, rows, b.piece, dtype);
+  // dweight is many tiles, but for a small vocabulary.
+  const NllProduct w = product(kWeight, d, b.piece, dtype);
+  const bool few = ceil_div(d, w.bm) * ceil_div(b.piece, w.bn) < kCus / 2;
+  b.w_splits = few ? splits_of(w, d, b.piece, rows, dtype) : 1;
   b.g = room(rows, d, size).more;
-  b.sums = b.g + padded * b.piece * size;
-  b.end = b.sums + b.splits * padded * up_to(d * size, kLineBytes) / size * 4;
+  b.rest = b.g + padded * b.piece * size;
+  b.sums = b.rest + (size == 2 ? kTwoParts * b.piece * size : 0);
+  b.w_sums = b.sums + b.splits * padded * up_to(d * size, kLineBytes) / size * 4;
+  b.end = b.w_sums + (b.w_splits > 1 ? b.w_splits * b.piece * d * 4 : 0);
   return b;
 }
 
@@ -186,7 +194,7 @@ SOFTMAX_API int softmax_linear_nll_fwd(const void* x, int64_t x_stride, const vo
   set_call(&a, x, x_stride, weight, w_stride, labels, rows, vocab, d, ignore, size, workspace);
   a.loss = loss;
   a.lse = lse;
-  const NllProduct p = product(kLogits, rows, dtype);
+  const NllProduct p = product(kLogits, vocab, rows, dtype);
   a.tiles = static_cast<int>(ceil_div(vocab, p.bm));
   a.at = reinterpret_cast<float*>(static_cast<char*>(workspace) + room(rows, d, size).more);
   a.part = reinterpret_cast<f32x2*>(a.at + a.padded_rows);
@@ -195,7 +203,8 @@ SOFTMAX_API int softmax_linear_nll_fwd(const void* x, int64_t x_stride, const vo
   if (e == hipSuccess) e = multiply_tiles(p, vocab, rows, 1, &a, stream);
   if (e == hipSuccess) {
     void* args[] = {&a};
-    e = start(reinterpret_cast<const void*>(&k_nll_join<4>), ceil_div(rows, 64), 1, 256, args,
+    e = start(reinterpret_cast<const void*>(&k_nll_join<16>), ceil_div(rows, kJoinTokens), 1,
+              16 * kJoinTokens, args,
               stream);
   }
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
@@ -250,22 +259,32 @@ SOFTMAX_API int softmax_linear_nll_bwd(const float* dloss, const void* x, int64_
   a.dx = dx;
   a.dweight = dweight;
   a.g = static_cast<char*>(workspace) + b.g;
+  a.g_rest = static_cast<char*>(workspace) + b.rest;
   a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + b.sums);
+  a.w_sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + b.w_sums);
   a.piece = static_cast<int>(b.piece);
   a.splits = static_cast<int>(b.splits);
+  a.w_splits = static_cast<int>(b.w_splits);
   if (dx == nullptr && dweight == nullptr) return SOFTMAX_OK;
   hipError_t e = pack<true>(&a, dtype, stream);
+  void* args[] = {&a};
   for (int64_t from = 0; from < vocab && e == hipSuccess; from += b.piece) {
     a.from = static_cast<int>(from);
     const int64_t left = std::min(vocab - from, b.piece);
-    e = multiply_tiles(product(kProbs, rows, dtype), b.piece, rows, 1, &a, stream);
+    e = multiply_tiles(product(kProbs, b.piece, rows, dtype), left, rows, 1, &a, stream);
     if (e == hipSuccess && dx != nullptr)
-      e = multiply_tiles(product(kInput, rows, dtype), d, rows, b.splits, &a, stream);
+      e = multiply_tiles(product(kInput, d, rows, dtype), d, rows, b.splits, &a, stream);
     if (e == hipSuccess && dweight != nullptr)
-      e = multiply_tiles(product(kWeight, rows, dtype), d, left, 1, &a, stream);
+      e = multiply_tiles(product(kWeight, d, b.piece, dtype), d, left, b.w_splits, &a, stream);
+    if (e == hipSuccess && dweight != nullptr && b.w_splits > 1) {
+      const void* fn = dtype == SOFTMAX_F32 ? reinterpret_cast<const void*>(&k_nll_weight<float>)
+                       : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_nll_weight<f16>)
+                                              : reinterpret_cast<const void*>(&k_nll_weight<bf16>);
+      e = start(fn, std::min<int64_t>(ceil_div(b.piece * d / 4, 256), 16 * kCus), 1, 256, args,
+                stream);
+    }
   }
   if (e == hipSuccess && dx != nullptr) {
-    void* args[] = {&a};
     const void* fn = dtype == SOFTMAX_F32   ? reinterpret_cast<const void*>(&k_nll_input<float>)
                      : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_nll_input<f16>)
                                             : reinterpret_cast<const void*>(&k_nll_input<bf16>);

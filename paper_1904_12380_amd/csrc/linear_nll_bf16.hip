@@ -3,6 +3,8 @@
 
 namespace smx {
 
-NllProduct nll_product_bf16(int kind, int64_t tokens) { return nll_product_16<bf16>(kind, tokens); }
+NllProduct nll_product_bf16(int kind, int64_t m, int64_t n) {
+  return nll_product_of<bf16>(kind, m, n);
+}
 
 }  // namespace smx

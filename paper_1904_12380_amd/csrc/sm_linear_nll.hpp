@@ -25,6 +25,11 @@
 // - 1 itself, not the product with 1 / tokens, whose rounding would be the same for
 // all tokens and not average out.  For fp16 it is 2^14 times as large on top: fp16
 // then holds 11 bits of it down to 2^-28 of the largest.
+//
+// A rounding of g averages out over the terms of a sum, unless one of them makes up
+// most of it.  Of dx that is the label's, and k_nll_input adds what its rounding left.
+// Of dweight any token's may be where there are few: up to kTwoParts tokens g is kept
+// in two parts of the type, and both products take both.
 #pragma once
 
 #include "sm_product.hpp"
@@ -73,15 +78,27 @@ struct NllArgs {
   f32x2* part;            // forward: (max, sum) [tiles, padded_rows]
   float* at;              // forward: the label's logit [padded_rows]
   char* g;                // backward: [padded_rows, piece] of the type
+  char* g_rest;           // [kTwoParts, piece]: what the rounding of g left
   float* sums;            // backward: [splits, padded_rows, padded_d]
+  float* w_sums;          // backward, w_splits > 1: [w_splits, piece, d]
   int tiles;              // tiles of the vocabulary that `part` has
   int from, piece;        // backward: first row of the piece, and its padded length
-  int splits;
+  int splits;             // of the piece's rows, for dx
+  int w_splits;           // of the tokens, for dweight
 };
 
-// The largest finite |dloss| is a power of two times this much in g.
+// What the largest finite |dloss| becomes in g.
 template <typename T>
 constexpr float kUnitUp = __is_same(T, f16) ? 0x1p14f : 1.0f;
+
+// Tokens with a loss up to which g of 16-bit types is kept in two parts.  The products
+// are bound by memory up to about as many: 256 tokens x 50001 x 2048 of bf16 take 1.1
+// times as long as with one part, 512 would take 1.4 times.
+constexpr int kTwoParts = 256;
+template <typename T>
+__device__ __forceinline__ int parts_of(int live) {
+  return sizeof(T) == 2 && live <= kTwoParts ? 2 : 1;
+}
 
 constexpr int kPackTokens = 16;  // fewest tokens of a workgroup
 
@@ -95,9 +112,11 @@ __global__ __launch_bounds__(256) void k_nll_pack(NllArgs a, int each) {
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
   const int first = blockIdx.x * each, last = min(first + each, a.rows);
   int count = 0;
+#pragma unroll 8
   for (int t = tid; t < first; t += 256) count += a.labels[t] != a.ignore;
   float most = 0.0f;
   if constexpr (BACK) {
+#pragma unroll 8
     for (int t = tid; t < a.rows; t += 256) {
       const float w = fabsf(a.dloss[t]);
       if (w <= 3.402823466e38f && a.labels[t] != a.ignore) most = fmaxf(most, w);
@@ -113,10 +132,9 @@ __global__ __launch_bounds__(256) void k_nll_pack(NllArgs a, int each) {
   float unit = 1.0f;
   if constexpr (BACK) {
     most = fmaxf(fmaxf(most_lds[0], most_lds[1]), fmaxf(most_lds[2], most_lds[3]));
-    // A |dloss| below the normal numbers is taken as it is.
+    // A |dloss| far below the normal numbers is taken as it is.
     unit = most < 0x1p-100f ? 1.0f : most;
   }
-  // Each wavefront copies a quarter of the tokens, all of them know all places.
   const int chunks = a.padded_d * static_cast<int>(sizeof(T)) / 16;
   const int whole = a.d * static_cast<int>(sizeof(T)) / 16;
   for (int t0 = first; t0 < last; t0 += 64) {
@@ -140,26 +158,29 @@ __global__ __launch_bounds__(256) void k_nll_pack(NllArgs a, int each) {
         a.token[row] = k;
       }
     }
+    // Each wavefront copies every fourth token of the 64.
     for (int i = wave; i < 64 && t0 + i < last; i += 4) {
       if (!(mask >> i & 1)) continue;
       const int64_t to = count + __popcll(mask & ((uint64_t(1) << i) - 1));
       const uint4* from = reinterpret_cast<const uint4*>(static_cast<const char*>(a.x) +
                                                          (t0 + i) * a.x_pitch);
       uint4* out = reinterpret_cast<uint4*>(a.packed) + to * chunks;
-      for (int c = lane; c < chunks; c += 64) out[c] = c < whole ? from[c] : uint4{0, 0, 0, 0};
+      for (int c0 = lane; c0 < chunks; c0 += 256) {
+        uint4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          v[u] = uint4{0, 0, 0, 0};
+          if (c0 + 64 * u < whole) v[u] = from[c0 + 64 * u];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (c0 + 64 * u < chunks) out[c0 + 64 * u] = v[u];
+      }
     }
     count += __popcll(mask);
   }
-  if (last != a.rows) return;
-  // The last workgroup knows the number of tokens, and clears the rows up to the
-  // end of their last tile.
-  if (tid == 0) *a.head = {count, unit / kUnitUp<T>, {0, 0}};
-  const int end = min((count + 255) / 256 * 256, a.padded_rows);
-  for (int r = count + wave; r < end; r += 4) {
-    if (lane == 0) a.token[r] = {INFINITY, 0.0f, 0.0f, -1};
-    uint4* out = reinterpret_cast<uint4*>(a.packed) + static_cast<int64_t>(r) * chunks;
-    for (int c = lane; c < chunks; c += 64) out[c] = uint4{0, 0, 0, 0};
-  }
+  // The last workgroup knows the number of tokens.
+  if (last == a.rows && tid == 0) *a.head = {count, unit / kUnitUp<T>, {0, 0}};
 }
 
 // A lane's four values of two tiles side by side (m), to the type, as 16 bytes: the
@@ -179,6 +200,15 @@ __device__ __forceinline__ uint4 strip8(f32x4 first, f32x4 second) {
   const auto x = __builtin_amdgcn_permlane16_swap(pu.x, qu.x, false, false);
   const auto y = __builtin_amdgcn_permlane16_swap(pu.y, qu.y, false, false);
   return {x[0], y[0], x[1], y[1]};
+}
+
+// What the rounding to the type leaves of four values.
+template <typename T>
+__device__ __forceinline__ f32x4 rest_of(f32x4 v) {
+  f32x4 r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r[j] = v[j] - static_cast<float>(static_cast<T>(v[j]));
+  return r;
 }
 
 template <int KIND>
@@ -206,7 +236,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
   const int left = min(a.vocab - a.from, a.piece);  // of the vocabulary
   int mt, nt;
   const int mtiles = KIND == kLogits  ? (a.vocab + BM - 1) / BM
-                     : KIND == kProbs ? a.piece / BM : (a.d + BM - 1) / BM;
+                     : KIND == kProbs ? (left + BM - 1) / BM : (a.d + BM - 1) / BM;
   const int ntiles = KIND == kWeight ? (left + BN - 1) / BN : rows;
   if (!tile_of(blockIdx.x, mtiles, ntiles, &mt, &nt)) return;
   const int m0 = mt * BM, n0 = nt * BN;
@@ -215,24 +245,33 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
   const char* const weight = static_cast<const char*>(a.weight) +
                              (KIND == kLogits ? 0 : a.from) * a.w_pitch;
   P p;
+  p.clear();
   if constexpr (KIND == kLogits || KIND == kProbs) {
     typename P::A x(weight, a.w_pitch, m0, KIND == kLogits ? a.vocab : left, 0, wave);
-    typename P::B y(a.packed, packed_pitch, n0, a.padded_rows, 0, wave);
+    typename P::B y(a.packed, packed_pitch, n0, live, 0, wave);
     p.run(x, y, lds, a.d, wave);
-  } else if constexpr (KIND == kInput) {
-    // A split's share of the piece, in whole stages.
-    const int stages = (left + P::A::kK - 1) / P::A::kK;
-    const int s0 = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / a.splits);
-    const int s1 = static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / a.splits);
-    const int64_t k0 = static_cast<int64_t>(s0) * P::A::kK;
-    const int64_t k1 = min(static_cast<int64_t>(s1) * P::A::kK, static_cast<int64_t>(left));
-    typename P::A x(weight, a.w_pitch, m0, a.d, k0, wave);
-    typename P::B y(a.g, g_pitch, n0, a.padded_rows, k0, wave);
-    p.run(x, y, lds, max(k1 - k0, static_cast<int64_t>(0)), wave);
   } else {
-    typename P::A x(a.packed, packed_pitch, m0, a.padded_d, 0, wave);
-    typename P::B y(a.g, g_pitch, n0, a.piece, 0, wave);
-    p.run(x, y, lds, live, wave);
+    // A split's share of the piece, or of the tokens, in whole stages.
+    const int all = KIND == kInput ? left : live;
+    const int stages = (all + P::A::kK - 1) / P::A::kK;
+    const int splits = KIND == kInput ? a.splits : a.w_splits;
+    const int s0 = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / splits);
+    const int s1 = static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / splits);
+    const int64_t k0 = static_cast<int64_t>(s0) * P::A::kK;
+    const int64_t k = max(min(static_cast<int64_t>(s1) * P::A::kK, static_cast<int64_t>(all)) - k0,
+                          static_cast<int64_t>(0));
+    for (int part = 0; part < parts_of<T>(live); ++part) {
+      const char* g = part == 0 ? a.g : a.g_rest;
+      if constexpr (KIND == kInput) {
+        typename P::A x(weight, a.w_pitch, m0, a.d, k0, wave);
+        typename P::B y(g, g_pitch, n0, live, k0, wave);
+        p.run(x, y, lds, k, wave);
+      } else {
+        typename P::A x(a.packed, packed_pitch, m0, a.padded_d, k0, wave);
+        typename P::B y(g, g_pitch, n0, a.piece, k0, wave);
+        p.run(x, y, lds, k, wave);
+      }
+    }
   }
   const int mw = m0 + wave % WM * (BM / WM);  // the wavefront's first row
   const int nw = n0 + wave / WM * (BN / WN) + lane % 16;
@@ -254,7 +293,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
 #pragma unroll
     for (int j = 0; j < P::kNT; ++j) {
       const int row = nw + 16 * j;
-      const int label = a.token[row].label;
+      const int label = row < live ? a.token[row].label : -1;
       float m = kNoLogit;
 #pragma unroll
       for (int i = 0; i < P::kMT; ++i)
@@ -310,11 +349,17 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
           v = rel == at ? k.label_g : v;
           p.acc[i][j][r] = at < rest ? v : 0.0f;
         }
+      const bool two = parts_of<T>(live) == 2 && row < kTwoParts;
 #pragma unroll
       for (int i = 0; i < P::kMT; i += kSize == 2 ? 2 : 1) {
-        if constexpr (kSize == 2)
+        if constexpr (kSize == 2) {
           *reinterpret_cast<uint4*>(out + (m8 + 16 * i) * 2) =
               strip8<T>(p.acc[i][j], p.acc[i + 1][j]);
+          if (__any(two)) {
+            const uint4 rest = strip8<T>(rest_of<T>(p.acc[i][j]), rest_of<T>(p.acc[i + 1][j]));
+            if (two) *reinterpret_cast<uint4*>(a.g_rest + row * g_pitch + (m8 + 16 * i) * 2) = rest;
+          }
+        }
         else
           *reinterpret_cast<f32x4*>(out + (m4 + 16 * i) * 4) = p.acc[i][j];
       }
@@ -330,6 +375,18 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
         if (m >= a.d) continue;
         f32x4* const o = reinterpret_cast<f32x4*>(out + m);
         *o = a.from > 0 ? *o + p.acc[i][j] : p.acc[i][j];
+      }
+    }
+  } else if (a.w_splits > 1) {
+    float* const sums = a.w_sums + static_cast<int64_t>(blockIdx.y) * a.piece * a.d;
+#pragma unroll
+    for (int j = 0; j < P::kNT; ++j) {
+      const int row = nw + 16 * j;
+#pragma unroll
+      for (int i = 0; i < P::kMT; ++i) {
+        const int m = m4 + 16 * i;
+        if (row < left && m < a.d)
+          *reinterpret_cast<f32x4*>(sums + static_cast<int64_t>(row) * a.d + m) = p.acc[i][j];
       }
     }
   } else {
@@ -354,34 +411,49 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
   }
 }
 
-// lse = M + ln S and loss = (M - x_label) + ln S from the tiles' statistics, in
-// binary64: 64 tokens per workgroup, four wavefronts over the tiles.
-template <int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_nll_join(NllArgs a) {
-  static_assert(WAVES == 4, "as summed up below");
-  __shared__ float m_lds[4][64];
-  __shared__ double s_lds[4][64];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int t = blockIdx.x * 64 + lane;
+// lse = M + ln S and loss = (M - x_label) + ln S from the tiles' statistics, summed in
+// binary64: 16 tokens per workgroup, 16 threads over the tiles of each, which load
+// eight tiles at a time.
+constexpr int kJoinTokens = 16;
+template <int SHARES>
+__global__ __launch_bounds__(kJoinTokens* SHARES) void k_nll_join(NllArgs a) {
+  __shared__ float m_lds[SHARES][kJoinTokens];
+  __shared__ double s_lds[SHARES][kJoinTokens];
+  const int lane = threadIdx.x % kJoinTokens, share = threadIdx.x / kJoinTokens;
+  const int t = blockIdx.x * kJoinTokens + lane;
   const int row = t < a.rows ? a.place[t] : -1;
   float m = kNoLogit;
-  if (row >= 0)
-    for (int i = wave; i < a.tiles; i += 4)
-      m = fmaxf(m, a.part[static_cast<int64_t>(i) * a.padded_rows + row].x);
-  m_lds[wave][lane] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(m_lds[0][lane], m_lds[1][lane]), fmaxf(m_lds[2][lane], m_lds[3][lane]));
-  const float ref = m == kNoLogit ? 0.0f : m;
   double s = 0.0;
   if (row >= 0)
-    for (int i = wave; i < a.tiles; i += 4) {
-      const f32x2 v = a.part[static_cast<int64_t>(i) * a.padded_rows + row];
-      s += static_cast<double>(v.y * __builtin_amdgcn_exp2f((v.x - ref) * kLog2eF));
+    for (int i0 = share; i0 < a.tiles; i0 += 8 * SHARES) {
+      f32x2 v[8];
+      float top = m;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = i0 + u * SHARES;
+        v[u] = f32x2{kNoLogit, 0.0f};
+        if (i < a.tiles) v[u] = a.part[static_cast<int64_t>(i) * a.padded_rows + row];
+        top = fmaxf(top, v[u].x);
+      }
+      const float ref = top == kNoLogit ? 0.0f : top;
+      s *= static_cast<double>(__builtin_amdgcn_exp2f((m - ref) * kLog2eF));
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        s += static_cast<double>(v[u].y * __builtin_amdgcn_exp2f((v[u].x - ref) * kLog2eF));
+      m = top;
     }
-  s_lds[wave][lane] = s;
+  m_lds[share][lane] = m;
+  s_lds[share][lane] = s;
   __syncthreads();
-  if (wave != 0 || t >= a.rows) return;
-  s = (s_lds[0][lane] + s_lds[1][lane]) + (s_lds[2][lane] + s_lds[3][lane]);
+  if (share != 0 || t >= a.rows) return;
+#pragma unroll
+  for (int w = 1; w < SHARES; ++w) m = fmaxf(m, m_lds[w][lane]);
+  const float ref = m == kNoLogit ? 0.0f : m;
+  s = 0.0;
+#pragma unroll
+  for (int w = 0; w < SHARES; ++w)
+    s += s_lds[w][lane] *
+         static_cast<double>(__builtin_amdgcn_exp2f((m_lds[w][lane] - ref) * kLog2eF));
   float loss = 0.0f, lse = 0.0f;
   if (row >= 0) {
     const double log_s = log(s);
@@ -394,6 +466,28 @@ __global__ __launch_bounds__(64 * WAVES) void k_nll_join(NllArgs a) {
   a.loss[t] = loss;
 }
 
+// The piece's rows of dweight from the splits' sums.
+template <typename T>
+__global__ __launch_bounds__(256) void k_nll_weight(NllArgs a) {
+  const int64_t strips = static_cast<int64_t>(min(a.vocab - a.from, a.piece)) * a.d / 4;
+  const int64_t each = static_cast<int64_t>(a.piece) * a.d;
+  const float unit = a.head->unit;
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4* const out = reinterpret_cast<T4*>(static_cast<T*>(a.dweight) + static_cast<int64_t>(a.from) * a.d);
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < strips;
+       i += static_cast<int64_t>(gridDim.x) * 256) {
+    f32x4 sum = {};
+#pragma unroll 8
+    for (int s = 0; s < a.w_splits; ++s)
+      sum += *reinterpret_cast<const f32x4*>(a.w_sums + s * each + 4 * i);
+    sum *= unit;
+    T4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = static_cast<T>(sum[j]);
+    out[i] = v;
+  }
+}
+
 template <int UNUSED>
 __global__ __launch_bounds__(256) void k_nll_clear(uint4* out, int64_t strips) {
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < strips;
@@ -401,12 +495,15 @@ __global__ __launch_bounds__(256) void k_nll_clear(uint4* out, int64_t strips) {
     out[i] = uint4{0, 0, 0, 0};
 }
 
-// dx of every token from the splits' sums: zeros for those without a loss.
+// dx of every token from the splits' sums, and what the rounding of g left at the label:
+// zeros for those without a loss.
 template <typename T>
 __global__ __launch_bounds__(256) void k_nll_input(NllArgs a) {
   const int strips = a.d / 8;
   const int64_t all = static_cast<int64_t>(a.rows) * strips;
   const float unit = a.head->unit;
+  const bool one = sizeof(T) == 2 && parts_of<T>(a.head->live) == 1;
+  typedef T T8 __attribute__((ext_vector_type(8)));
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all;
        i += static_cast<int64_t>(gridDim.x) * 256) {
     const int t = static_cast<int>(i / strips), c = static_cast<int>(i % strips) * 8;
@@ -419,11 +516,21 @@ __global__ __launch_bounds__(256) void k_nll_input(NllArgs a) {
         lo += *reinterpret_cast<const f32x4*>(p);
         hi += *reinterpret_cast<const f32x4*>(p + 4);
       }
+      const NllToken k = a.token[row];
+      if (one && k.label >= 0) {
+        const float rest = k.label_g - static_cast<float>(static_cast<T>(k.label_g));
+        const T8 w = *reinterpret_cast<const T8*>(static_cast<const char*>(a.weight) +
+                                                  k.label * a.w_pitch + c * sizeof(T));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          lo[j] += rest * static_cast<float>(w[j]);
+          hi[j] += rest * static_cast<float>(w[4 + j]);
+        }
+      }
     }
     lo *= unit;
     hi *= unit;
     T* const out = static_cast<T*>(a.dx) + static_cast<int64_t>(t) * a.d + c;
-    typedef T T8 __attribute__((ext_vector_type(8)));
     T8 v;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

@@ -12,8 +12,10 @@ struct NllProduct {
   int bm, bn, threads;
 };
 
-NllProduct nll_product_f32(int kind, int64_t tokens);
-NllProduct nll_product_f16(int kind, int64_t tokens);
-NllProduct nll_product_bf16(int kind, int64_t tokens);
+constexpr int kNarrow = 0, kSmall = 1, kLarge = 2;
+
+NllProduct nll_product_f32(int kind, int64_t m, int64_t n);
+NllProduct nll_product_f16(int kind, int64_t m, int64_t n);
+NllProduct nll_product_bf16(int kind, int64_t m, int64_t n);
 
 }  // namespace smx

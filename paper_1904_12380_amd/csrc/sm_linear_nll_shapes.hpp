@@ -1,4 +1,4 @@
-// Tile shapes of the products of 16-bit types.
+// Tile shapes of the products.
 #pragma once
 
 #include "sm_linear_nll.hpp"
@@ -12,21 +12,35 @@ NllProduct nll_shape() {
           64 * WM * WN};
 }
 
+// Up to kNllFew tokens: bound by the weight's bytes, so tiles are narrow in tokens.
+// Otherwise the largest tiles, unless they are too few to fill the device.
+constexpr int64_t kNllFew = 64;
+
+template <typename T, int KIND>
+NllProduct nll_shape_of(int size) {
+  if constexpr (KIND != kWeight) {
+    if (size == kNarrow) return nll_shape<T, KIND, 128, 64, 4, 1, 3>();
+  }
+  if constexpr (sizeof(T) == 2) {
+    return size == kLarge ? nll_shape<T, KIND, 256, 256, 2, 4, 2>()
+                          : nll_shape<T, KIND, 128, 128, 2, 2, 2>();
+  } else {
+    return size == kLarge ? nll_shape<T, KIND, 128, 128, 2, 2, 2>()
+                          : nll_shape<T, KIND, 64, 64, 2, 2, 3>();
+  }
+}
+
+// The product of `kind` for m x n entries.
 template <typename T>
-NllProduct nll_product_16(int kind, int64_t tokens) {
-  const bool few = tokens <= 64;
+NllProduct nll_product_of(int kind, int64_t m, int64_t n) {
+  constexpr int64_t kEdge = sizeof(T) == 2 ? 256 : 128;
+  const int64_t tiles = ((m + kEdge - 1) / kEdge) * ((n + kEdge - 1) / kEdge);
+  const int size = kind != kWeight && n <= kNllFew ? kNarrow : tiles >= 192 ? kLarge : kSmall;
   switch (kind) {
-    case kLogits:
-      return few ? nll_shape<T, kLogits, 128, 64, 4, 1, 3>()
-                 : nll_shape<T, kLogits, 256, 256, 2, 4, 2>();
-    case kProbs:
-      return few ? nll_shape<T, kProbs, 128, 64, 4, 1, 3>()
-                 : nll_shape<T, kProbs, 256, 256, 2, 4, 2>();
-    case kInput:
-      return few ? nll_shape<T, kInput, 128, 64, 4, 1, 3>()
-                 : nll_shape<T, kInput, 256, 256, 2, 4, 2>();
-    default:
-      return nll_shape<T, kWeight, 256, 256, 2, 4, 2>();
+    case kLogits: return nll_shape_of<T, kLogits>(size);
+    case kProbs: return nll_shape_of<T, kProbs>(size);
+    case kInput: return nll_shape_of<T, kInput>(size);
+    default: return nll_shape_of<T, kWeight>(size);
   }
 }
 

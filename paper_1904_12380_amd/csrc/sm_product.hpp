@@ -87,7 +87,7 @@ struct Side {
   static constexpr int kChunks = kRowBytes / 16;
   static constexpr int kRowsPer = 64 / kChunks;  // rows of a block
   static_assert(kBlocks % WAVES == 0 && 64 % kChunks == 0, "whole loads");
-  static_assert(BY_ROWS ? LINES % 64 == 0 : kRowBytes == 512 || (kSize == 2 && kRowBytes == 256),
+  static_assert(BY_ROWS ? LINES % 64 == 0 : kRowBytes == 512 || kRowBytes == 256,
                 "known layouts");
 
   // Blocks.  The banks repeat every 256 bytes, of which 16 lanes' reads at a time may
@@ -98,13 +98,15 @@ struct Side {
   //   by columns   16 bits: 32 bytes of the rows 0 .. 3 and 8 .. 11 are read at once,
   //                or of these rows + 4, + 16 or + 20.  A block has one (rows of 256
   //                bytes: two) of each.
-  //                fp32: 64 bytes of the rows 0, 4, 8 and 12, or the next ones.
+  //                fp32: 64 bytes of the rows 0, 4, 8 and 12, or the next ones.  A
+  //                block has two rows that follow each other, or all four between two
+  //                of these.
   __host__ __device__ static constexpr int block_at(int n) { return 1056 * n; }
   static constexpr int kBytes = block_at(kBlocks);
   // Row j of block n.
   __device__ __forceinline__ static constexpr int row_of(int n, int j) {
     return BY_ROWS        ? n / 8 * 64 + j / 2 * 16 + n % 8 * 2 + j % 2
-           : kSize == 4   ? 2 * n + j
+           : kSize == 4   ? (kRowsPer == 2 ? 2 * n + j : n % 2 * 16 + n / 2 * 4 + j)
            : kRowsPer == 2 ? n / 8 * 16 + n / 4 % 2 * 8 + n % 4 + 4 * j
                            : n / 8 * 32 + n / 4 % 2 * 8 + n % 4 + j % 2 * 4 + j / 2 * 16;
   }
@@ -173,11 +175,12 @@ struct Side {
       p += block_at(t / 4 * 8) + t % 4 * 2 * kLineBytes + 64 * s;
       return *reinterpret_cast<const V SMX_LDS*>(p);
     } else if constexpr (kSize == 4) {
-      p += block_at(8 * s) + 64 * t;
+      p += block_at(kRowsPer == 2 ? 8 * s : s) + 64 * t;
       V v;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        v[j] = *reinterpret_cast<const float SMX_LDS*>(p + block_at(j / 2) + j % 2 * kRowBytes);
+        v[j] = *reinterpret_cast<const float SMX_LDS*>(
+            p + (kRowsPer == 2 ? block_at(j / 2) + j % 2 * kRowBytes : j * kRowBytes));
       return v;
     } else {
       p += block_at(kRowsPer == 2 ? 16 * s : 8 * s) + 32 * t;
@@ -226,6 +229,11 @@ struct Product {
     });
   }
 
+  __device__ __forceinline__ void clear() {
+    unrolled<kOps>([&](auto n) { acc[n / kNT][n % kNT] = f32x4{}; });
+  }
+
+  // Adds the products of the next `k` entries of two operands.
   __device__ __forceinline__ void run(A& a, B& b, char SMX_LDS* lds, int64_t k, int wave) {
     const unsigned at = lds_offset(lds);
     int64_t left = k;  // from the next stage to load on
@@ -244,7 +252,6 @@ struct Product {
     };
     a.reader(wave % WM * (BM / WM));
     b.reader(wave / WM * (BN / WN));
-    unrolled<kOps>([&](auto n) { acc[n / kNT][n % kNT] = f32x4{}; });
 #pragma unroll
     for (int s = 0; s < STAGES; ++s) {
       ready();
