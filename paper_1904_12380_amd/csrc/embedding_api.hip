@@ -37,28 +37,33 @@ const void* by_group(int g, int what) {
 // wavefront.
 int group_of(int64_t strips) { return strips <= 8 ? 8 : strips <= 16 ? 16 : strips <= 32 ? 32 : 64; }
 
-// Sorted tokens of a chunk: 32, or more once that makes 8192 chunks, which keeps
-// the parts of a run that an id with many tokens has few.
-int64_t chunk_of(int64_t tokens) { return up_to(std::max<int64_t>(ceil_div(tokens, 8192), 32), 32); }
+// Sorted tokens of a chunk: 8, or so many more that the chunks' columns still make
+// 4096 wavefronts, up to 32; and more once that makes 8192 chunks, which keeps the
+// parts of a run that an id with many tokens has few.
+int64_t chunk_of(int64_t tokens, int64_t strips) {
+  const int64_t waves = ceil_div(tokens * strips, 64);
+  const int64_t chunk = std::clamp<int64_t>(waves / 4096 / 8 * 8, 8, 32);
+  return std::max(chunk, up_to(ceil_div(tokens, 8192), 8));
+}
 
 struct Room {
   int64_t key[2], token[2], bins, part, end;
   int64_t tiles, chunk, chunks;
 };
 
-Room room(int64_t tokens, int64_t d) {
+Room room(int64_t tokens, int64_t d, int dtype) {
   Room r;
   const int64_t list = up_to(tokens * 4, 16);
-  const bool alone = tokens <= kSortMost;
-  r.chunk = chunk_of(tokens);
+  const bool radix = tokens > kMergeMost;
+  r.chunk = chunk_of(tokens, d * dtype_size(dtype) / 16);
   r.chunks = ceil_div(tokens, r.chunk);
-  r.tiles = ceil_div(tokens, kMoveTile);
-  r.key[0] = 0;
-  r.token[0] = list;
-  r.key[1] = alone ? 0 : 2 * list;
-  r.token[1] = alone ? list : 3 * list;
-  r.bins = (alone ? 2 : 4) * list;
-  r.part = r.bins + (alone ? 0 : up_to(r.tiles * kBins * 4, 16));
+  r.tiles = ceil_div(tokens, radix ? kMoveTile : kTile);
+  for (int i = 0; i < 2; ++i) {
+    r.key[i] = 2 * i * list;
+    r.token[i] = (2 * i + 1) * list;
+  }
+  r.bins = 4 * list;
+  r.part = r.bins + (radix ? up_to(r.tiles * kBins * 4, 16) : 0);
   r.end = r.part + (r.chunks > 1 ? r.chunks * 2 * d * 4 : 0);
   return r;
 }
@@ -115,7 +120,7 @@ SOFTMAX_API int softmax_embedding_fwd(const int64_t* ids, int64_t tokens, const 
 SOFTMAX_API int64_t softmax_embedding_bwd_workspace(int64_t tokens, int64_t rows, int64_t d,
                                                     int dtype) {
   if (!sizes_ok(tokens, rows, d, dtype)) return -1;
-  return rows == 0 ? 0 : room(tokens, d).end;
+  return rows == 0 ? 0 : room(tokens, d, dtype).end;
 }
 
 SOFTMAX_API int softmax_embedding_bwd(const void* dout, int64_t dout_stride, const int64_t* ids,
@@ -129,7 +134,7 @@ SOFTMAX_API int softmax_embedding_bwd(const void* dout, int64_t dout_stride, con
       !aligned16(workspace))
     return SOFTMAX_ERR_INVALID_ARG;
   if (rows == 0) return SOFTMAX_OK;
-  const Room r = room(tokens, d);
+  const Room r = room(tokens, d, dtype);
   if (workspace_bytes < r.end) return SOFTMAX_ERR_INVALID_ARG;
   const int64_t strips = d * size / 16;
   const int g = group_of(strips);
@@ -165,21 +170,26 @@ SOFTMAX_API int softmax_embedding_bwd(const void* dout, int64_t dout_stride, con
   a.passes = passes;
   hipError_t e = hipSuccess;
   void* one[] = {&a};
-  if (tokens <= kSortMost) {
-    const int64_t clear = std::min<int64_t>(ceil_div(a.clear, 4 * kSortThreads), 512);
-    e = start(reinterpret_cast<const void*>(&k_embed_sort<0>), 1 + clear, kSortThreads, one, stream);
-    a.key[1] = a.key[0];
-    a.token[1] = a.token[0];
+  const int64_t clear = std::min<int64_t>(ceil_div(a.clear, 4 * kSortThreads), 2048);
+  if (tokens <= kMergeMost) {
+    int tiles = static_cast<int>(r.tiles), to = tiles > 1 ? 1 : 0;
+    void* sort[] = {&a, &tiles, &to};
+    e = start(reinterpret_cast<const void*>(&k_embed_sort<0>), tiles + clear, kSortThreads, sort,
+              stream);
+    void* merge[] = {&a, &tiles};
+    if (e == hipSuccess && tiles > 1)
+      e = start(reinterpret_cast<const void*>(&k_embed_merge<0>),
+                ceil_div(tokens * kMergeLanes, kSortThreads), kSortThreads, merge, stream);
   } else {
-    const int64_t clear = std::min<int64_t>(ceil_div(a.clear, 4 * kMoveThreads), 2048);
+    a.sorted = passes & 1;
     for (int p = 0; p < passes && e == hipSuccess; ++p) {
       void* two[] = {&a, &p};
       e = start(reinterpret_cast<const void*>(&k_embed_count<0>), r.tiles + (p == 0 ? clear : 0),
-                kMoveThreads, two, stream);
+                kSortThreads, two, stream);
       if (e == hipSuccess)
         e = start(reinterpret_cast<const void*>(&k_embed_base<0>), 1, 1024, one, stream);
       if (e == hipSuccess)
-        e = start(reinterpret_cast<const void*>(&k_embed_move<0>), r.tiles, kMoveThreads, two,
+        e = start(reinterpret_cast<const void*>(&k_embed_move<0>), r.tiles, kSortThreads, two,
                   stream);
     }
   }

@@ -42,10 +42,9 @@ Shape forward_of(int64_t strips, int64_t rows) {
   if (strips <= 16) return instance<B, T, 16, 1>();
   if (strips <= 32) return instance<B, T, 32, 1>();
   if (strips <= 64) return instance<B, T, 64, 1>();
-  if (rows > 1024) {
+  if (rows > 1024 && strips <= 256) {
     if (strips <= 128) return instance<B, T, 64, 2>();
-    if (strips <= 256) return instance<B, T, 64, 4>();
-    if (strips <= 512) return instance<B, T, 64, 8>();
+    return instance<B, T, 64, 4>();
   }
   if (strips <= 256) return instance<B, T, 256, 1>();
   if (strips <= 512) return instance<B, T, 256, 2>();
@@ -80,16 +79,10 @@ Shape backward_shape(int dtype, int64_t strips) {
          : dtype == SOFTMAX_F16 ? backward_of<f16>(strips) : backward_of<bf16>(strips);
 }
 
-// The backward pass' workgroups, a fixed number whatever the device (the order of
-// the sums goes by it), and the rows of sums that they leave.
-constexpr int64_t kGroups = 1024;
-struct Backward {
-  int64_t grid, groups;
-};
-Backward backward_grid(int lanes, int64_t rows) {
-  const int64_t per = lanes < 256 ? 256 / lanes : 1;
-  const int64_t grid = std::min(ceil_div(rows, per), lanes == 1024 ? kGroups / 2 : kGroups);
-  return {grid, lanes <= 64 ? grid * 4 : grid};
+// The backward pass' workgroups, each of which leaves a row of sums: a fixed number
+// whatever the device, since the order of the sums goes by it.
+int64_t groups_of(int lanes, int64_t rows) {
+  return std::min<int64_t>(ceil_div(rows, lanes < 256 ? 256 / lanes : 1), lanes == 1024 ? 512 : 1024);
 }
 
 bool sizes_ok(int64_t rows, int64_t d, int dtype) {
@@ -139,7 +132,7 @@ SOFTMAX_API int softmax_layer_norm_fwd(const void* x, int64_t x_stride, const vo
 
 SOFTMAX_API int64_t softmax_layer_norm_bwd_workspace(int64_t rows, int64_t d, int dtype) {
   if (!sizes_ok(rows, d, dtype)) return -1;
-  return backward_grid(backward_shape(dtype, strips_of(d, dtype)).lanes, rows).groups * 2 * d * 4;
+  return groups_of(backward_shape(dtype, strips_of(d, dtype)).lanes, rows) * 2 * d * 4;
 }
 
 SOFTMAX_API int softmax_layer_norm_bwd(const void* dy, int64_t dy_stride, const void* x,
@@ -156,8 +149,8 @@ SOFTMAX_API int softmax_layer_norm_bwd(const void* dy, int64_t dy_stride, const 
   const bool columns = dweight != nullptr || dbias != nullptr;
   if (!columns && (dx == nullptr || rows == 0)) return SOFTMAX_OK;
   const Shape s = backward_shape(dtype, strips_of(d, dtype));
-  const Backward b = backward_grid(s.lanes, rows);
-  const int64_t need = columns ? b.groups * 2 * d * 4 : 0;
+  const int64_t groups = groups_of(s.lanes, rows);
+  const int64_t need = columns ? groups * 2 * d * 4 : 0;
   if (workspace_bytes < need) return SOFTMAX_ERR_INVALID_ARG;
   const Range inputs[] = {{x, xb},
                           {dy, db},
@@ -184,16 +177,17 @@ SOFTMAX_API int softmax_layer_norm_bwd(const void* dy, int64_t dy_stride, const 
   a.part = static_cast<float*>(workspace);
   a.rows = static_cast<int>(rows);
   a.d = static_cast<int>(d);
-  a.groups = static_cast<int>(b.groups);
+  a.groups = static_cast<int>(groups);
   void* args[] = {&a};
   hipError_t e = hipSuccess;
-  if (rows > 0) e = launch(s.fn, b.grid, std::max(s.lanes, 256), args, stream);
+  if (rows > 0)
+    e = launch(s.fn, groups, std::max(s.lanes, 256), args, stream);
   if (e == hipSuccess && columns) {
     const void* fn = dtype == SOFTMAX_F32   ? reinterpret_cast<const void*>(&k_norm_join<float>)
                      : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_norm_join<f16>)
                                             : reinterpret_cast<const void*>(&k_norm_join<bf16>);
-    e = hipLaunchKernel(fn, dim3(static_cast<uint32_t>(ceil_div(d, 32)), 2),
-                        dim3(32 * kJoinShares), args, 0, stream);
+    e = hipLaunchKernel(fn, dim3(static_cast<uint32_t>(ceil_div(d, kJoinCols)), 2),
+                        dim3(kJoinCols * kJoinShares), args, 0, stream);
   }
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
 }

@@ -3,32 +3,36 @@
 // lookup reads and writes a row per token, the gradient reads a row per token and
 // writes the table.
 //
-// The gradient sorts the tokens by id (a radix sort, digits of kDigit bits, which
-// keeps tokens of one id in their order) and sums runs of equal ids:
+// The gradient sorts the tokens by id, tokens of one id in their order, and sums runs
+// of equal ids:
 //
-//   k_embed_sort    up to kSortMost tokens: one workgroup sorts them in registers
-//                   and LDS, while the others clear the table
+//   k_embed_sort    tiles of kTile tokens, each sorted by a workgroup in registers and
+//                   LDS (a radix sort, digits of kDigit bits); further workgroups
+//                   clear the table
+//   k_embed_merge   up to kMergeMost tokens: a token's place among all is its place in
+//                   its own tile and, by bisection, in every other one
 //   k_embed_count, k_embed_base, k_embed_move
-//                   more tokens: one pass per digit, by tiles of tokens
+//                   more tokens: the radix sort over all of them, a pass per digit
 //   k_embed_sums    chunks of sorted tokens: a run that lies within a chunk is
 //                   summed, scaled and written; the ends of runs that cross chunks
 //                   go to the workspace
 //   k_embed_join    sums the parts of those runs, in order
 //
-// No atomics: the order of every sum follows from the ids alone.
+// No atomics but in counts: the order of every sum follows from the ids alone.
 #pragma once
 
 #include "sm_strips.hpp"
 
 namespace smx {
 
-constexpr int kDigit = 8;
+constexpr int kDigit = 9;
 constexpr int kBins = 1 << kDigit;
-constexpr int kSortItems = 16;                          // of a thread
-constexpr int kSortThreads = 1024;                      // of the workgroup that sorts alone
-constexpr int kSortMost = kSortThreads * kSortItems;
-constexpr int kMoveThreads = 256;
-constexpr int kMoveTile = kMoveThreads * kSortItems;
+constexpr int kSortThreads = 256;
+constexpr int kSortItems = 4;  // of a thread
+constexpr int kTile = kSortThreads * kSortItems;
+constexpr int kMergeMost = 32 * kTile;
+constexpr int kMoveItems = 16;
+constexpr int kMoveTile = kSortThreads * kMoveItems;
 
 struct EmbedArgs {
   const int64_t* ids;
@@ -38,8 +42,9 @@ struct EmbedArgs {
   int tokens, rows, d;
   float scale;
   // Workspace of the gradient.
-  unsigned* key[2];     // ids of the sorted tokens (rows: padding), and the tokens
+  unsigned* key[2];     // ids of tokens in order (rows: padding), and the tokens
   int* token[2];
+  int sorted;           // which of the two is
   int* bins;            // [kBins, tiles]
   float* part;          // [chunks, 2, d]: sums of a run that began before the chunk, and
                         // of one that goes on behind it
@@ -93,16 +98,15 @@ __device__ __forceinline__ void clear_strips(const EmbedArgs& a, int64_t from, i
 }
 
 // The places of a wavefront's items by digit, in the order item by item and lane
-// by lane; `counts` (its own, cleared) ends as the number of items per digit.  A
-// lane's items with live = false have no place.
-template <typename F>
-__device__ __forceinline__ void rank_items(int (&rank)[kSortItems], int* counts, F digit) {
+// by lane; `counts` (its own, cleared) ends as the number of items per digit.  An item
+// of digit -1 has no place.
+template <int ITEMS, typename F>
+__device__ __forceinline__ void rank_items(int (&rank)[ITEMS], int* counts, F digit) {
   const int lane = static_cast<int>(__lane_id());
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
-    const int x = digit(i);  // -1: none
+  for (int i = 0; i < ITEMS; ++i) {
+    const int x = digit(i);
     uint64_t same = __ballot(x >= 0);
-    if (x < 0) same = ~same;
 #pragma unroll
     for (int b = 0; b < kDigit; ++b) {
       const uint64_t ones = __ballot(x >> b & 1);
@@ -111,113 +115,158 @@ __device__ __forceinline__ void rank_items(int (&rank)[kSortItems], int* counts,
     const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
     int base = 0;
     if (x >= 0) base = counts[x];
-    // The wavefront's reads of LDS come before its writes: in order, and not
-    // moved by the compiler (the addresses may be the same).
+    // The first of the lanes with a digit counts them.  A wavefront's reads and
+    // writes of LDS take place in order.
     if (x >= 0 && before == 0) counts[x] = base + __popcll(same);
     __builtin_amdgcn_wave_barrier();
     rank[i] = base + before;
   }
 }
 
-// One workgroup sorts all tokens; the others clear the table's gradient.
+constexpr int kSortWaves = kSortThreads / 64;
+
+// Tiles of tokens, each sorted by id.  The workgroups behind them clear the table's
+// gradient.
 template <int UNUSED>
-__global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a) {
-  constexpr int kWaves = kSortThreads / 64;
-  __shared__ unsigned items[kSortMost];
-  __shared__ int counts[kWaves][kBins];
-  __shared__ int total[kBins];
+__global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a, int tiles, int to) {
+  __shared__ unsigned keys[kTile];
+  __shared__ int tokens[kTile];
+  __shared__ int counts[kSortWaves][kBins];
+  __shared__ int total[kSortWaves];
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64;
-  if (blockIdx.x != 0) {
-    clear_strips(a, static_cast<int64_t>(blockIdx.x - 1) * kSortThreads + tid,
-                 static_cast<int64_t>(gridDim.x - 1) * kSortThreads);
+  if (static_cast<int>(blockIdx.x) >= tiles) {
+    clear_strips(a, static_cast<int64_t>(blockIdx.x - tiles) * kSortThreads + tid,
+                 static_cast<int64_t>(gridDim.x - tiles) * kSortThreads);
     return;
   }
   unsigned key[kSortItems];
   int token[kSortItems], rank[kSortItems];
-  const int at = wave * (64 * kSortItems) + lane;
+  const int first = blockIdx.x * kTile, at = wave * (64 * kSortItems) + lane;
 #pragma unroll
   for (int i = 0; i < kSortItems; ++i) {
-    token[i] = at + 64 * i;
+    token[i] = first + at + 64 * i;
+    // Items past the tokens have the largest key, and are behind others of it.
     key[i] = token[i] < a.tokens ? embed_key(a, token[i]) : 0xffffffffu;
   }
   for (int p = 0; p < a.passes; ++p) {
-    for (int i = tid; i < kWaves * kBins; i += kSortThreads) counts[i / kBins][i % kBins] = 0;
+    for (int i = tid; i < kSortWaves * kBins; i += kSortThreads) counts[i / kBins][i % kBins] = 0;
     __syncthreads();
-    // Items past the tokens have the largest key, so that they stay last.
     auto digit = [&](int i) { return static_cast<int>(key[i] >> (kDigit * p) & (kBins - 1)); };
     rank_items(rank, counts[wave], digit);
     __syncthreads();
-    if (tid < kBins) {
-      int sum = 0;
-      for (int w = 0; w < kWaves; ++w) {
-        const int c = counts[w][tid];
-        counts[w][tid] = sum;
-        sum += c;
+    // A thread's two digits: the items before them, over digits and wavefronts.
+    static_assert(kBins == 2 * kSortThreads, "two digits a thread");
+    int own[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) {
+        const int c = counts[w][2 * tid + j];
+        counts[w][2 * tid + j] = own[j];
+        own[j] += c;
       }
-      total[tid] = sum;
+    int before = own[0] + own[1];
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      const int o = __shfl_up(before, s);
+      if (lane >= s) before += o;
+    }
+    if (lane == 63) total[wave] = before;
+    __syncthreads();
+    before -= own[0] + own[1];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) before += w < wave ? total[w] : 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      counts[w][2 * tid] += before;
+      counts[w][2 * tid + 1] += before + own[0];
     }
     __syncthreads();
-    if (wave == 0) {  // sums of the digits before each digit, four to a lane
-      int c[kBins / 64], own = 0;
 #pragma unroll
-      for (int j = 0; j < kBins / 64; ++j) {
-        c[j] = own;
-        own += total[lane * (kBins / 64) + j];
-      }
-      int before = own;
-#pragma unroll
-      for (int s = 1; s < 64; s *= 2) {
-        const int o = __shfl_up(before, s);
-        if (lane >= s) before += o;
-      }
-#pragma unroll
-      for (int j = 0; j < kBins / 64; ++j) total[lane * (kBins / 64) + j] = before - own + c[j];
+    for (int i = 0; i < kSortItems; ++i) {
+      rank[i] += counts[wave][digit(i)];
+      keys[rank[i]] = key[i];
+      tokens[rank[i]] = token[i];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) rank[i] += total[digit(i)] + counts[wave][digit(i)];
-#pragma unroll
-    for (int i = 0; i < kSortItems; ++i) items[rank[i]] = key[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kSortItems; ++i) key[i] = items[at + 64 * i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kSortItems; ++i) items[rank[i]] = static_cast<unsigned>(token[i]);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kSortItems; ++i) token[i] = static_cast<int>(items[at + 64 * i]);
+    for (int i = 0; i < kSortItems; ++i) {
+      key[i] = keys[at + 64 * i];
+      token[i] = tokens[at + 64 * i];
+    }
     __syncthreads();
   }
 #pragma unroll
   for (int i = 0; i < kSortItems; ++i)
-    if (at + 64 * i < a.tokens) {
-      a.key[0][at + 64 * i] = key[i];
-      a.token[0][at + 64 * i] = token[i];
+    if (first + at + 64 * i < a.tokens) {
+      a.key[to][first + at + 64 * i] = key[i];
+      a.token[to][first + at + 64 * i] = token[i];
     }
 }
 
-// Items of a tile by digit.  In the first pass further workgroups clear the table's
-// gradient.
+// Sorted tiles (key[1], token[1]) to one order (key[0], token[0]): before a token come
+// those of smaller ids, and those of its own id in earlier tiles.  Eight lanes take a
+// token, each every eighth tile: a bisection is a chain of loads, and a lane's up to
+// four are independent (16384 tokens: 36 us with one lane for all tiles, 8.3 so).
+constexpr int kMergeLanes = 8;
 template <int UNUSED>
-__global__ __launch_bounds__(kMoveThreads) void k_embed_count(EmbedArgs a, int pass) {
+__global__ __launch_bounds__(kSortThreads) void k_embed_merge(EmbedArgs a, int tiles) {
+  constexpr int kEach = kMergeMost / kTile / kMergeLanes;
+  const int at = blockIdx.x * (kSortThreads / kMergeLanes) + threadIdx.x / kMergeLanes;
+  const int e = min(at, a.tokens - 1);
+  const int own = e / kTile, part = threadIdx.x % kMergeLanes;
+  const unsigned key = a.key[1][e];
+  int lo[kEach], hi[kEach];
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int j = part + u * kMergeLanes;
+    lo[u] = 0;
+    hi[u] = j < tiles && j != own ? min(a.tokens - j * kTile, kTile) : 0;
+  }
+  static_assert(kTile == 1 << 10, "steps of a bisection");
+  for (int step = 0; step <= 10; ++step) {
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+      const int j = part + u * kMergeLanes, mid = (lo[u] + hi[u]) / 2;
+      if (lo[u] >= hi[u]) continue;
+      const unsigned other = a.key[1][j * kTile + mid];
+      if (other < key || (other == key && j < own)) lo[u] = mid + 1;
+      else hi[u] = mid;
+    }
+  }
+  int before = 0;
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) before += lo[u];
+#pragma unroll
+  for (int s = 1; s < kMergeLanes; s *= 2) before += __shfl_xor(before, s);
+  if (part == 0 && at < a.tokens) {
+    const int to = e - own * kTile + before;
+    a.key[0][to] = key;
+    a.token[0][to] = a.token[1][e];
+  }
+}
+
+// Items of a tile by digit.
+template <int UNUSED>
+__global__ __launch_bounds__(kSortThreads) void k_embed_count(EmbedArgs a, int pass) {
   __shared__ int counts[kBins];
   const int tid = threadIdx.x, tile = blockIdx.x;
   if (tile >= a.tiles) {
-    clear_strips(a, static_cast<int64_t>(tile - a.tiles) * kMoveThreads + tid,
-                 static_cast<int64_t>(gridDim.x - a.tiles) * kMoveThreads);
+    clear_strips(a, static_cast<int64_t>(tile - a.tiles) * kSortThreads + tid,
+                 static_cast<int64_t>(gridDim.x - a.tiles) * kSortThreads);
     return;
   }
-  counts[tid] = 0;
+  for (int b = tid; b < kBins; b += kSortThreads) counts[b] = 0;
   __syncthreads();
   const int end = min(a.tokens - tile * kMoveTile, kMoveTile);
-  for (int i = tid; i < end; i += kMoveThreads) {
+  for (int i = tid; i < end; i += kSortThreads) {
     const int t = tile * kMoveTile + i;
     const unsigned key = pass == 0 ? embed_key(a, t) : a.key[pass & 1][t];
     atomicAdd(&counts[key >> (kDigit * pass) & (kBins - 1)], 1);
   }
   __syncthreads();
-  a.bins[static_cast<int64_t>(tid) * a.tiles + tile] = counts[tid];
+  for (int b = tid; b < kBins; b += kSortThreads)
+    a.bins[static_cast<int64_t>(b) * a.tiles + tile] = counts[b];
 }
 
 // Counts by digit and tile to the items before them, by one workgroup.
@@ -250,15 +299,14 @@ __global__ __launch_bounds__(1024) void k_embed_base(EmbedArgs a) {
 
 // Items of a tile to their places by digit.
 template <int UNUSED>
-__global__ __launch_bounds__(kMoveThreads) void k_embed_move(EmbedArgs a, int pass) {
-  constexpr int kWaves = kMoveThreads / 64;
-  __shared__ int counts[kWaves][kBins];
+__global__ __launch_bounds__(kSortThreads) void k_embed_move(EmbedArgs a, int pass) {
+  __shared__ int counts[kSortWaves][kBins];
   const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, tile = blockIdx.x;
-  const int at = tile * kMoveTile + wave * (64 * kSortItems) + lane;
-  unsigned key[kSortItems];
-  int token[kSortItems], rank[kSortItems];
+  const int at = tile * kMoveTile + wave * (64 * kMoveItems) + lane;
+  unsigned key[kMoveItems];
+  int token[kMoveItems], rank[kMoveItems];
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
+  for (int i = 0; i < kMoveItems; ++i) {
     const int t = at + 64 * i;
     token[i] = t;
     key[i] = 0;
@@ -267,22 +315,25 @@ __global__ __launch_bounds__(kMoveThreads) void k_embed_move(EmbedArgs a, int pa
       if (pass != 0) token[i] = a.token[pass & 1][t];
     }
   }
-  for (int w = 0; w < kWaves; ++w) counts[w][tid] = 0;
+  for (int i = tid; i < kSortWaves * kBins; i += kSortThreads) counts[i / kBins][i % kBins] = 0;
   __syncthreads();
   auto digit = [&](int i) {
     return at + 64 * i < a.tokens ? static_cast<int>(key[i] >> (kDigit * pass) & (kBins - 1)) : -1;
   };
   rank_items(rank, counts[wave], digit);
   __syncthreads();
-  int sum = a.bins[static_cast<int64_t>(tid) * a.tiles + tile];
-  for (int w = 0; w < kWaves; ++w) {
-    const int c = counts[w][tid];
-    counts[w][tid] = sum;
-    sum += c;
+  for (int b = tid; b < kBins; b += kSortThreads) {
+    int sum = a.bins[static_cast<int64_t>(b) * a.tiles + tile];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const int c = counts[w][b];
+      counts[w][b] = sum;
+      sum += c;
+    }
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kSortItems; ++i) {
+  for (int i = 0; i < kMoveItems; ++i) {
     if (digit(i) < 0) continue;
     const int to = rank[i] + counts[wave][digit(i)];
     a.key[~pass & 1][to] = key[i];
@@ -300,8 +351,8 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a) {
   const int c = static_cast<int>(unit / slabs);
   const int strip = static_cast<int>(unit % slabs) * G + threadIdx.x % G;
   if (c >= a.chunks || strip >= strips) return;
-  const unsigned* key = a.key[a.passes & 1];
-  const int* token = a.token[a.passes & 1];
+  const unsigned* key = a.key[a.sorted];
+  const int* token = a.token[a.sorted];
   const T* in = static_cast<const T*>(a.in) + strip * kN;
   const int64_t from = static_cast<int64_t>(c) * a.chunk;
   const int64_t to = min(from + a.chunk, static_cast<int64_t>(a.tokens));
@@ -323,16 +374,27 @@ __global__ __launch_bounds__(256) void k_embed_sums(EmbedArgs a) {
       Strip<T>::store(static_cast<T*>(a.out) + static_cast<int64_t>(now) * a.d + strip * kN, sum);
     }
   };
-  for (int64_t p = from; p < to; p += kAhead) {
-    unsigned k[kAhead];
-    typename Strip<T>::type v[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) k[u] = p + u < to ? key[p + u] : none;
+  // Ids and tokens are loaded a turn ahead of the rows.
+  unsigned k[kAhead], k_next[kAhead];
+  int t_next[kAhead];
+  auto ahead = [&](int64_t p) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      v[u] = typename Strip<T>::type{};
-      if (k[u] != none) v[u] = Strip<T>::load(in + token[p + u] * a.pitch);
+      const int64_t at = min(p + u, to - 1);
+      k_next[u] = p + u < to ? key[at] : none;
+      t_next[u] = token[at];
     }
+  };
+  ahead(from);
+  for (int64_t p = from; p < to; p += kAhead) {
+    typename Strip<T>::type v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      k[u] = k_next[u];
+      v[u] = typename Strip<T>::type{};
+      if (k[u] != none) v[u] = Strip<T>::load(in + t_next[u] * a.pitch);
+    }
+    ahead(p + kAhead);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (p + u >= to) continue;
@@ -359,7 +421,7 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedArgs a) {
   const int c = static_cast<int>(unit / slabs);
   const int strip = static_cast<int>(unit % slabs) * G + threadIdx.x % G;
   if (c + 1 >= a.chunks || strip >= strips) return;
-  const unsigned* key = a.key[a.passes & 1];
+  const unsigned* key = a.key[a.sorted];
   const int64_t from = static_cast<int64_t>(c) * a.chunk, to = from + a.chunk;
   const unsigned now = key[to - 1];
   if (now == static_cast<unsigned>(a.rows) || key[to] != now || (from > 0 && key[from - 1] == now))

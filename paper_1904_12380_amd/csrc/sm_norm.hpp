@@ -219,37 +219,56 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void k_norm_bwd(NormArgs a) {
         }
       }
   }
-  // Each wavefront (L <= 64) or workgroup has a row of sums of its own.
-  const int64_t row = L <= 64 ? static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 64 : blockIdx.x;
-  float* const out = a.part + row * 2 * a.d;
-  if (L < 64 && threadIdx.x % 64 >= L) return;
+  float* const out = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.d;
+  if constexpr (L <= 64) {
+    // The workgroup's four wavefronts.
+    __shared__ __attribute__((aligned(16))) float sums[4][2][L * S * kN];
+    const int wave = threadIdx.x / 64;
+    if (threadIdx.x % 64 < L) {
 #pragma unroll
-  for (int s = 0; s < S; ++s) {
-    if (j + L * s >= strips) continue;
+      for (int s = 0; s < S; ++s)
 #pragma unroll
-    for (int e = 0; e < kN; e += 4) {
-      const int at = (j + L * s) * kN + e;
-      *reinterpret_cast<f32x4*>(out + at) = f32x4{dw[s][e], dw[s][e + 1], dw[s][e + 2], dw[s][e + 3]};
-      *reinterpret_cast<f32x4*>(out + a.d + at) =
-          f32x4{db[s][e], db[s][e + 1], db[s][e + 2], db[s][e + 3]};
+        for (int e = 0; e < kN; ++e) {
+          sums[wave][0][(j + L * s) * kN + e] = dw[s][e];
+          sums[wave][1][(j + L * s) * kN + e] = db[s][e];
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.d; i += 256) {
+      const int k = i < a.d ? 0 : 1, c = i - k * a.d;
+      out[i] = (sums[0][k][c] + sums[1][k][c]) + (sums[2][k][c] + sums[3][k][c]);
+    }
+  } else {
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      if (j + L * s >= strips) continue;
+#pragma unroll
+      for (int e = 0; e < kN; e += 4) {
+        const int at = (j + L * s) * kN + e;
+        *reinterpret_cast<f32x4*>(out + at) =
+            f32x4{dw[s][e], dw[s][e + 1], dw[s][e + 2], dw[s][e + 3]};
+        *reinterpret_cast<f32x4*>(out + a.d + at) =
+            f32x4{db[s][e], db[s][e + 1], db[s][e + 2], db[s][e + 3]};
+      }
     }
   }
 }
 
-// Columns over the groups: 32 lanes take a column each, the workgroup's 32 half
+// Columns over the groups: 32 lanes take a column each, the workgroup's 32 halves of
 // wavefronts a share of the groups.  blockIdx.y: dweight, dbias.
+constexpr int kJoinCols = 32;
 constexpr int kJoinShares = 32;
 template <typename T>
-__global__ __launch_bounds__(32 * kJoinShares) void k_norm_join(NormArgs a) {
-  __shared__ float lds[kJoinShares][32];
-  const int lane = threadIdx.x % 32, share = threadIdx.x / 32;
-  const int c = blockIdx.x * 32 + lane;
+__global__ __launch_bounds__(kJoinCols* kJoinShares) void k_norm_join(NormArgs a) {
+  __shared__ float lds[kJoinShares][kJoinCols];
+  const int lane = threadIdx.x % kJoinCols, share = threadIdx.x / kJoinCols;
+  const int c = blockIdx.x * kJoinCols + lane;
   void* const to = blockIdx.y == 0 ? a.dweight : a.dbias;
   if (to == nullptr) return;
   float sum = 0.0f;
   if (c < a.d) {
     const float* p = a.part + blockIdx.y * static_cast<int64_t>(a.d) + c;
-#pragma unroll 4
+#pragma unroll 16
     for (int i = share; i < a.groups; i += kJoinShares) sum += p[static_cast<int64_t>(i) * 2 * a.d];
   }
   lds[share][lane] = sum;
