@@ -295,7 +295,7 @@ struct Product {
         read_at_op(n, kSteps % 2, 0);
         // Load l behind the op l kOps / kLoads + 2, or the last one.
         unrolled<kLoads>([&](auto l) {
-          constexpr int at = l * 2;
+          constexpr int at = l * kOps / kLoads + 2;
           if constexpr (n == (at < kOps ? at : kOps - 1)) load(l, buf);
         });
       });

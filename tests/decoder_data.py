@@ -67,19 +67,28 @@ def nll_bounds(x, weight, labels, ignore, dloss, dtype, exact):
     # the token's weight (two roundings), and the rounding to the type.
     rel = (logit + b_lse + 2.0 ** -24 * (4 * most + 6))[:, None]
     b_g = p.abs() * (torch.expm1(rel) + b_loss[:, None]) + g.abs() * (4 * 2.0 ** -24)
-    if dtype != "f32":
-        b_g = b_g + (g.abs() + b_g) * HALF[dtype]
-    if dtype == "f16":
-        # Relative to the largest dloss, times 2^14: half a step of denormal numbers.
-        b_g = b_g + 2.0 ** -25 * 2.0 ** -14 * dloss.abs().max()
     # Exponentials below the normal numbers, 2^-126, are taken as 0 by the
     # instruction, and what the largest dloss leaves of g below them by the matrix
     # operations.
     b_g = b_g + 2.0 ** -125 * dloss.abs().max()
-    b_g = torch.where(live, b_g, 0.0)
-    gs, v, t = g.abs() + b_g, w.shape[0], x.shape[0]
-    b_dx = b_g @ w.abs() + (v + 64) * CUT * (gs @ w.abs())
-    b_dw = b_g.t() @ x.abs() + (t + 2) * CUT * (gs.t() @ x.abs())
+    rounding = torch.zeros_like(b_g)
+    if dtype != "f32":
+        # Up to 256 tokens g is held in two parts of the type.
+        few = int(live.sum()) <= 256
+        rounding = (g.abs() + b_g) * (HALF[dtype] ** 2 if few else HALF[dtype])
+        if dtype == "f16":
+            # Relative to the largest dloss, times 2^14: half a step of denormal numbers.
+            rounding = rounding + 2.0 ** -25 * 2.0 ** -14 * dloss.abs().max()
+    b_g, rounding = torch.where(live, b_g, 0.0), torch.where(live, rounding, 0.0)
+    b_gw = b_g + rounding
+    # dx takes in what the rounding left at the label, in fp32.
+    at = torch.where(live[:, 0] & (labels >= 0) & (labels < len(w)), labels, 0)[:, None]
+    rest = rounding.gather(1, at) * 2.0 ** -22 if dtype != "f32" else torch.zeros(len(at), 1)
+    b_gx = b_g + rounding.scatter(1, at, rest.to(rounding.dtype))
+    gs, v, t = g.abs() + b_gw, w.shape[0], x.shape[0]
+    # Products are summed in up to 64 splits, and g's two parts one after the other.
+    b_dx = b_gx @ w.abs() + (2 * v + 64) * CUT * (gs @ w.abs())
+    b_dw = b_gw.t() @ x.abs() + (2 * t + 64) * CUT * (gs.t() @ x.abs())
     out = [b_loss, b_lse, b_dx, b_dw]
     for i, want in ((2, dx), (3, dweight)):
         out[i] = out[i] + (want.abs() + out[i]) * (HALF[dtype] + 2.0 ** -24) + TINY[dtype]

@@ -50,6 +50,22 @@ def test_sizes(rows, vocab, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(data.TYPES))
+@pytest.mark.parametrize("rows,vocab,d", [(3100, 300, 4096), (4000, 4001, 24), (1700, 9000, 48)])
+def test_large_tiles(rows, vocab, d, dtype):
+    """Sizes whose products have large tiles, whole and ragged."""
+    check(*inputs(rows, vocab, d, dtype, ignored=0.05), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("live", [1, 255, 256, 257, 258])
+def test_around_the_tokens_of_two_parts(live, dtype):
+    """The number of tokens with a loss decides, whatever the rows."""
+    x, weight, labels, dloss = inputs(400, 300, 72, dtype)
+    labels[torch.randperm(400, generator=torch.Generator().manual_seed(live))[live:]] = IGNORE
+    check(x, weight, labels, dloss, dtype)
+
+
+@pytest.mark.parametrize("dtype", list(data.TYPES))
 @pytest.mark.parametrize("rows,vocab,d,share", [(1, 40, 8, 1.1), (70, 300, 64, 1.1), (70, 300, 64, 0.5),
                                                 (513, 260, 48, 0.9), (2000, 64, 16, 0.3)])
 def test_ignored_rows_cost_and_leave_nothing(rows, vocab, d, share, dtype):
