@@ -4,7 +4,10 @@
 
 Training packs documents of all lengths into one row of tokens:
 ``softmax_packed_attention`` keeps each document's tokens to themselves and
-gives the gradients.  Serving keeps the keys and values of all requests in one
+gives the gradients.  ``softmax_embedding`` takes the tokens' rows of the table,
+``softmax_layer_norm`` (without mean and weight) norms the residual stream, and
+``softmax_linear_nll`` takes the loss against the head's rows without keeping the
+logits, each with its gradients.  Serving keeps the keys and values of all requests in one
 paged cache: a step takes prompt chunks and single tokens of any requests
 together, ``softmax_cache_slots`` hands out blocks and slots for the new tokens
 on the device, ``softmax_cache_append`` writes their keys and values, and
@@ -44,25 +47,37 @@ class Decoder(torch.nn.Module):
         self.register_buffer("slopes", torch.tensor(
             [2.0 ** (-8.0 * (i + 1) / HEADS) for i in range(HEADS)], device=device))
 
-    def forward(self, tokens, attend):
-        """Logits of ``tokens``; ``attend(layer, q, k, v)`` is the attention of
-        [tokens, heads, d] slices of one projection."""
-        x = self.embed(tokens)
+    def hidden(self, tokens, attend):
+        """What the head takes of ``tokens``; ``attend(layer, q, k, v)`` is the
+        attention of [tokens, heads, d] slices of one projection."""
+        x = sm.softmax_embedding(tokens, self.embed.weight)
         for i in range(LAYERS):
             rows = self.qkv[i](_norm(x)).bfloat16().unflatten(1, (-1, HEAD))
             q, k, v = rows.split([HEADS, KV_HEADS, KV_HEADS], 1)
             x = x + self.out[i](attend(i, q, k, v).float().flatten(1))
             x = x + self.down[i](torch.relu(self.up[i](_norm(x))))
-        return self.head(_norm(x))
+        return _norm(x)
+
+    def forward(self, tokens, attend):
+        """Logits of ``tokens``."""
+        return self.head(self.hidden(tokens, attend))
+
+    def _within(self, cu):
+        return lambda _, q, k, v: sm.softmax_packed_attention(q, k, v, cu, cap=CAP,
+                                                              slopes=self.slopes)
 
     def packed(self, tokens, cu):
         """Logits of packed documents, differentiable."""
-        return self(tokens, lambda _, q, k, v: sm.softmax_packed_attention(
-            q, k, v, cu, cap=CAP, slopes=self.slopes))
+        return self(tokens, self._within(cu))
+
+    def losses(self, tokens, cu, labels):
+        """Each token's loss, 0 where its label is -100, differentiable."""
+        return sm.softmax_linear_nll(self.hidden(tokens, self._within(cu)), self.head.weight,
+                                     labels)
 
 
 def _norm(x):
-    return x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6)
+    return sm.softmax_layer_norm(x, eps=1e-6, center=False)
 
 
 class Server:
@@ -117,11 +132,9 @@ def train(model, g, table, steps):
     losses = []
     for _ in range(steps):
         tokens, cu, lens = documents(g, table, 24, 120)
-        last = cu[1:].long() - 1  # a document's last token has no successor in it
-        keep = torch.ones(len(tokens), dtype=torch.bool, device=tokens.device)
-        keep[last] = False
-        logp = torch.log_softmax(model.packed(tokens, cu), 1)
-        loss = -logp[keep].gather(1, tokens.roll(-1)[keep][:, None]).mean()
+        labels = tokens.roll(-1)
+        labels[cu[1:].long() - 1] = -100  # a document's last token has no successor in it
+        loss = model.losses(tokens, cu, labels).sum() / (len(tokens) - len(lens))
         opt.zero_grad()
         loss.backward()
         opt.step()

@@ -150,3 +150,35 @@ def test_outputs_that_are_given():
     assert float((loss.double().cpu() - want[0]).abs().max()) < 1e-4
     with pytest.raises(sm.SoftmaxError):        # the output is an input
         sm.softmax_embedding_fwd(ids, table[:150], out=table[:150])
+
+
+def test_example_losses_and_gradients():
+    """The example decoder's loss, against its own logits taken by elementary
+    operations."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "decoder.py")
+    spec = importlib.util.spec_from_file_location("example_decoder", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    torch.manual_seed(3)
+    model = example.Decoder()
+    g = torch.Generator().manual_seed(4)
+    tokens, cu, lens = example.documents(g, torch.randperm(example.VOCAB, generator=g), 9, 60)
+    labels = tokens.roll(-1)
+    labels[cu[1:].long() - 1] = -100
+    got = model.losses(tokens, cu, labels)
+    got.sum().backward()
+    grads = [p.grad.clone() for p in model.parameters()]
+    model.zero_grad()
+    logp = torch.log_softmax(model.packed(tokens, cu).double(), 1)
+    keep = labels != -100
+    want = torch.where(keep, -logp.gather(1, torch.where(keep, labels, 0)[:, None])[:, 0], 0.0)
+    want.sum().backward()
+    # fp32 throughout but for the attention, which both go through with the same
+    # inputs: 256 terms in a logit, each with a factor up to 64 of sizes.
+    assert float((got.double() - want).detach().abs().max()) < 64 * 256 * 2.0 ** -24
+    # The gradients pass through the attention's in bf16: half a step, twice over.
+    for p, grad in zip(model.parameters(), grads):
+        assert float((p.grad - grad).norm()) <= 2.0 ** -8 * float(p.grad.norm())
