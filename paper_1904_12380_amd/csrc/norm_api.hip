@@ -33,8 +33,9 @@ Shape wide() {
   else return instance<BACK, T, 1024, 2>();
 }
 
-// Forward: a wavefront holds up to eight strips per lane, a workgroup takes longer
-// rows, and rows that are too few to fill the device with a wavefront each.
+// Forward: a wavefront holds up to four strips per lane, a workgroup takes longer rows
+// (16384 x 4096 of bf16: 64 us with a wavefront and eight strips per lane, 50 with 256
+// threads and two), and rows that are too few to fill the device with a wavefront each.
 template <typename T>
 Shape forward_of(int64_t strips, int64_t rows) {
   constexpr bool B = false;

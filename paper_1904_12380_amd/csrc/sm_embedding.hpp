@@ -18,6 +18,9 @@
 //                   go to the workspace
 //   k_embed_join    sums the parts of those runs, in order
 //
+// 16384 tokens x 50001 x 2048 of bf16: lookup 26 us (4.9 TB/s); sort beside the clearing
+// 34 (6.1 TB/s), merge 9, sums 30, join 10.
+//
 // No atomics but in counts: the order of every sum follows from the ids alone.
 #pragma once
 
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(kSortThreads) void k_embed_sort(EmbedArgs a, int ti
 // Sorted tiles (key[1], token[1]) to one order (key[0], token[0]): before a token come
 // those of smaller ids, and those of its own id in earlier tiles.  Eight lanes take a
 // token, each every eighth tile: a bisection is a chain of loads, and a lane's up to
-// four are independent (16384 tokens: 36 us with one lane for all tiles, 8.3 so).
+// four are independent (16384 tokens: 36 us with one lane for all tiles, 8.8 so).
 constexpr int kMergeLanes = 8;
 template <int UNUSED>
 __global__ __launch_bounds__(kSortThreads) void k_embed_merge(EmbedArgs a, int tiles) {

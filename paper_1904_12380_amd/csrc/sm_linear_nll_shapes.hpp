@@ -12,8 +12,11 @@ NllProduct nll_shape() {
           64 * WM * WN};
 }
 
-// Up to kNllFew tokens: bound by the weight's bytes, so tiles are narrow in tokens.
-// Otherwise the largest tiles, unless they are too few to fill the device.
+// Up to kNllFew tokens: bound by the weight's bytes, so tiles are narrow in tokens
+// (forward, 50001 x 2048 of bf16: 64 tokens 44 us, 65 in the next tiles 54).  Otherwise
+// the largest tiles, unless they are too few to fill three quarters of the CUs (351
+// tokens x 10007 x 520 of fp16, 80 large tiles: 21.1 us with them, 13.8 with the small
+// ones).
 constexpr int64_t kNllFew = 64;
 
 template <typename T, int KIND>

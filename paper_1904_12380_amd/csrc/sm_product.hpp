@@ -20,10 +20,13 @@
 // alone 2110 against 1880 TFLOP/s.
 //
 // A wavefront's load into LDS writes 1024 bytes side by side, a block: whole rows, in
-// their order in memory, since lanes that fetch a 128-byte line in any other order
-// make more requests of it to the L2 (half as many again with chunks permuted by row,
-// as the attention's tiles have them).  Bank conflicts are avoided by which rows share
-// a block, and by blocks that lie 1056 bytes apart (Side).
+// their order in memory.  Bank conflicts are avoided by which rows share a block, and
+// by blocks that lie 1056 bytes apart (Side); a read's address is then one register
+// and constants.
+//
+// What bounds the large tiles is power: on random values the clock is 1.8 GHz, with
+// the matrix pipes busy 64 to 72% of the cycles, and the forward product of 4096 x
+// 131072 x 4096 of bf16 runs at 1390 TFLOP/s (on zeros, at the full clock, 1700).
 #pragma once
 
 #include <utility>
