@@ -98,8 +98,8 @@ template <typename T>
 constexpr float kUnitUp = __is_same(T, f16) ? 0x1p14f : 1.0f;
 
 // Tokens with a loss up to which g of 16-bit types is kept in two parts: the backward
-// pass of 256 tokens x 50001 x 2048 of bf16 takes 424 us with two, that of 257 tokens
-// 370 with one.
+// pass of 256 tokens x 50001 x 2048 of bf16 takes 406 us with two, that of 257 tokens
+// 344 with one.
 constexpr int kTwoParts = 256;
 template <typename T>
 __device__ __forceinline__ int parts_of(int live) {

@@ -10,6 +10,7 @@ namespace smx {
 struct NllProduct {
   const void* fn;
   int bm, bn, threads;
+  int resident;  // workgroups of a CU that a split counts on
 };
 
 constexpr int kNarrow = 0, kSmall = 1, kLarge = 2;

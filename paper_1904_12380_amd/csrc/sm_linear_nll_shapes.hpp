@@ -8,15 +8,18 @@ namespace smx {
 
 template <typename T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
 NllProduct nll_shape() {
+  typedef Product<T, NllShape<KIND>::kARows, NllShape<KIND>::kBRows, BM, BN, WM, WN, STAGES> P;
   return {reinterpret_cast<const void*>(&k_nll_product<T, KIND, BM, BN, WM, WN, STAGES>), BM, BN,
-          64 * WM * WN};
+          64 * WM * WN, P::kLds <= 72 * 1024 ? 2 : 1};
 }
 
 // Up to kNllFew tokens: bound by the weight's bytes, so tiles are narrow in tokens
 // (forward, 50001 x 2048 of bf16: 64 tokens 44 us, 65 in the next tiles 54).  Otherwise
 // the largest tiles, unless they are too few to fill three quarters of the CUs (351
 // tokens x 10007 x 520 of fp16, 80 large tiles: 21.1 us with them, 13.8 with the small
-// ones).
+// ones) or half of each would be empty (probabilities of 128 tokens x 50001 x 2048 85 us,
+// with small ones 67).  dweight of few tokens keeps the large ones: 128 tokens 111 us,
+// with small ones 123.
 constexpr int64_t kNllFew = 64;
 
 template <typename T, int KIND>
@@ -38,7 +41,9 @@ template <typename T>
 NllProduct nll_product_of(int kind, int64_t m, int64_t n) {
   constexpr int64_t kEdge = sizeof(T) == 2 ? 256 : 128;
   const int64_t tiles = ((m + kEdge - 1) / kEdge) * ((n + kEdge - 1) / kEdge);
-  const int size = kind != kWeight && n <= kNllFew ? kNarrow : tiles >= 192 ? kLarge : kSmall;
+  const bool tokens = kind != kWeight;  // n
+  const int size = tokens && n <= kNllFew                           ? kNarrow
+                   : tiles >= 192 && !(tokens && n <= kEdge / 2) ? kLarge : kSmall;
   switch (kind) {
     case kLogits: return nll_shape_of<T, kLogits>(size);
     case kProbs: return nll_shape_of<T, kProbs>(size);
