@@ -56,6 +56,12 @@ def test_large_tiles(rows, vocab, d, dtype):
     check(*inputs(rows, vocab, d, dtype, ignored=0.05), dtype)
 
 
+@pytest.mark.parametrize("dtype", list(data.TYPES))
+def test_many_rows(dtype):
+    """More rows than a packing workgroup takes at a time, a third of them ignored."""
+    check(*inputs(70001, 130, 16, dtype, ignored=0.33), dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("live", [1, 255, 256, 257, 258])
 def test_around_the_tokens_of_two_parts(live, dtype):
