@@ -158,6 +158,25 @@ hipError_t pack(NllArgs* a, int dtype, hipStream_t stream) {
   return start(fn, ceil_div(a->rows, each), 1, 256, args, stream);
 }
 
+// lse and loss from the tiles' statistics.  A launch of 2^32 threads or more wraps
+// around without an error: 16 threads for each of at most 2^27 tokens at a time.
+hipError_t join(NllArgs a, hipStream_t stream) {
+  constexpr int64_t kMost = int64_t(1) << 27;
+  const int64_t rows = a.rows;
+  hipError_t e = hipSuccess;
+  for (int64_t from = 0; from < rows && e == hipSuccess; from += kMost) {
+    const int64_t some = std::min(rows - from, kMost);
+    a.rows = static_cast<int>(some);
+    void* args[] = {&a};
+    e = start(reinterpret_cast<const void*>(&k_nll_join<16>), ceil_div(some, kJoinTokens), 1,
+              16 * kJoinTokens, args, stream);
+    a.place += some;
+    a.loss += some;
+    a.lse += some;
+  }
+  return e;
+}
+
 hipError_t multiply_tiles(const NllProduct& p, int64_t m, int64_t n, int64_t splits, NllArgs* a,
                           hipStream_t stream) {
   void* args[] = {a};
@@ -204,12 +223,7 @@ SOFTMAX_API int softmax_linear_nll_fwd(const void* x, int64_t x_stride, const vo
   a.piece = static_cast<int>(up_to(vocab, kTile));
   hipError_t e = pack<false>(&a, dtype, stream);
   if (e == hipSuccess) e = multiply_tiles(p, vocab, rows, 1, &a, stream);
-  if (e == hipSuccess) {
-    void* args[] = {&a};
-    e = start(reinterpret_cast<const void*>(&k_nll_join<16>), ceil_div(rows, kJoinTokens), 1,
-              16 * kJoinTokens, args,
-              stream);
-  }
+  if (e == hipSuccess) e = join(a, stream);
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
 }
 

@@ -6,7 +6,8 @@
 
 namespace smx_host {
 
-// Rows and tokens of a call: a launch with four threads for each stays below 2^32.
+// Rows and tokens of a call: indices stay below 2^31, and a launch with four threads
+// for each below 2^32.
 constexpr int64_t kMaxRows = int64_t(1) << 29;
 
 inline bool width_ok(int64_t d) { return d >= 8 && d <= SOFTMAX_MAX_WIDTH && d % 8 == 0; }
