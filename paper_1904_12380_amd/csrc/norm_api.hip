@@ -12,6 +12,8 @@ namespace {
 using namespace smx;
 using namespace smx_host;
 
+constexpr int64_t kMostThreads = int64_t(1) << 31;  // of a launch
+
 struct Shape {
   const void* fn;
   int lanes;
@@ -112,22 +114,27 @@ SOFTMAX_API int softmax_layer_norm_fwd(const void* x, int64_t x_stride, const vo
   const int rc = check_ranges(inputs, outputs);
   if (rc != SOFTMAX_OK) return rc;
   NormArgs a = {};
-  a.x = x;
   a.x_pitch = x_stride;
   a.weight = weight;
   a.bias = bias;
-  a.out = y;
-  a.mean = mean;
-  a.rstd = rstd;
-  a.rows = static_cast<int>(rows);
   a.d = static_cast<int>(d);
   a.eps = eps;
   const Shape s = forward_shape(dtype, strips_of(d, dtype), rows);
   const int threads = std::max(s.lanes, 256);
-  const int64_t grid = ceil_div(rows, threads / s.lanes);
-  if (grid >= (int64_t(1) << 32) / threads) return SOFTMAX_ERR_INVALID_ARG;
-  void* args[] = {&a};
-  const hipError_t e = launch(s.fn, grid, threads, args, stream);
+  const int64_t each = threads / s.lanes;
+  // A launch takes fewer than 2^32 threads.
+  const int64_t most = kMostThreads / threads * each;
+  hipError_t e = hipSuccess;
+  for (int64_t from = 0; from < rows && e == hipSuccess; from += most) {
+    const int64_t some = std::min(rows - from, most);
+    a.x = static_cast<const char*>(x) + from * x_stride * size;
+    a.out = static_cast<char*>(y) + from * d * size;
+    a.mean = mean == nullptr ? nullptr : mean + from;
+    a.rstd = rstd + from;
+    a.rows = static_cast<int>(some);
+    void* args[] = {&a};
+    e = launch(s.fn, ceil_div(some, each), threads, args, stream);
+  }
   return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
 }
 

@@ -36,3 +36,20 @@ def test_loss_of_more_rows_than_one_launch_joins():
     for name, got, want, bound in zip(("loss", "lse"), (loss, lse), exact, bounds):
         data.close(name, got[at], want, bound)
         assert int(got.count_nonzero()) == 50
+
+
+def test_norm_of_more_wide_rows_than_one_launch_takes():
+    """2^24 rows and a few of a workgroup each."""
+    rows, d = (1 << 24) + 3, 2056
+    room(100)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(1, d, device="cuda", generator=g).bfloat16()
+    y, mean, rstd = sm.softmax_layer_norm_fwd(x.expand(rows, d))
+    want = oracle.layer_norm(x.cpu())
+    # Sums of 2056 terms by at most 33 roundings in a row; y's own rounding on top.
+    assert abs(float(mean[0]) - float(want[1])) < 40 * 2.0 ** -24 * float(x.double().abs().mean())
+    data.close("y", y[:1], want[0], want[0].abs() * 2.0 ** -8 + 1e-4)
+    assert torch.equal(mean, mean[:1].expand(rows)) and torch.equal(rstd, rstd[:1].expand(rows))
+    for at in range(0, rows, 1 << 20):
+        some = y[at:at + (1 << 20)]
+        assert torch.equal(some, y[:1].expand(len(some), d)), at
