@@ -13,8 +13,8 @@
  * in fp32 or more, and results rounded once.  Results are bitwise deterministic.
  *
  * Layout: rows of d entries side by side; d is a multiple of 8 up to
- * SOFTMAX_MAX_WIDTH.  Strides between rows are in elements, not negative, and with
- * the data multiples of 16 bytes.  What a call writes is contiguous, and overlaps
+ * SOFTMAX_MAX_WIDTH.  Rows and tokens are at most 2^29.  Strides between rows are in
+ * elements, not negative, and with the data multiples of 16 bytes.  What a call writes is contiguous, and overlaps
  * neither its inputs nor anything else that it writes.  Where there are no rows,
  * pointers may be null.
  *
@@ -58,8 +58,9 @@ SOFTMAX_API int64_t softmax_linear_nll_fwd_workspace(int64_t rows, int64_t vocab
  *
  * This is softmax_nll_fwd of x weight^T without a clip: the row softmax of the
  * paper's Sec. 1.1 Eq. (1) behind the product that makes its logits.  A row whose
- * logits hold NaN or +infinity has no finite loss.  rows and vocab are at most
- * 2^29, and there are fewer than 2^23 tiles of 256 x 256 (fp32: 2^24 of 128 x 128).
+ * logits hold NaN or +infinity has no finite loss.  vocab is at most 2^29, and of
+ * rows x vocab, rows x d and vocab x d each has fewer than 2^23 - 64 tiles of 256 x 256
+ * (fp32: 2^24 - 64 of 128 x 128).
  */
 SOFTMAX_API int softmax_linear_nll_fwd(const void* x, int64_t x_stride, const void* weight,
                                        int64_t w_stride, const int64_t* labels, int64_t rows,
@@ -106,8 +107,8 @@ SOFTMAX_API int softmax_linear_nll_bwd(const float* dloss, const void* x, int64_
  *
  *   ids    device, [tokens] int64; an id outside [0, rows), such as -1, is padding
  *          and gets zeros
- *   table  [rows, d], rows table_stride apart
- *   out    [tokens, d]; written
+ *   table  [rows, d], rows table_stride apart (at most SOFTMAX_MAX_ROW_STRIDE)
+ *   out    [tokens, d], at most 2^38 - 2^14 bytes; written
  *   scale  finite
  */
 SOFTMAX_API int softmax_embedding_fwd(const int64_t* ids, int64_t tokens, const void* table,
@@ -125,8 +126,6 @@ SOFTMAX_API int64_t softmax_embedding_bwd_workspace(int64_t tokens, int64_t rows
  *
  *   dout    [tokens, d], rows dout_stride apart
  *   dtable  [rows, d]; written in full (zeros for rows that no token has)
- *
- * tokens and rows are at most 2^29.
  */
 SOFTMAX_API int softmax_embedding_bwd(const void* dout, int64_t dout_stride, const int64_t* ids,
                                       int64_t tokens, int64_t rows, int64_t d, float scale,
@@ -147,6 +146,10 @@ SOFTMAX_API int softmax_embedding_bwd(const void* dout, int64_t dout_stride, con
  *   y       [rows, d]; written
  *   mean    [rows] fp32, written; NULL exactly where center = 0
  *   rstd    [rows] fp32; written
+ *
+ * The sums over a row are held in fp32: where one of them is past its range (entries
+ * from 10^17 on) rstd is 0 or NaN, and where all squares are below it (entries under
+ * 10^-19, which only matters with eps = 0) rstd is infinite.
  */
 SOFTMAX_API int softmax_layer_norm_fwd(const void* x, int64_t x_stride, const void* weight,
                                        const void* bias, int64_t rows, int64_t d, float eps,
