@@ -38,7 +38,8 @@ HIPCC_FLAGS = [
     "-ffp-contract=off",
     # No packed fp32 instructions in any generated code.
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    "-Wall",
+    # Warnings end the build: a quiet one hides them.
+    "-Wall", "-Werror",
     "-Wno-unused-command-line-argument",
 ]
 

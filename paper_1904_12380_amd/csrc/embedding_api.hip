@@ -101,7 +101,7 @@ SOFTMAX_API int softmax_embedding_fwd(const int64_t* ids, int64_t tokens, const 
   if (grid < 0) return SOFTMAX_ERR_INVALID_ARG;
   const Range inputs[] = {{ids, tokens * 8}, {table, tb}};
   const Range outputs[] = {{out, tokens * d * size}};
-  const const int rc = check_ranges(inputs, outputs);
+  const int rc = check_ranges(inputs, outputs);
   if (rc != SOFTMAX_OK) return rc;
   EmbedArgs a = {};
   a.ids = ids;
