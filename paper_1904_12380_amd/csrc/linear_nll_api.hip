@@ -85,8 +85,9 @@ int64_t splits_of(const NllProduct& p, int64_t m, int64_t n, int64_t k, int dtyp
   return best;
 }
 
+// Of the pieces, in whole tiles, the first has `most` rows of the vocabulary.
 struct Backward {
-  int64_t g, rest, sums, w_sums, end, piece, splits, w_splits;
+  int64_t g, rest, sums, w_sums, end, piece, most, splits, w_splits;
 };
 
 Backward backward_room(int64_t rows, int64_t vocab, int64_t d, int dtype) {
@@ -94,11 +95,12 @@ Backward backward_room(int64_t rows, int64_t vocab, int64_t d, int dtype) {
   const int64_t padded = up_to(rows, kTile);
   Backward b;
   b.piece = piece_of(rows, vocab, d, size);
-  b.splits = splits_of(product(kInput, d, rows, dtype), d, rows, b.piece, dtype);
+  b.most = std::min(b.piece, vocab);
+  b.splits = splits_of(product(kInput, d, rows, dtype), d, rows, b.most, dtype);
   // dweight is many tiles, but for a small vocabulary.
-  const NllProduct w = product(kWeight, d, b.piece, dtype);
-  const bool few = ceil_div(d, w.bm) * ceil_div(b.piece, w.bn) < kCus / 2;
-  b.w_splits = few ? splits_of(w, d, b.piece, rows, dtype) : 1;
+  const NllProduct w = product(kWeight, d, b.most, dtype);
+  const bool few = ceil_div(d, w.bm) * ceil_div(b.most, w.bn) < kCus / 2;
+  b.w_splits = few ? splits_of(w, d, b.most, rows, dtype) : 1;
   b.g = room(rows, d, size).more;
   b.rest = b.g + padded * b.piece * size;
   b.sums = b.rest + (size == 2 ? kTwoParts * b.piece * size : 0);
@@ -288,16 +290,16 @@ SOFTMAX_API int softmax_linear_nll_bwd(const float* dloss, const void* x, int64_
   for (int64_t from = 0; from < vocab && e == hipSuccess; from += b.piece) {
     a.from = static_cast<int>(from);
     const int64_t left = std::min(vocab - from, b.piece);
-    e = multiply_tiles(product(kProbs, b.piece, rows, dtype), left, rows, 1, &a, stream);
+    e = multiply_tiles(product(kProbs, b.most, rows, dtype), left, rows, 1, &a, stream);
     if (e == hipSuccess && dx != nullptr)
       e = multiply_tiles(product(kInput, d, rows, dtype), d, rows, b.splits, &a, stream);
     if (e == hipSuccess && dweight != nullptr)
-      e = multiply_tiles(product(kWeight, d, b.piece, dtype), d, left, b.w_splits, &a, stream);
+      e = multiply_tiles(product(kWeight, d, b.most, dtype), d, left, b.w_splits, &a, stream);
     if (e == hipSuccess && dweight != nullptr && b.w_splits > 1) {
       const void* fn = dtype == SOFTMAX_F32 ? reinterpret_cast<const void*>(&k_nll_weight<float>)
                        : dtype == SOFTMAX_F16 ? reinterpret_cast<const void*>(&k_nll_weight<f16>)
                                               : reinterpret_cast<const void*>(&k_nll_weight<bf16>);
-      e = start(fn, std::min<int64_t>(ceil_div(b.piece * d / 4, 256), 16 * kCus), 1, 256, args,
+      e = start(fn, std::min<int64_t>(ceil_div(left * d / 4, 256), 16 * kCus), 1, 256, args,
                 stream);
     }
   }
