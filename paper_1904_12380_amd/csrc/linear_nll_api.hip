@@ -42,12 +42,6 @@ Room room(int64_t rows, int64_t d, int size) {
 }
 static_assert(sizeof(NllHead) <= kAlign, "the head's place");
 
-int64_t forward_bytes(int64_t rows, int64_t vocab, int64_t d, int dtype) {
-  const int64_t padded = up_to(rows, kTile);
-  const int64_t tiles = ceil_div(vocab, product(kLogits, vocab, rows, dtype).bm);
-  return room(rows, d, dtype_size(dtype)).more + padded * 4 + tiles * padded * 8;
-}
-
 // The piece of the vocabulary whose g is kept at a time: what fits kPieceBytes, in
 // whole rounds of dweight's tiles over the CUs (8192 tokens x 50001 x 2048 of bf16: 8
 // rounds in two equal pieces, 7 in pieces of 128 and 68 tiles of the vocabulary).
@@ -67,11 +61,12 @@ int64_t piece_of(int64_t rows, int64_t vocab, int64_t d, int size) {
 // Splits of the sums behind a product's tiles: as few as leave at most a tenth of the
 // device idle, or else those that leave the least, with all workgroups that a CU holds
 // (dx of 512 tokens x 50001 x 2048 of bf16: 208 us with one, 142 with two); a split has
-// four stages or more.
-int64_t splits_of(const NllProduct& p, int64_t m, int64_t n, int64_t k, int dtype) {
+// `least` stages or more.
+int64_t splits_of(const NllProduct& p, int64_t m, int64_t n, int64_t k, int dtype,
+                  int64_t least = 4) {
   const int64_t tiles = ceil_div(m, p.bm) * ceil_div(n, p.bn);
   const int64_t stages = ceil_div(k * dtype_size(dtype), kLineBytes);
-  const int64_t most = std::clamp<int64_t>(stages / 4, 1, 64);
+  const int64_t most = std::clamp<int64_t>(stages / least, 1, 64);
   const int64_t slots = kCus * p.resident;
   int64_t best = 1;
   double full = 0.0;
@@ -85,9 +80,33 @@ int64_t splits_of(const NllProduct& p, int64_t m, int64_t n, int64_t k, int dtyp
   return best;
 }
 
+// Splits of d for the logits, the same in both passes, which form equal ones: of fp32,
+// whose matrix ops take 16 times as long, where the tiles leave a quarter of the CUs
+// without one.  16 stages each pay for the partial logits, or 8 where the tiles are very
+// few (fp32 forward calls, not split and split: 30 tokens x 969 x 4096 171 and 31 us, 64 x
+// 15000 x 1024 52 and 43; 256 x 3000 x 512 23 and 26 with 8 stages, not split now).
+int64_t d_splits_of(int64_t rows, int64_t vocab, int64_t d, int dtype) {
+  if (dtype != SOFTMAX_F32) return 1;
+  const NllProduct p = nll_product_f32(kPartial, vocab, rows);
+  const int64_t tiles = ceil_div(vocab, p.bm) * ceil_div(rows, p.bn);
+  return tiles < kCus * 3 / 4 ? splits_of(p, vocab, rows, d, dtype, tiles < kCus / 4 ? 8 : 16) : 1;
+}
+
+int64_t logits_bytes(int64_t rows, int64_t vocab, int64_t splits) {
+  return splits > 1 ? splits * up_to(rows, kTile) * up_to(vocab, kTile) * 4 : 0;
+}
+
+int64_t forward_bytes(int64_t rows, int64_t vocab, int64_t d, int dtype) {
+  const int64_t padded = up_to(rows, kTile);
+  const int64_t splits = d_splits_of(rows, vocab, d, dtype);
+  const int64_t tiles = ceil_div(vocab, product(kLogits, vocab, rows, dtype).bm);
+  return room(rows, d, dtype_size(dtype)).more +
+         (splits > 1 ? logits_bytes(rows, vocab, splits) : padded * 4 + tiles * padded * 8);
+}
+
 // Of the pieces, in whole tiles, the first has `most` rows of the vocabulary.
 struct Backward {
-  int64_t g, rest, sums, w_sums, end, piece, most, splits, w_splits;
+  int64_t g, rest, sums, w_sums, logits, end, piece, most, splits, w_splits, d_splits;
 };
 
 Backward backward_room(int64_t rows, int64_t vocab, int64_t d, int dtype) {
@@ -105,7 +124,9 @@ Backward backward_room(int64_t rows, int64_t vocab, int64_t d, int dtype) {
   b.rest = b.g + padded * b.piece * size;
   b.sums = b.rest + (size == 2 ? kTwoParts * b.piece * size : 0);
   b.w_sums = b.sums + b.splits * padded * up_to(d * size, kLineBytes) / size * 4;
-  b.end = b.w_sums + (b.w_splits > 1 ? b.w_splits * b.piece * d * 4 : 0);
+  b.logits = b.w_sums + up_to(b.w_splits > 1 ? b.w_splits * b.piece * d * 4 : 0, kAlign);
+  b.d_splits = d_splits_of(rows, vocab, d, dtype);
+  b.end = b.logits + logits_bytes(rows, vocab, b.d_splits);
   return b;
 }
 
@@ -138,6 +159,7 @@ void set_call(NllArgs* a, const void* x, int64_t x_stride, const void* weight, i
   a->d = static_cast<int>(d);
   a->padded_rows = static_cast<int>(up_to(rows, kTile));
   a->padded_d = static_cast<int>(up_to(d * size, kLineBytes) / size);
+  a->padded_vocab = static_cast<int>(up_to(vocab, kTile));
   a->head = reinterpret_cast<NllHead*>(at);
   a->place = reinterpret_cast<int*>(at + r.place);
   a->token = reinterpret_cast<NllToken*>(at + r.token);
@@ -218,6 +240,18 @@ SOFTMAX_API int softmax_linear_nll_fwd(const void* x, int64_t x_stride, const vo
   set_call(&a, x, x_stride, weight, w_stride, labels, rows, vocab, d, ignore, size, workspace);
   a.loss = loss;
   a.lse = lse;
+  const int64_t splits = d_splits_of(rows, vocab, d, dtype);
+  if (splits > 1) {
+    a.d_splits = static_cast<int>(splits);
+    a.logits = reinterpret_cast<float*>(static_cast<char*>(workspace) + room(rows, d, size).more);
+    hipError_t e = pack<false>(&a, dtype, stream);
+    if (e == hipSuccess)
+      e = multiply_tiles(nll_product_f32(kPartial, vocab, rows), vocab, rows, splits, &a, stream);
+    void* args[] = {&a};
+    if (e == hipSuccess)
+      e = start(reinterpret_cast<const void*>(&k_nll_total<256>), rows, 1, 256, args, stream);
+    return e == hipSuccess ? SOFTMAX_OK : fail_hip(e);
+  }
   const NllProduct p = product(kLogits, vocab, rows, dtype);
   a.tiles = static_cast<int>(ceil_div(vocab, p.bm));
   a.at = reinterpret_cast<float*>(static_cast<char*>(workspace) + room(rows, d, size).more);
@@ -281,6 +315,8 @@ SOFTMAX_API int softmax_linear_nll_bwd(const float* dloss, const void* x, int64_
   a.g_rest = static_cast<char*>(workspace) + b.rest;
   a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + b.sums);
   a.w_sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + b.w_sums);
+  a.logits = reinterpret_cast<float*>(static_cast<char*>(workspace) + b.logits);
+  a.d_splits = static_cast<int>(b.d_splits);
   a.piece = static_cast<int>(b.piece);
   a.splits = static_cast<int>(b.splits);
   a.w_splits = static_cast<int>(b.w_splits);
@@ -290,7 +326,15 @@ SOFTMAX_API int softmax_linear_nll_bwd(const float* dloss, const void* x, int64_
   for (int64_t from = 0; from < vocab && e == hipSuccess; from += b.piece) {
     a.from = static_cast<int>(from);
     const int64_t left = std::min(vocab - from, b.piece);
-    e = multiply_tiles(product(kProbs, b.most, rows, dtype), left, rows, 1, &a, stream);
+    if (b.d_splits > 1) {  // few tiles are one piece
+      e = multiply_tiles(nll_product_f32(kPartial, vocab, rows), vocab, rows, b.d_splits, &a, stream);
+      if (e == hipSuccess)
+        e = start(reinterpret_cast<const void*>(&k_nll_grad<256>),
+                  std::min<int64_t>(ceil_div(rows * ceil_div(vocab, 4), 256), 16 * kCus), 1, 256,
+                  args, stream);
+    } else {
+      e = multiply_tiles(product(kProbs, b.most, rows, dtype), left, rows, 1, &a, stream);
+    }
     if (e == hipSuccess && dx != nullptr)
       e = multiply_tiles(product(kInput, d, rows, dtype), d, rows, b.splits, &a, stream);
     if (e == hipSuccess && dweight != nullptr)

@@ -5,14 +5,17 @@
 //                   goes to row place[t] of a matrix with rows of whole stages,
 //                   so that tokens without a loss cost nothing in the products,
 //                   whatever their x holds, and strides and row tails end here.
-//   k_nll_product   four products of tiles (sm_product.hpp):
+//   k_nll_product   products of tiles (sm_product.hpp):
 //     kLogits   logits of a tile of the vocabulary by tokens; what stays of them
 //               is each token's maximum and sum of exponentials over the tile
 //     kProbs    the same logits again, turned into g = dl/dlogit, kept for a
 //               piece of the vocabulary
 //     kInput    sums over the piece's rows for dx, in splits, fp32
 //     kWeight   sums over the tokens for the piece's rows of dweight, whole
+//     kPartial  fp32: logits over a split of d, kept, where their tiles are few
 //   k_nll_join      the tiles' statistics to lse and loss
+//   k_nll_total     kPartial's sums to lse and loss
+//   k_nll_grad      kPartial's sums to g
 //   k_nll_input     the splits' sums to dx
 //
 // The products are bound by the matrix ops where there are thousands of tokens, by the
@@ -21,7 +24,8 @@
 // x 50001 x 2048 of bf16: pack 16 us, logits 1253, join 7; pack 29, probabilities 1426,
 // dx 1216, dweight 1303, join of dx 24.
 //
-// The logits are formed in both passes by the same operations in the same order.
+// The logits are formed in both passes by the same operations in the same order, also
+// where d is split.
 // Of g the label's entry is taken from the loss, e^-loss - 1, which keeps it exact
 // where the likelihood is near 1 and lse and the label's logit cancel.
 //
@@ -45,7 +49,7 @@ namespace smx {
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kNoLogit = -__builtin_inff();
-constexpr int kLogits = 0, kProbs = 1, kInput = 2, kWeight = 3;
+constexpr int kLogits = 0, kProbs = 1, kInput = 2, kWeight = 3, kPartial = 4;
 
 // What the products know of a token: g = e^(logit - lse) * weight, and `label_g`
 // at the label (-1: the label is no row of the vocabulary).
@@ -85,10 +89,13 @@ struct NllArgs {
   float* at;              // forward: the label's logit [padded_rows]
   char* g;                // backward: [padded_rows, piece] of the type
   char* g_rest;           // [kTwoParts, piece]: what the rounding of g left
+  float* logits;          // d_splits > 1: [d_splits, padded_rows, padded_vocab]
   float* sums;            // backward: [splits, padded_rows, padded_d]
   float* w_sums;          // backward, w_splits > 1: [w_splits, piece, d]
   int tiles;              // tiles of the vocabulary that `part` has
   int from, piece;        // backward: first row of the piece, and its padded length
+  int padded_vocab;       // vocab, in whole tiles
+  int d_splits;           // of d, for the logits
   int splits;             // of the piece's rows, for dx
   int w_splits;           // of the tokens, for dweight
 };
@@ -219,7 +226,8 @@ __device__ __forceinline__ f32x4 rest_of(f32x4 v) {
 
 template <int KIND>
 struct NllShape {
-  static constexpr bool kARows = KIND == kLogits || KIND == kProbs;  // m by rows
+  // m by rows
+  static constexpr bool kARows = KIND == kLogits || KIND == kProbs || KIND == kPartial;
   static constexpr bool kBRows = KIND != kWeight;
 };
 
@@ -227,6 +235,7 @@ struct NllShape {
 // lie side by side in the result are the rows (m) of the tile:
 //
 //     kLogits, kProbs   m: vocabulary   n: tokens      k: d
+//     kPartial          m: vocabulary   n: tokens      k: d (split)
 //     kInput            m: d            n: tokens      k: vocabulary (piece, split)
 //     kWeight           m: d            n: vocabulary  k: tokens
 template <typename T, int KIND, int BM, int BN, int WM, int WN, int STAGES>
@@ -241,8 +250,9 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
   const int rows = (live + BN - 1) / BN;  // tiles of tokens
   const int left = min(a.vocab - a.from, a.piece);  // of the vocabulary
   int mt, nt;
-  const int mtiles = KIND == kLogits  ? (a.vocab + BM - 1) / BM
-                     : KIND == kProbs ? (left + BM - 1) / BM : (a.d + BM - 1) / BM;
+  const int mtiles = KIND == kLogits || KIND == kPartial ? (a.vocab + BM - 1) / BM
+                     : KIND == kProbs                    ? (left + BM - 1) / BM
+                                                         : (a.d + BM - 1) / BM;
   const int ntiles = KIND == kWeight ? (left + BN - 1) / BN : rows;
   if (!tile_of(blockIdx.x, mtiles, ntiles, &mt, &nt)) return;
   const int m0 = mt * BM, n0 = nt * BN;
@@ -257,18 +267,22 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
     typename P::B y(a.packed, packed_pitch, n0, live, 0, wave);
     p.run(x, y, lds, a.d, wave);
   } else {
-    // A split's share of the piece, or of the tokens, in whole stages.
-    const int all = KIND == kInput ? left : live;
+    // A split's share of the piece, of the tokens or of d, in whole stages.
+    const int all = KIND == kInput ? left : KIND == kPartial ? a.d : live;
     const int stages = (all + P::A::kK - 1) / P::A::kK;
-    const int splits = KIND == kInput ? a.splits : a.w_splits;
+    const int splits = KIND == kInput ? a.splits : KIND == kPartial ? a.d_splits : a.w_splits;
     const int s0 = static_cast<int>(static_cast<int64_t>(stages) * blockIdx.y / splits);
     const int s1 = static_cast<int>(static_cast<int64_t>(stages) * (blockIdx.y + 1) / splits);
     const int64_t k0 = static_cast<int64_t>(s0) * P::A::kK;
     const int64_t k = max(min(static_cast<int64_t>(s1) * P::A::kK, static_cast<int64_t>(all)) - k0,
                           static_cast<int64_t>(0));
-    for (int part = 0; part < parts_of<T>(live); ++part) {
+    for (int part = 0; part < (KIND == kPartial ? 1 : parts_of<T>(live)); ++part) {
       const char* g = part == 0 ? a.g : a.g_rest;
-      if constexpr (KIND == kInput) {
+      if constexpr (KIND == kPartial) {
+        typename P::A x(weight, a.w_pitch, m0, a.vocab, k0, wave);
+        typename P::B y(a.packed, packed_pitch, n0, live, k0, wave);
+        p.run(x, y, lds, k, wave);
+      } else if constexpr (KIND == kInput) {
         typename P::A x(weight, a.w_pitch, m0, a.d, k0, wave);
         typename P::B y(g, g_pitch, n0, live, k0, wave);
         p.run(x, y, lds, k, wave);
@@ -370,6 +384,17 @@ __global__ __launch_bounds__(64 * WM * WN) void k_nll_product(NllArgs a) {
           *reinterpret_cast<f32x4*>(out + (m4 + 16 * i) * 4) = p.acc[i][j];
       }
     }
+  } else if constexpr (KIND == kPartial) {
+    float* const logits =
+        a.logits + static_cast<int64_t>(blockIdx.y) * a.padded_rows * a.padded_vocab;
+#pragma unroll
+    for (int j = 0; j < P::kNT; ++j) {
+      const int row = nw + 16 * j;
+      if (row >= live) continue;
+      float* const out = logits + static_cast<int64_t>(row) * a.padded_vocab + m4;
+#pragma unroll
+      for (int i = 0; i < P::kMT; ++i) *reinterpret_cast<f32x4*>(out + 16 * i) = p.acc[i][j];
+    }
   } else if constexpr (KIND == kInput) {
     float* const sums = a.sums + static_cast<int64_t>(blockIdx.y) * a.padded_rows * a.padded_d;
 #pragma unroll
@@ -470,6 +495,96 @@ __global__ __launch_bounds__(kJoinTokens* SHARES) void k_nll_join(NllArgs a) {
   }
   a.lse[t] = lse;
   a.loss[t] = loss;
+}
+
+// Four logits of a token, v and on, from the splits of d.
+__device__ __forceinline__ f32x4 logits_of(const NllArgs& a, int row, int v) {
+  const float* p = a.logits + static_cast<int64_t>(row) * a.padded_vocab + v;
+  const int64_t each = static_cast<int64_t>(a.padded_rows) * a.padded_vocab;
+  f32x4 sum = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll 4
+  for (int s = 1; s < a.d_splits; ++s) sum += *reinterpret_cast<const f32x4*>(p + s * each);
+  return sum;
+}
+
+// lse and loss as k_nll_join has them, from the splits' logits: a workgroup for each
+// token, whose threads take eight logits at a time.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_nll_total(NllArgs a) {
+  __shared__ float m_lds[THREADS / 64];
+  __shared__ double s_lds[THREADS / 64];
+  const int t = blockIdx.x, tid = threadIdx.x;
+  const int row = a.place[t];
+  if (row < 0) {
+    if (tid == 0) a.lse[t] = a.loss[t] = 0.0f;
+    return;
+  }
+  float m = kNoLogit;
+  double s = 0.0;
+  for (int v0 = 4 * tid; v0 < a.vocab; v0 += 8 * THREADS) {
+    float v[8];
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int at = v0 + u * 4 * THREADS;
+      f32x4 l = {};
+      if (at < a.vocab) l = logits_of(a, row, at);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[4 * u + j] = at + j < a.vocab ? l[j] : kNoLogit;
+        top = fmaxf(top, v[4 * u + j]);
+      }
+    }
+    const float ref = top == kNoLogit ? 0.0f : top;
+    s *= static_cast<double>(__builtin_amdgcn_exp2f((m - ref) * kLog2eF));
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      s += static_cast<double>(__builtin_amdgcn_exp2f((v[j] - ref) * kLog2eF));
+    m = top;
+  }
+  const float wave_m = seg_max<64>(m);
+  float ref = wave_m == kNoLogit ? 0.0f : wave_m;
+  s = wave_sum64(s * static_cast<double>(__builtin_amdgcn_exp2f((m - ref) * kLog2eF)));
+  if (tid % 64 == 0) {
+    m_lds[tid / 64] = wave_m;
+    s_lds[tid / 64] = s;
+  }
+  __syncthreads();
+  if (tid != 0) return;
+  m = m_lds[0];
+#pragma unroll
+  for (int w = 1; w < THREADS / 64; ++w) m = fmaxf(m, m_lds[w]);
+  ref = m == kNoLogit ? 0.0f : m;
+  s = 0.0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w)
+    s += s_lds[w] * static_cast<double>(__builtin_amdgcn_exp2f((m_lds[w] - ref) * kLog2eF));
+  const double log_s = log(s);
+  const int label = a.token[row].label;
+  a.lse[t] = static_cast<float>(m + log_s);
+  a.loss[t] = label < 0 ? __builtin_nanf("")
+                        : static_cast<float>(static_cast<double>(m) -
+                                             logits_of(a, row, label & ~3)[label & 3] + log_s);
+}
+
+// g (fp32) of the tokens that have a loss, as kProbs leaves it, from the splits' logits.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void k_nll_grad(NllArgs a) {
+  const int strips = (a.vocab + 3) / 4;
+  const int64_t all = static_cast<int64_t>(a.head->live) * strips;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * THREADS + threadIdx.x; i < all;
+       i += static_cast<int64_t>(gridDim.x) * THREADS) {
+    const int row = static_cast<int>(i / strips), v = static_cast<int>(i % strips) * 4;
+    const f32x4 l = logits_of(a, row, v);
+    const NllToken k = a.token[row];
+    f32x4 g;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float x = __builtin_amdgcn_exp2f((l[j] - k.lse) * kLog2eF) * k.weight;
+      g[j] = v + j >= a.vocab ? 0.0f : v + j == k.label ? k.label_g : x;
+    }
+    *reinterpret_cast<f32x4*>(a.g + (static_cast<int64_t>(row) * a.piece + v) * 4) = g;
+  }
 }
 
 // The piece's rows of dweight from the splits' sums.

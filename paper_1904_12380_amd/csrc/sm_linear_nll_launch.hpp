@@ -6,7 +6,7 @@
 
 namespace smx {
 
-// One of the products (kLogits .. kWeight of sm_linear_nll.hpp) and its shape.
+// One of the products (kLogits .. kPartial of sm_linear_nll.hpp) and its shape.
 struct NllProduct {
   const void* fn;
   int bm, bn, threads;

@@ -31,8 +31,10 @@ NllProduct nll_shape_of(int size) {
     return size == kLarge ? nll_shape<T, KIND, 256, 256, 2, 4, 2>()
                           : nll_shape<T, KIND, 128, 128, 2, 2, 2>();
   } else {
-    return size == kLarge ? nll_shape<T, KIND, 128, 128, 2, 2, 2>()
-                          : nll_shape<T, KIND, 64, 64, 2, 2, 3>();
+    if constexpr (KIND != kPartial) {  // for few tiles
+      if (size == kLarge) return nll_shape<T, KIND, 128, 128, 2, 2, 2>();
+    }
+    return nll_shape<T, KIND, 64, 64, 2, 2, 3>();
   }
 }
 
@@ -44,6 +46,9 @@ NllProduct nll_product_of(int kind, int64_t m, int64_t n) {
   const bool tokens = kind != kWeight;  // n
   const int size = tokens && n <= kNllFew                           ? kNarrow
                    : tiles >= 192 && !(tokens && n <= kEdge / 2) ? kLarge : kSmall;
+  if constexpr (sizeof(T) == 4) {
+    if (kind == kPartial) return nll_shape_of<T, kPartial>(size);
+  }
   switch (kind) {
     case kLogits: return nll_shape_of<T, kLogits>(size);
     case kProbs: return nll_shape_of<T, kProbs>(size);

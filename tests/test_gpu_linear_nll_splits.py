@@ -1,0 +1,87 @@
+"""The loss over a vocabulary where its logits are few tiles, and d of fp32 is split."""
+import pytest
+import torch
+
+import paper_1904_12380_amd as sm
+from oracle import decoder_f64 as oracle
+from tests import decoder_data as data
+from tests.test_gpu_linear_nll import IGNORE, check, inputs
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", list(data.TYPES))
+@pytest.mark.parametrize("rows,vocab,d", [
+    (1, 1, 4096), (1, 5, 520), (1, 2500, 4096), (4, 2500, 4096), (17, 129, 1032), (63, 1001, 2056),
+    (64, 127, 16384), (65, 300, 1160), (257, 257, 2048), (256, 259, 2048), (700, 250, 1024),
+    (1100, 574, 3000), (2500, 9, 1544),
+    (256, 3000, 512), (70, 11000, 520)])
+def test_sizes(rows, vocab, d, dtype):
+    check(*inputs(rows, vocab, d, dtype, ignored=0.2), dtype)
+
+
+@pytest.mark.parametrize("dtype", list(data.TYPES))
+def test_strides(dtype):
+    check(*inputs(70, 203, 1040, dtype, ignored=0.2), dtype, apart=24)
+
+
+@pytest.mark.parametrize("dtype", list(data.TYPES))
+def test_ignored_rows_may_hold_anything(dtype):
+    x, weight, labels, dloss = inputs(90, 203, 1040, dtype, ignored=0.6)
+    x[labels == IGNORE] = torch.nan
+    loss, lse, dx, _ = check(x, weight, labels, dloss, dtype)
+    for t in (loss, lse, dx):
+        assert not t[(labels == IGNORE).cuda()].any()
+    labels[:] = IGNORE
+    for t in check(x, weight, labels, dloss, dtype):
+        assert not t.any()
+
+
+@pytest.mark.parametrize("dtype", list(data.TYPES))
+def test_bad_labels_and_bad_values(dtype):
+    x, weight, labels, dloss = inputs(90, 203, 1040, dtype)
+    labels[3], labels[40] = 203, -7
+    loss, lse, dx, dw = (t.cpu() for t in check(x, weight, labels, dloss, dtype))
+    assert loss[[3, 40]].isnan().all() and lse[[3, 40]].isfinite().all()
+    assert dx[[3, 40]].isnan().all() and dw.isnan().all()
+    x, weight, labels, dloss = inputs(90, 203, 1040, dtype)
+    x[5, 7], x[60] = torch.nan, torch.inf
+    args = [t.cuda() for t in (x, weight, labels)]
+    loss, lse = sm.softmax_linear_nll_fwd(*args)
+    dx, _ = sm.softmax_linear_nll_bwd(dloss.cuda(), *args, loss, lse)
+    exact = oracle.linear_nll(x, weight, labels, IGNORE, dloss)
+    rest = torch.ones(90, dtype=torch.bool)
+    rest[[5, 60]] = False
+    bounds = data.nll_bounds(x[rest], weight, labels[rest], IGNORE, dloss[rest], dtype,
+                             oracle.linear_nll(x[rest], weight, labels[rest], IGNORE, dloss[rest]))
+    for name, got, want, bound in zip(("loss", "lse", "dx"), (loss, lse, dx), exact, bounds):
+        assert got[5].isnan().all() and not got[60].isfinite().any(), name
+        data.close(name, got[rest.cuda()], want[rest], bound)
+
+
+@pytest.mark.parametrize("dtype", list(data.TYPES))
+def test_same_bits_each_time_and_in_a_graph(dtype):
+    x, weight, labels, dloss = (t.cuda() for t in inputs(130, 700, 2056, dtype, ignored=0.3))
+
+    def step():
+        loss, lse = sm.softmax_linear_nll_fwd(x, weight, labels)
+        return [loss, lse, *sm.softmax_linear_nll_bwd(dloss, x, weight, labels, loss, lse)]
+
+    first = step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, out))
+        assert all(torch.equal(a, b) for a, b in zip(first, step()))
+
+
+@pytest.mark.parametrize("dx,dw", [(True, False), (False, True)])
+def test_one_gradient_alone(dx, dw):
+    x, weight, labels, dloss = inputs(100, 300, 2048, "bf16")
+    both = check(x, weight, labels, dloss, "bf16")
+    some = check(x, weight, labels, dloss, "bf16", need_dx=dx, need_dweight=dw)
+    for need, a, b in ((dx, both[2], some[2]), (dw, both[3], some[3])):
+        assert torch.equal(a, b) if need else b is None

@@ -16,3 +16,16 @@ def test_one_row_more_than_a_tile_keeps_the_splits_of_dweight(rows, d, dtype):
     those of its piece of 512, and shares their sums over the tokens out as well: the
     splits' sums are most of the workspace."""
     assert bytes_of(rows, 257, d, dtype) > bytes_of(rows, 256, d, dtype)
+
+
+@pytest.mark.parametrize("what", ["fwd", "bwd"])
+@pytest.mark.parametrize("rows,vocab,d", [(1, 256, 4096), (30, 969, 4096), (4, 2500, 4096),
+                                          (1121, 574, 3000), (256, 3000, 4096)])
+def test_fp32_logits_of_few_tiles_are_split(rows, vocab, d, what):
+    """A workgroup for each of a few tiles would run all of d alone: the workspace has
+    the logits of two splits at least, beside the packed rows and g."""
+    size = getattr(sm.load_library(), f"softmax_linear_nll_{what}_workspace")
+    padded, logits = -(-rows // 256) * 256, -(-rows // 256) * 256 * -(-vocab // 256) * 256 * 4
+    assert size(rows, vocab, d, 0) > padded * d * 4 + 2 * logits
+    # One stage of d cannot be split.
+    assert size(rows, vocab, 32, 0) < size(rows, vocab, d, 0) - 2 * logits
