@@ -216,16 +216,14 @@ struct Product {
 
   typedef typename Operand<T>::type V;
 
-  static constexpr int kOps = kMT * kNT;  // of a step
-
   // The matrix ops of one step, and behind the n-th of them `then(n)`: what is read,
   // and loaded, for later steps.  In this order: the compiler by itself reads each
   // operand right before its use.
-  template <typename F>
-  __device__ __forceinline__ void step(const V (&x)[kMT], const V (&y)[kNT], F then) {
-    unrolled<kOps>([&](auto n) {
+  template <int NT, typename F>
+  __device__ __forceinline__ void step(const V (&x)[kMT], const V (&y)[NT], F then) {
+    unrolled<kMT * NT>([&](auto n) {
       // Rows in turn from either end: one operand stays from op to op.
-      constexpr int i = n / kNT, j = i % 2 == 0 ? n % kNT : kNT - 1 - n % kNT;
+      constexpr int i = n / NT, j = i % 2 == 0 ? n % NT : NT - 1 - n % NT;
       acc[i][j] = multiply(x[i], y[j], acc[i][j]);
       then(n);
       __builtin_amdgcn_sched_barrier(0);
@@ -233,11 +231,14 @@ struct Product {
   }
 
   __device__ __forceinline__ void clear() {
-    unrolled<kOps>([&](auto n) { acc[n / kNT][n % kNT] = f32x4{}; });
+    unrolled<kMT * kNT>([&](auto n) { acc[n / kNT][n % kNT] = f32x4{}; });
   }
 
-  // Adds the products of the next `k` entries of two operands.
+  // Adds the products of the next `k` entries of two operands, of the first NT of a
+  // wavefront's kNT tiles of columns.
+  template <int NT = kNT>
   __device__ __forceinline__ void run(A& a, B& b, char SMX_LDS* lds, int64_t k, int wave) {
+    constexpr int kOps = kMT * NT;  // of a step
     const unsigned at = lds_offset(lds);
     int64_t left = k;  // from the next stage to load on
     auto load = [&](int n, int buf) {
@@ -264,19 +265,19 @@ struct Product {
     }
     staged_but<(STAGES - 1) * kLoads>();
     __builtin_amdgcn_s_barrier();
-    V x[2][kMT], y[2][kNT];
+    V x[2][kMT], y[2][NT];
     const char SMX_LDS* tile = lds;
     // Operands of the next step are read between the first of a step's matrix ops: by
     // its end they have arrived, and nothing waits for them at the barrier.
     auto read = [&](auto n, int to, int s) {
-      if constexpr (n < kNT) y[to][n] = b.read(tile + A::kBytes, s, n);
-      else if constexpr (n < kNT + kMT) x[to][n - kNT] = a.read(tile, s, n - kNT);
+      if constexpr (n < NT) y[to][n] = b.read(tile + A::kBytes, s, n);
+      else if constexpr (n < NT + kMT) x[to][n - NT] = a.read(tile, s, n - NT);
     };
-    unrolled<kMT + kNT>([&](auto n) { read(n, 0, 0); });
+    unrolled<kMT + NT>([&](auto n) { read(n, 0, 0); });
     // The op that a read comes behind; a step of few ops takes several at once.
     auto read_at_op = [&](auto n, int to, int s) {
-      unrolled<kMT + kNT>([&](auto r) {
-        if constexpr (n == r * kOps / (kMT + kNT) * 3 / 4) read(r, to, s);
+      unrolled<kMT + NT>([&](auto r) {
+        if constexpr (n == r * kOps / (kMT + NT) * 3 / 4) read(r, to, s);
       });
     };
     int buf = 0;
@@ -287,14 +288,14 @@ struct Product {
     for (int64_t done = 0; done < k; done += A::kK) {
 #pragma unroll
       for (int s = 0; s < kSteps - 1; ++s)
-        step(x[s % 2], y[s % 2], [&](auto n) { read_at_op(n, (s + 1) % 2, s + 1); });
+        step<NT>(x[s % 2], y[s % 2], [&](auto n) { read_at_op(n, (s + 1) % 2, s + 1); });
       const int next = buf + 1 == STAGES ? 0 : buf + 1;
       tile = lds + next * kStageBytes;
       lds_read();
       staged_but<(STAGES - 2) * kLoads>();
       __builtin_amdgcn_s_barrier();
       ready();
-      step(x[(kSteps - 1) % 2], y[(kSteps - 1) % 2], [&](auto n) {
+      step<NT>(x[(kSteps - 1) % 2], y[(kSteps - 1) % 2], [&](auto n) {
         read_at_op(n, kSteps % 2, 0);
         // Load l behind the op l kOps / kLoads + 2, or the last one.
         unrolled<kLoads>([&](auto l) {
