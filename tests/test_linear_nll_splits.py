@@ -29,3 +29,11 @@ def test_fp32_logits_of_few_tiles_are_split(rows, vocab, d, what):
     assert size(rows, vocab, d, 0) > padded * d * 4 + 2 * logits
     # One stage of d cannot be split.
     assert size(rows, vocab, 32, 0) < size(rows, vocab, d, 0) - 2 * logits
+
+
+@pytest.mark.parametrize("rows", [12, 60])
+def test_splits_of_dx_count_on_both_fp32_workgroups_of_a_cu(rows):
+    """22 narrow tiles of dx: 21 splits nearly fill two workgroups on each of 256 CUs."""
+    vocab, d = 75898, 2816
+    packed, g = 256 * d * 4, 256 * -(-vocab // 256) * 256 * 4
+    assert bytes_of(rows, vocab, d) > packed + g + 20 * 256 * d * 4
