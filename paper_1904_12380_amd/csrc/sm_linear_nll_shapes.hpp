@@ -21,9 +21,11 @@ NllProduct nll_shape() {
 // (forward, 50001 x 2048 of bf16: 64 tokens 44 us, 65 in the next tiles 54).  Otherwise
 // the largest tiles, unless they are too few to fill three quarters of the CUs (351
 // tokens x 10007 x 520 of fp16, 80 large tiles: 21.1 us with them, 13.8 with the small
-// ones) or half of each would be empty (probabilities of 128 tokens x 50001 x 2048 85 us,
-// with small ones 67).  dweight of few tokens keeps the large ones: 128 tokens 111 us,
-// with small ones 123.
+// ones; fp32's run two to a CU, so that takes 384, but for dx, whose splits make up for
+// it: 1000 x 5000 x 1000 with gradients 528 us with 320 large ones, 397 with small ones)
+// or half of each would be empty (probabilities of 128 tokens x 50001 x 2048 85 us, with
+// small ones 67).  dweight of few tokens keeps the large ones: 128 tokens 111 us, with
+// small ones 123.
 constexpr int64_t kNllFew = 64;
 
 template <typename T, int KIND>
@@ -48,8 +50,9 @@ NllProduct nll_product_of(int kind, int64_t m, int64_t n) {
   constexpr int64_t kEdge = sizeof(T) == 2 ? 256 : 128;
   const int64_t tiles = ((m + kEdge - 1) / kEdge) * ((n + kEdge - 1) / kEdge);
   const bool tokens = kind != kWeight;  // n
-  const int size = tokens && n <= kNllFew                           ? kNarrow
-                   : tiles >= 192 && !(tokens && n <= kEdge / 2) ? kLarge : kSmall;
+  const int64_t full = sizeof(T) == 4 && kind != kInput ? 384 : 192;
+  const int size = tokens && n <= kNllFew                            ? kNarrow
+                   : tiles >= full && !(tokens && n <= kEdge / 2) ? kLarge : kSmall;
   if constexpr (sizeof(T) == 4) {
     if (kind == kPartial) return nll_shape_of<T, kPartial>(size);
   }
