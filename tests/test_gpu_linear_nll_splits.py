@@ -142,3 +142,13 @@ def test_few_fp32_tokens_take_no_longer_than_elementary_operations(rows, vocab, 
 
     ours, theirs = shortest([own, lambda: elementary(x, weight, labels, dloss, grads)])
     assert ours < theirs
+
+
+@pytest.mark.parametrize("rows,vocab,d", [(1500, 2433, 520), (1400, 4200, 136), (300, 2000, 2056)])
+def test_fp32_of_a_few_hundred_large_tiles(rows, vocab, d):
+    check(*inputs(rows, vocab, d, "f32", ignored=0.1), "f32")
+
+
+@pytest.mark.parametrize("rows,vocab,d", [(4096, 250, 2048), (3000, 500, 1160)])
+def test_fp32_dweight_of_less_than_a_tile_for_each_cu(rows, vocab, d):
+    check(*inputs(rows, vocab, d, "f32", ignored=0.1), "f32")

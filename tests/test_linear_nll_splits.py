@@ -37,3 +37,10 @@ def test_splits_of_dx_count_on_both_fp32_workgroups_of_a_cu(rows):
     vocab, d = 75898, 2816
     packed, g = 256 * d * 4, 256 * -(-vocab // 256) * 256 * 4
     assert bytes_of(rows, vocab, d) > packed + g + 20 * 256 * d * 4
+
+
+@pytest.mark.parametrize("rows,vocab,d", [(4096, 256, 2048), (3000, 500, 1160)])
+def test_fp32_dweight_of_less_than_a_tile_for_each_cu_is_split(rows, vocab, d):
+    """Beside the packed rows, g and a split of dx: the sums of two splits of dweight."""
+    padded, whole = -(-rows // 256) * 256, -(-vocab // 256) * 256
+    assert bytes_of(rows, vocab, d) > padded * (2 * d + whole) * 4 + 2 * whole * d * 4
