@@ -21,8 +21,10 @@
 // The products are bound by the matrix ops where there are thousands of tokens, by the
 // weight's bytes for up to about a hundred (one token x 50001 x 2048 of bf16: 45 us,
 // 4.5 TB/s); the other kernels move each of their bytes once.  8192 tokens (5% ignored)
-// x 50001 x 2048 of bf16: pack 16 us, logits 1253, join 7; pack 29, probabilities 1426,
-// dx 1216, dweight 1303, join of dx 24.
+// x 50001 x 2048 of bf16: pack 16 us, logits 1250, join 7; pack 29, probabilities 1415,
+// dx 1210, dweight 1300, join of dx 24.  fp32, 4 tokens x 2500 x 4096, in 16 splits of d:
+// pack 4, logits 14, k_nll_total 10; pack 5, logits 14, k_nll_grad 4, dx 15, dweight 20,
+// join of dx 7.
 //
 // The logits are formed in both passes by the same operations in the same order, also
 // where d is split.

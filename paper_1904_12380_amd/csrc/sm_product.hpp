@@ -24,8 +24,8 @@
 // by blocks that lie 1056 bytes apart (Side); a read's address is then one register
 // and constants.
 //
-// What bounds the large tiles is power: on random values the clock is 1.8 GHz, with
-// the matrix pipes busy 64 to 72% of the cycles, and the forward product of 4096 x
+// What bounds the large tiles is power: on random values the clock is 1.8 to 2.0 GHz,
+// with the matrix pipes busy 55 to 72% of the cycles, and the forward product of 4096 x
 // 131072 x 4096 of bf16 runs at 1390 TFLOP/s (on zeros, at the full clock, 1700).
 #pragma once
 
