@@ -116,8 +116,8 @@ Backward backward_room(int64_t rows, int64_t vocab, int64_t d, int dtype) {
   b.piece = piece_of(rows, vocab, d, size);
   b.most = std::min(b.piece, vocab);
   b.splits = splits_of(product(kInput, d, rows, dtype), d, rows, b.most, dtype);
-  // dweight is many tiles, but for a small vocabulary.  Those of fp32 take longer, and a
-  // few stages more pay for splits up to a tile for each CU (4096 tokens x 256 x 2048 with
+  // dweight is many tiles, but for a small vocabulary.  Those of fp32 take longer: splits
+  // of 16 stages pay there up to a tile for each CU (4096 tokens x 256 x 2048 with
   // gradients, 128 tiles: 291 us, split 238).
   const NllProduct w = product(kWeight, d, b.most, dtype);
   const int64_t w_tiles = ceil_div(d, w.bm) * ceil_div(b.most, w.bn);
